@@ -309,6 +309,120 @@ void gnn_embed_destroy(gnn_embedder *m);
 int gnn_frnn(const float *z, int64_t n_nodes, int32_t dim, float r2, int32_t *edge_index,
              int64_t max_pairs, int64_t *n_pairs, hipStream_t stream);
 
+/* ---- linear layers of wide and per-region networks -------------------------
+ * Paper section 2.1: the embedding and the filter are multilayer perceptrons
+ * over hits and candidate edges; the paper gives no widths.  gnn_embed_* and
+ * gnn_filter_* cover networks 64 or 128 wide.  The calls below are their
+ * building blocks for wider networks (to 16384), with weights of 8 or 16 bits,
+ * and for detectors whose regions (barrel and endcap, pixel and strip, pairs of
+ * them for edges) have weights of their own.
+ *
+ * Tables of rows are device memory: a pointer, an element type and a stride in
+ * elements from one row to the next (>= the row's width; the gap between rows
+ * is neither read nor written).  Pointers need the alignment of their elements
+ * only.  Up to 2^30 rows.  All calls are asynchronous on `stream` and allocate
+ * nothing; scratch is the caller's (device memory aligned to 256 bytes, which
+ * the call may overwrite until the stream has passed it; each call in flight
+ * needs its own), so calls may overlap and may be captured into graphs.
+ * Outputs must not overlap inputs.  Results are bitwise deterministic. */
+#define GNN_F16 2  /* element and weight type: IEEE half precision               */
+#define GNN_INT8 3 /* whole numbers -127..127, with fp32 scales beside them      */
+
+/* Rows to 8 bits.  scales[m] = max |x[m][k]| / 127 rounded to fp32, and
+ * q[m][k] = the whole number nearest to x[m][k] / scales[m], ties to even (the
+ * exact quotient's).  A row whose scale would be below 2^-126 gets scale 0 and
+ * zeros; a row with an infinity or a NaN gets scale NaN and zeros, so that its
+ * products are NaN and no other row's are touched.  x_type GNN_FP32, GNN_BF16
+ * or GNN_F16.  Runs on the current device.  GNN_E_INVALID_ARG for bad counts,
+ * types, strides or pointers; GNN_E_UNSUPPORTED above 2^30 rows. */
+int gnn_quantize_rows(const void *x, int32_t x_type, int64_t x_stride, int64_t n_rows,
+                      int32_t width, int8_t *q, int64_t q_stride, float *scales,
+                      hipStream_t stream);
+
+/* The rows in the order of their groups: group_ids [n_rows] int32 gives each
+ * row's group.  order [n_rows] lists the rows by ascending group, ascending
+ * within a group; offsets [n_groups + 1]: group g's rows are
+ * order[offsets[g] .. offsets[g + 1] - 1].  Rows whose id is outside
+ * [0, n_groups) have no group; they come last, from offsets[n_groups] on.
+ * n_groups 1..4096.  Runs on the current device.  workspace:
+ * gnn_group_workspace bytes (may be 0; 0 also for bad arguments). */
+size_t gnn_group_workspace(int64_t n_rows, int32_t n_groups);
+int gnn_group_rows(const int32_t *group_ids, int64_t n_rows, int32_t n_groups, int32_t *offsets,
+                   int32_t *order, void *workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* One linear layer with a weight set per group:
+ *   16-bit weights: y = t(W_g) t(x) + b_g, t rounding to the weight type;
+ *                   products and sums in fp32
+ *   GNN_INT8:       y[n] = xs ws_g[n] sum_k q(x)[k] q(W_g)[n][k] + b_g[n], rows
+ *                   (scale xs) and the weights of each output channel (scale
+ *                   ws_g[n]) to 8 bits as by gnn_quantize_rows; the sum in int32
+ *                   (exact). */
+typedef struct gnn_linear_dims {
+  uint32_t struct_size; /* = sizeof(gnn_linear_dims)                         */
+  int32_t in_features;  /* 1..16384                                           */
+  int32_t out_features; /* 1..16384                                           */
+  int32_t n_groups;     /* weight sets, 1..4096                               */
+  int32_t dtype;        /* GNN_BF16, GNN_F16 or GNN_INT8                      */
+} gnn_linear_dims;
+typedef struct gnn_linear gnn_linear;
+
+/* Floats in the blob: for each group W [out][in], then b [out]; 0 if dims are
+ * invalid. */
+size_t gnn_linear_weight_count(const gnn_linear_dims *dims);
+/* Converts, lays out and uploads the HOST fp32 blob to the current device;
+ * NULL on error (gnn_last_error). */
+gnn_linear *gnn_linear_create(const float *weights, const gnn_linear_dims *dims);
+/* Scratch bytes of gnn_linear_apply for rows of that type and number; often 0. */
+size_t gnn_linear_workspace(const gnn_linear *l, int32_t x_type, int64_t n_rows);
+/* y [n_rows][out] from x [n_rows][in], on the layer's device.
+ *   x_type   GNN_FP32, GNN_BF16 or GNN_F16; for GNN_INT8 layers also GNN_INT8
+ *            (with x_scales [n_rows], as gnn_quantize_rows gives them; NULL for
+ *            the other types)
+ *   offsets  [n_groups + 1] ascending, or NULL with one group (all rows): group
+ *            g's rows are at positions offsets[g] .. offsets[g + 1] - 1
+ *   order    [n_rows], or NULL: position p is row order[p], of x and of y alike
+ * Rows of no group are left as they were in y.  Offsets and order entries out
+ * of range are clamped (no fault, meaningless rows); a row that several
+ * positions name gets the result of one of them.
+ * y_type GNN_FP32, GNN_BF16 or GNN_F16, rounded once from fp32. */
+int gnn_linear_apply(gnn_linear *l, const void *x, int32_t x_type, int64_t x_stride,
+                     const float *x_scales, int64_t n_rows, const int32_t *offsets,
+                     const int32_t *order, void *y, int32_t y_type, int64_t y_stride,
+                     void *workspace, int64_t workspace_bytes, hipStream_t stream);
+void gnn_linear_destroy(gnn_linear *l); /* waits for the device; NULL-safe */
+
+/* A whole network of such layers, with LayerNorm and ReLU between them as in
+ * the other networks here: z = W_L phi(... phi(W_1 x + b_1) ...) + b_L, every
+ * layer with one parameter set per group.  It groups the rows by their ids,
+ * and hands 8-bit layers rows that leave the LayerNorm in 8 bits.  Its output
+ * is, for example, the embedding that gnn_frnn searches. */
+#define GNN_MLP_MAX_LAYERS 8
+typedef struct gnn_mlp_dims {
+  uint32_t struct_size;                      /* = sizeof(gnn_mlp_dims)         */
+  int32_t n_layers;                          /* 1..GNN_MLP_MAX_LAYERS           */
+  int32_t widths[GNN_MLP_MAX_LAYERS + 1];    /* widths[0] in, widths[n_layers]
+                                                out (1..16384); hidden 1..4096  */
+  int32_t n_groups;                          /* 1..4096                         */
+  int32_t dtype;                             /* GNN_BF16, GNN_F16 or GNN_INT8   */
+  float ln_eps;                              /* LayerNorm epsilon               */
+} gnn_mlp_dims;
+typedef struct gnn_mlp gnn_mlp;
+
+/* Floats in the blob: for each layer, for each group: W [out][in], b [out] and,
+ * in all but the last layer, gamma [out], beta [out]; 0 if dims are invalid. */
+size_t gnn_mlp_weight_count(const gnn_mlp_dims *dims);
+gnn_mlp *gnn_mlp_create(const float *weights, const gnn_mlp_dims *dims); /* HOST blob */
+size_t gnn_mlp_workspace(const gnn_mlp *m, int32_t x_type, int64_t n_rows);
+/* y [n_rows][widths[n_layers]] from x [n_rows][widths[0]], on the network's
+ * device.  group_ids [n_rows] int32 as for gnn_group_rows with several groups,
+ * NULL with one; rows of no group are left as they were in y.  Pre-activations
+ * are held in fp32; what a hidden layer hands on is rounded to the weight type. */
+int gnn_mlp_apply(gnn_mlp *m, const void *x, int32_t x_type, int64_t x_stride,
+                  const int32_t *group_ids, int64_t n_rows, void *y, int32_t y_type,
+                  int64_t y_stride, void *workspace, int64_t workspace_bytes,
+                  hipStream_t stream);
+void gnn_mlp_destroy(gnn_mlp *m); /* waits for the device; NULL-safe */
+
 /* ---- serving: a request queue in front of several model instances --------
  * Paper sections 2.3 and 3.2: the GNN runs as a service, one GPU holding
  * several instances of the model (Fig. 4b) behind a queue of requests from

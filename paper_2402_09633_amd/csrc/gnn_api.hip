@@ -44,6 +44,15 @@ int fail(int code, const char *fmt, ...) {
 
 }  // namespace
 
+int gnn::cu_count(int dev) {
+  int n = 0;
+  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) {
+    (void)hipGetLastError();
+    n = 256;
+  }
+  return n;
+}
+
 int gnn::set_error(int code, const char *msg) { return fail(code, "%s", msg ? msg : ""); }
 
 namespace {
@@ -503,18 +512,6 @@ LayerDev fix_layer(const LayerOff &o, const unsigned char *base) {
 MlpDev fix_mlp(const MlpOff &o, const unsigned char *base) {
   return MlpDev{fix_layer(o.l0, base), fix_layer(o.l1, base)};
 }
-
-struct DeviceGuard {
-  int prev = -1;
-  explicit DeviceGuard(int dev) {
-    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
-    if (prev != dev) (void)hipSetDevice(dev);
-  }
-  ~DeviceGuard() {
-    int cur = -1;
-    if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
-  }
-};
 
 size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
 
@@ -2023,15 +2020,6 @@ struct SmallMlpOff {
     return m;
   }
 };
-
-int cu_count(int dev) {
-  int n = 0;
-  if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) {
-    (void)hipGetLastError();
-    n = 256;
-  }
-  return n;
-}
 
 }  // namespace
 

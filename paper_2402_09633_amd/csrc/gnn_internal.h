@@ -342,6 +342,83 @@ hipError_t launch_frnn_pairs(const FrnnArgs &a, hipStream_t stream);
 hipError_t launch_wcc(const int32_t *edge_index, const float *scores, float threshold,
                       int64_t n_edges, int32_t n_nodes, int32_t *labels, hipStream_t stream);
 
+// ---- row operators (rows.hip, linear.hip) ----
+// Element types GNN_FP32, GNN_BF16, GNN_F16 and GNN_INT8 by number.
+inline int type_bytes(int t) { return t == 0 ? 4 : t == 3 ? 1 : 2; }
+
+// Rows to 8 bits with a scale each (rows_common.h).
+struct QuantArgs {
+  const void *x = nullptr;
+  int32_t x_type = 0;
+  int64_t x_stride = 0;  // elements
+  int64_t n = 0;
+  int32_t K = 0;
+  int8_t *q = nullptr;
+  int64_t q_stride = 0;  // K <= q_stride; columns K .. pad - 1 are zeroed
+  int32_t pad = 0;       // 0: none
+  float *scales = nullptr;
+};
+hipError_t launch_quantize(const QuantArgs &a, hipStream_t stream);
+
+// Rows in the order of their groups (rows.hip).
+struct GroupArgs {
+  const int32_t *ids = nullptr;
+  int64_t n = 0;
+  int32_t G = 0;
+  int32_t *offsets = nullptr, *order = nullptr;
+  int32_t *counts = nullptr;  // scratch, group_scratch_bytes
+};
+size_t group_scratch_bytes(int64_t n, int32_t G);
+hipError_t launch_group(const GroupArgs &a, hipStream_t stream);
+
+// LayerNorm and ReLU of the rows of a hidden layer (rows.hip): fp32 rows x
+// [n][H] in group order to rows of 16 bits, or of 8 with a scale each.
+struct NormArgs {
+  const float *x = nullptr;
+  int64_t n = 0;
+  int32_t H = 0, G = 1;
+  const float *gamma = nullptr, *beta = nullptr;  // [G][H]
+  const int32_t *ids = nullptr, *order = nullptr;  // group of position p: ids[order[p]]
+  const int32_t *n_in = nullptr;  // device: rows that have a group (nullptr: n)
+  float eps = 1e-5f;
+  void *y = nullptr;
+  int32_t y_type = 0;
+  float *scales = nullptr;
+};
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream);
+
+// A linear layer, one weight set per group (linear.hip).
+struct LinearArgs {
+  const void *w = nullptr;        // fragments [G][NB][S][64 lanes][16 bytes]
+  const float *ws = nullptr;      // channel scales [G][32 NB] (8-bit weights)
+  const float *bias = nullptr;    // [G][32 NB]
+  int32_t K = 0, N = 0, NB = 0, S = 0, G = 1;
+  int32_t w_type = 0;
+  const void *x = nullptr;
+  int32_t x_type = 0;
+  int64_t x_stride = 0;           // elements
+  const float *xs = nullptr;      // row scales (8-bit rows)
+  // position p of the group order reads row order[p] (nullptr: p) and writes
+  // row y_order[p]
+  const int32_t *off = nullptr, *order = nullptr, *y_order = nullptr;
+  int32_t n = 0;
+  void *y = nullptr;
+  int32_t y_type = 0;
+  int64_t y_stride = 0;
+  int32_t chunk = 0;              // bytes of a row staged at a time
+  int32_t nsplit = 1;             // workgroups that share the output blocks of a row tile
+};
+// Bytes of a layer's fragments, and the steps of 32 bytes of a row.
+int32_t linear_steps(int32_t K, int w_type);
+size_t linear_frag_bytes(int32_t K, int32_t N, int32_t G, int w_type);
+// Lays out `blob` (device fp32, per group W [N][K] and b [N]).
+hipError_t launch_linear_layout(const float *blob, const LinearArgs &a, void *w, float *ws,
+                                float *bias, hipStream_t stream);
+// Whether rows of this width are too wide to be rounded to 8 bits while they
+// are staged.
+bool linear_needs_rows8(const LinearArgs &a);
+hipError_t launch_linear(const LinearArgs &a, int n_cu, hipStream_t stream);
+
 // flag <- 1 if any of the 2*n_edges indices lies outside [0, n_nodes).
 hipError_t launch_validate(const int32_t *edge_index, int64_t n_edges, int32_t n_nodes,
                            int32_t *flag, hipStream_t stream);
@@ -356,6 +433,22 @@ void ws_forget_stream(gnn_handle *h, hipStream_t stream);
 // gnn_infer for one of several calls that share the GPU (NodeArgs::pack).
 int infer_shared(gnn_handle *h, const float *node_feat, const int32_t *edge_index, int64_t n_nodes,
                  int64_t n_edges, float *edge_scores, hipStream_t stream);
+
+// Makes `dev` the current device for its lifetime (host).
+struct DeviceGuard {
+  int prev = -1;
+  explicit DeviceGuard(int dev) {
+    if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+    if (prev != dev) (void)hipSetDevice(dev);
+  }
+  ~DeviceGuard() {
+    int cur = -1;
+    if (prev >= 0 && hipGetDevice(&cur) == hipSuccess && cur != prev) (void)hipSetDevice(prev);
+  }
+};
+
+// Compute units of device `dev` (256 if it cannot be asked).
+int cu_count(int dev);
 
 // Sets the calling thread's gnn_last_error() text; returns code (host).
 int set_error(int code, const char *msg);

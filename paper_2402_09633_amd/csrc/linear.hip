@@ -1,0 +1,368 @@
+// Linear layers of wide and per-region networks: y = W_g x + b_g for the rows
+// of every group g, with weights of 8 bits (one scale for each output channel,
+// rows rounded to 8 bits with a scale of their own) or of 16.
+//
+//   8 bits:  y[m][n] = xs[m] ws[n] sum_k q(x)[m][k] q(W)[n][k] + b[n]
+//   16 bits: y[m][n] = sum_k t(x[m][k]) t(W[n][k]) + b[n]
+//
+// with the sums in int32 (exact) and fp32.
+#include <type_traits>
+
+#include "rows_common.h"
+
+namespace gnn {
+namespace {
+
+constexpr int WAVES = 4;
+constexpr int CHUNK = 4096;  // most bytes of a row staged at a time
+constexpr int LDS_PAD = 16;  // bytes between staged rows: 16-byte slots of 8 rows differ
+
+template <int WT>
+struct Mma {
+  typedef f16v acc;
+};
+template <>
+struct Mma<T_I8> {
+  typedef i16v acc;
+};
+
+// 32 output channels x 32 rows over 32 bytes of a row: lane l supplies 16
+// bytes of channel l % 32 and of row l % 32 from byte 16 (l / 32) on.
+template <int WT>
+__device__ __forceinline__ void mma(typename Mma<WT>::acc &c, const i4 &w, const i4 &x) {
+  if constexpr (WT == T_I8)
+    c = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x, c, 0, 0, 0);
+  else if constexpr (WT == T_BF16)
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, w),
+                                                __builtin_bit_cast(bf8, x), c, 0, 0, 0);
+  else
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, w), __builtin_bit_cast(h8, x),
+                                               c, 0, 0, 0);
+}
+
+// Stages PM rows of a tile in LDS as the products read them, bytes
+// [0, chunk) of a row from element k0 on.  A wave takes 64 / L rows at a
+// time, L lanes to a row, C units of eight elements to a lane; with QUANT the
+// row's scale is formed from the same registers.  B such passes are loaded
+// before the first is stored.
+template <int WT, int XT, bool QUANT, int C, int B>
+__device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *rows, float *scale,
+                                           unsigned char *lds, int pitch, int PM, int k0, int kn) {
+  typedef typename std::conditional<WT == T_I8, u2, u4>::type unit;
+  const int units = (kn + 7) / 8;
+  int L = 64;
+  if (C == 1)
+    while (L / 2 >= units) L /= 2;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = 64 / L;
+  const int sub = lane / L, u0 = lane % L;
+  const int cap = (int)(pitch - LDS_PAD) / (int)sizeof(unit);  // units a staged row holds
+  for (int r = wave * per + sub; r < PM; r += WAVES * per * B) {
+    Raw8<XT> raw[B][C];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int rr = min(r + b * WAVES * per, PM - 1);
+      const elem_t<XT> *row = (const elem_t<XT> *)a.x + (int64_t)rows[rr] * a.x_stride + k0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) raw[b][c] = load8<XT>(row, 8 * (u0 + 64 * c), kn);
+    }
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+      const int rr = r + b * WAVES * per;
+      float s = 0.f, inv = 0.f;
+      if constexpr (QUANT) {
+        float top = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) top = max_abs8(to_f32<XT>(raw[b][c]), top);
+        for (int m = L / 2; m; m /= 2)
+          top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
+        s = quant_scale(top);
+        inv = quant_inv(s);
+        if (u0 == 0 && rr < PM) scale[rr] = s;
+      }
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int u = u0 + 64 * c;
+        unit q;
+        if constexpr (XT == WT)
+          q = __builtin_bit_cast(unit, raw[b][c].v);
+        else if constexpr (WT == T_I8)
+          q = quantize8(to_f32<XT>(raw[b][c]), s, inv);
+        else if constexpr (WT == T_BF16)
+          q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[b][c]), bf8));
+        else
+          q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[b][c]), h8));
+        if (rr < PM && u < cap) *(unit *)(lds + rr * pitch + u * (int)sizeof(unit)) = q;
+      }
+    }
+    // units past the last lane's: zeros up to the staged width
+    for (int b = 0; b < B; ++b)
+      if (r + b * WAVES * per < PM)
+        for (int u = u0 + L * C; u < cap; u += L)
+          *(unit *)(lds + (r + b * WAVES * per) * pitch + u * (int)sizeof(unit)) = unit{};
+  }
+}
+
+template <int WT, int XT, bool QUANT>
+__device__ __forceinline__ void stage(const LinearArgs &a, const int32_t *rows, float *scale,
+                                      unsigned char *lds, int pitch, int PM, int k0, int kn) {
+  const int units = (kn + 7) / 8;
+  if (units <= 64)
+    stage_rows<WT, XT, QUANT, 1, 4>(a, rows, scale, lds, pitch, PM, k0, kn);
+  else if (units <= 128)
+    stage_rows<WT, XT, QUANT, 2, 2>(a, rows, scale, lds, pitch, PM, k0, kn);
+  else if (units <= 256)
+    stage_rows<WT, XT, QUANT, 4, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
+  else
+    stage_rows<WT, XT, QUANT, 8, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
+}
+
+template <int T>
+__device__ __forceinline__ void store4(void *y, int64_t at, const f4 &v, int left) {
+  typedef elem_t<T> vec __attribute__((ext_vector_type(4)));
+  elem_t<T> *p = (elem_t<T> *)y + at;
+  const vec o = __builtin_convertvector(v, vec);
+  if (left >= 4) {
+    __builtin_memcpy(p, &o, sizeof o);
+  } else {
+#pragma unroll
+    for (int t = 0; t < 3; ++t)
+      if (t < left) p[t] = o[t];
+  }
+}
+
+// One row tile (PM = 32 RB rows of one group) by all waves: the rows are
+// staged once (chunk by chunk where they do not fit), the weights come from
+// the caches in fragment order, NBW blocks of 32 channels to a wave at a time.
+template <int WT, int XT, int RB, int NBW>
+__global__ __launch_bounds__(64 * WAVES, 2) void linear_panel(LinearArgs a) {
+  constexpr int PM = 32 * RB;
+  typedef typename Mma<WT>::acc acc_t;
+  constexpr bool QUANT = WT == T_I8 && XT != T_I8;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ int32_t rows[PM], yrows[PM];
+  __shared__ float scale[PM];
+  const int bid = xcd_remap(blockIdx.x, gridDim.x);
+  const int tile = bid / a.nsplit, split = bid % a.nsplit;
+  const TileRows t = find_tile(a.off, a.G, a.n, tile, PM);
+  if (t.r0 >= t.r1) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int nrow = min(PM, t.r1 - t.r0);
+  if (tid < PM) {
+    const int p = t.r0 + min(tid, nrow - 1);
+    const int r = a.order ? clamp_idx(a.order[p], a.n) : p;
+    rows[tid] = r;
+    yrows[tid] = a.y_order ? clamp_idx(a.y_order[p], a.n) : p;
+    if (WT == T_I8 && !QUANT) scale[tid] = a.xs[r];
+  }
+  const int pitch = a.chunk + LDS_PAD;
+  const int esz = WT == T_I8 ? 1 : 2;
+  const int steps = a.chunk / 32;  // of a chunk
+  const int nchunk = (a.S + steps - 1) / steps;
+  const int ntile = (a.NB + WAVES * NBW - 1) / (WAVES * NBW);
+  const int col = lane & 31, hh = lane >> 5;
+  const unsigned char *xl = smem + col * pitch + hh * 16;
+  __syncthreads();
+  for (int nt = split; nt < ntile; nt += a.nsplit) {
+    const int nb0 = (nt * WAVES + wave) * NBW;
+    const bool live = nb0 < a.NB;
+    acc_t acc[NBW][RB];
+#pragma unroll
+    for (int i = 0; i < NBW; ++i)
+#pragma unroll
+      for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[i][r][v] = 0;
+    const i4 *wf[NBW];
+#pragma unroll
+    for (int i = 0; i < NBW; ++i)
+      wf[i] = (const i4 *)a.w + ((int64_t)t.g * a.NB + min(nb0 + i, a.NB - 1)) * a.S * 64 + lane;
+    for (int ch = 0; ch < nchunk; ++ch) {
+      if (nchunk > 1 || nt == split) {
+        if (nchunk > 1) __syncthreads();
+        const int k0 = ch * (a.chunk / esz);
+        stage<WT, XT, QUANT>(a, rows, scale, smem, pitch, PM, k0, min(a.K - k0, a.chunk / esz));
+        __syncthreads();
+      }
+      if (live) {
+        const int s0 = ch * steps, s1 = min(steps, a.S - s0);
+        for (int s = 0; s < s1; s += 2) {
+          i4 w[2][NBW], x[2][RB];
+#pragma unroll
+          for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int i = 0; i < NBW; ++i) w[d][i] = wf[i][(s0 + s + d) * 64];
+#pragma unroll
+          for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int r = 0; r < RB; ++r)
+              x[d][r] = *(const i4 *)(xl + r * 32 * pitch + (s + d) * 32);
+#pragma unroll
+          for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int i = 0; i < NBW; ++i)
+#pragma unroll
+              for (int r = 0; r < RB; ++r) mma<WT>(acc[i][r], w[d][i], x[d][r]);
+        }
+      }
+    }
+    if (!live) continue;
+#pragma unroll
+    for (int i = 0; i < NBW; ++i) {
+      if (nb0 + i >= a.NB) break;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int f = (nb0 + i) * 32 + 8 * q + 4 * hh;
+        const int64_t fo = (int64_t)t.g * a.NB * 32 + f;
+        const f4 b = *(const f4 *)(a.bias + fo);
+        f4 ws = {1.f, 1.f, 1.f, 1.f};
+        if constexpr (WT == T_I8) ws = *(const f4 *)(a.ws + fo);
+#pragma unroll
+        for (int r = 0; r < RB; ++r) {
+          const int row = r * 32 + col;
+          f4 v;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            v[k] = (float)acc[i][r][4 * q + k];
+            if constexpr (WT == T_I8) v[k] *= scale[row] * ws[k];
+            v[k] += b[k];
+          }
+          if (row < nrow && f < a.N) {
+            const int64_t at = (int64_t)yrows[row] * a.y_stride + f;
+            if (a.y_type == T_F32)
+              store4<T_F32>(a.y, at, v, a.N - f);
+            else if (a.y_type == T_BF16)
+              store4<T_BF16>(a.y, at, v, a.N - f);
+            else
+              store4<T_F16>(a.y, at, v, a.N - f);
+          }
+        }
+      }
+    }
+  }
+}
+
+// Weight fragments of one block of 32 channels of one group: [S][64][16
+// bytes], lane l holding channel l % 32 from byte 16 (l / 32) of the step on.
+template <int WT>
+__global__ __launch_bounds__(256) void linear_layout(const float *__restrict__ blob, LinearArgs a,
+                                                     unsigned char *w, float *ws, float *bias) {
+  const int nb = blockIdx.x, g = blockIdx.y, tid = threadIdx.x;
+  const float *W = blob + (int64_t)g * ((int64_t)a.N * a.K + a.N);
+  const float *bs = W + (int64_t)a.N * a.K;
+  const int row = tid / 8, part = tid % 8;
+  const int n = nb * 32 + row;
+  __shared__ float sc[32];
+  if constexpr (WT == T_I8) {
+    uint32_t top = 0;
+    if (n < a.N)
+      for (int k = part; k < a.K; k += 8)
+        top = max(top, __float_as_uint(W[(int64_t)n * a.K + k]) & 0x7fffffffu);
+    for (int m = 4; m; m /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m));
+    if (part == 0) {
+      sc[row] = quant_scale(__uint_as_float(top));
+      ws[((int64_t)g * a.NB + nb) * 32 + row] = sc[row];
+    }
+    __syncthreads();
+  }
+  if (tid < 32)
+    bias[((int64_t)g * a.NB + nb) * 32 + tid] = nb * 32 + tid < a.N ? bs[nb * 32 + tid] : 0.f;
+  unsigned char *out = w + ((int64_t)g * a.NB + nb) * a.S * 1024;
+  constexpr int PER = WT == T_I8 ? 16 : 8;  // elements of 16 bytes
+  for (int i = tid; i < a.S * 64; i += 256) {
+    const int ln = i & 63, s = i >> 6;
+    const int ch = ln % 32, c = nb * 32 + ch;
+    const int k0 = (2 * s + ln / 32) * PER;
+    f8 v[PER / 8];
+#pragma unroll
+    for (int h = 0; h < PER / 8; ++h)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int k = k0 + 8 * h + j;
+        v[h][j] = c < a.N && k < a.K ? W[(int64_t)c * a.K + k] : 0.f;
+      }
+    u4 q;
+    if constexpr (WT == T_I8) {
+      const float sch = sc[ch], inv = quant_inv(sch);
+      const u2 lo = quantize8(v[0], sch, inv), hi = quantize8(v[PER / 8 - 1], sch, inv);
+      q = u4{lo[0], lo[1], hi[0], hi[1]};
+    } else if constexpr (WT == T_BF16) {
+      q = __builtin_bit_cast(u4, __builtin_convertvector(v[0], bf8));
+    } else {
+      q = __builtin_bit_cast(u4, __builtin_convertvector(v[0], h8));
+    }
+    *(u4 *)(out + (int64_t)i * 16) = q;
+  }
+}
+
+template <int WT, int XT, int RB>
+hipError_t panel(const LinearArgs &a, int64_t tiles, hipStream_t stream) {
+  const size_t lds = (size_t)32 * RB * (a.chunk + LDS_PAD);
+  return launch_lds(linear_panel<WT, XT, RB, 2>, dim3((uint32_t)(tiles * a.nsplit)),
+                    dim3(64 * WAVES), lds, stream, a);
+}
+
+template <int WT, int XT>
+hipError_t panel_rows(const LinearArgs &a, int RB, int64_t tiles, hipStream_t stream) {
+  if (RB == 4) return panel<WT, XT, 4>(a, tiles, stream);
+  if (RB == 2) return panel<WT, XT, 2>(a, tiles, stream);
+  return panel<WT, XT, 1>(a, tiles, stream);
+}
+
+}  // namespace
+
+int32_t linear_steps(int32_t K, int w_type) {
+  const int per = w_type == T_I8 ? 64 : 32;  // elements of two steps
+  return 2 * ((K + per - 1) / per);
+}
+
+size_t linear_frag_bytes(int32_t K, int32_t N, int32_t G, int w_type) {
+  return (size_t)G * ((N + 31) / 32) * linear_steps(K, w_type) * 1024;
+}
+
+hipError_t launch_linear_layout(const float *blob, const LinearArgs &a, void *w, float *ws,
+                                float *bias, hipStream_t stream) {
+  const dim3 grid(a.NB, a.G);
+  if (a.w_type == T_I8)
+    return launch(linear_layout<T_I8>, grid, dim3(256), 0, stream, blob, a, (unsigned char *)w, ws,
+                  bias);
+  if (a.w_type == T_BF16)
+    return launch(linear_layout<T_BF16>, grid, dim3(256), 0, stream, blob, a, (unsigned char *)w,
+                  ws, bias);
+  return launch(linear_layout<T_F16>, grid, dim3(256), 0, stream, blob, a, (unsigned char *)w, ws,
+                bias);
+}
+
+bool linear_needs_rows8(const LinearArgs &a) { return a.S * 32 > CHUNK; }
+
+hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
+  LinearArgs a = args;
+  // The rows of a tile stay in LDS: 128 of them where they fit in half of it
+  // (two workgroups to a CU), fewer of wide ones and where there are few.
+  constexpr int HALF = 78 * 1024;
+  const int row_bytes = a.S * 32;
+  a.chunk = row_bytes < CHUNK ? row_bytes : CHUNK;
+  int RB = 4;
+  while (RB > 1 && (32 * RB * (a.chunk + LDS_PAD) > HALF || a.n / a.G <= 16 * RB)) RB /= 2;
+  const int64_t PM = 32 * RB;
+  const int64_t tiles = a.off ? a.n / PM + a.G : (a.n + PM - 1) / PM;
+  const int ntile = (a.NB + 2 * WAVES - 1) / (2 * WAVES);
+  a.nsplit = (int)((2 * n_cu + tiles - 1) / tiles);
+  if (a.nsplit > ntile) a.nsplit = ntile;
+  if (a.w_type == T_I8) {
+    if (a.x_type == T_I8) return panel_rows<T_I8, T_I8>(a, RB, tiles, stream);
+    if (a.x_type == T_F32) return panel_rows<T_I8, T_F32>(a, RB, tiles, stream);
+    if (a.x_type == T_BF16) return panel_rows<T_I8, T_BF16>(a, RB, tiles, stream);
+    return panel_rows<T_I8, T_F16>(a, RB, tiles, stream);
+  }
+  if (a.w_type == T_BF16) {
+    if (a.x_type == T_F32) return panel_rows<T_BF16, T_F32>(a, RB, tiles, stream);
+    if (a.x_type == T_BF16) return panel_rows<T_BF16, T_BF16>(a, RB, tiles, stream);
+    return panel_rows<T_BF16, T_F16>(a, RB, tiles, stream);
+  }
+  if (a.x_type == T_F32) return panel_rows<T_F16, T_F32>(a, RB, tiles, stream);
+  if (a.x_type == T_BF16) return panel_rows<T_F16, T_BF16>(a, RB, tiles, stream);
+  return panel_rows<T_F16, T_F16>(a, RB, tiles, stream);
+}
+
+}  // namespace gnn

@@ -1,0 +1,348 @@
+// Row operators that feed the linear layers (linear.hip): rows rounded to 8
+// bits with a scale each, and rows put in the order of their groups.
+#include "rows_common.h"
+
+namespace gnn {
+namespace {
+
+// ---- rows to 8 bits ----
+// One pass over the rows: L lanes hold a row (C units of eight elements
+// each), form its largest absolute value and round the values they hold.  B
+// rows are loaded before the first is reduced, so that a wave keeps several
+// loads in flight.  Bound by memory: x is read and q written once.
+constexpr int Q_WAVES = 4;
+
+__device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q) {
+  if (k + 8 <= K) {
+    __builtin_memcpy(row + k, &q, 8);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (k + j < K) row[k + j] = (int8_t)(q[j / 4] >> (8 * (j % 4)));
+  }
+}
+
+template <int XT, int C, int B>
+__global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = 64 / L, sub = lane / L, u0 = lane % L;
+  const int64_t r0 = ((int64_t)blockIdx.x * Q_WAVES + wave) * per * B + sub;
+  const int width = a.pad ? a.pad : a.K;
+  Raw8<XT> raw[B][C];
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    const int64_t r = min(r0 + (int64_t)b * per, a.n - 1);
+    const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
+#pragma unroll
+    for (int c = 0; c < C; ++c) raw[b][c] = load8<XT>(row, 8 * (u0 + 64 * c), a.K);
+  }
+#pragma unroll
+  for (int b = 0; b < B; ++b) {
+    const int64_t r = r0 + (int64_t)b * per;
+    float top = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) top = max_abs8(to_f32<XT>(raw[b][c]), top);
+    for (int m = L / 2; m; m /= 2)
+      top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
+    const float s = quant_scale(top), inv = quant_inv(s);
+    if (r >= a.n) continue;
+    if (u0 == 0) a.scales[r] = s;
+    int8_t *q = a.q + r * a.q_stride;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      store_q8(q, 8 * (u0 + 64 * c), width, quantize8(to_f32<XT>(raw[b][c]), s, inv));
+    for (int u = u0 + L * C; 8 * u < width; u += L) store_q8(q, 8 * u, width, u2{0u, 0u});
+  }
+}
+
+// Rows too wide for a wave's registers: one workgroup to a row, which is read
+// twice (the second time from the caches).
+template <int XT>
+__global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
+  __shared__ float part[Q_WAVES];
+  const int tid = threadIdx.x;
+  const int64_t r = blockIdx.x;
+  const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
+  float top = 0.f;
+  for (int k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
+    top = max_abs8(to_f32<XT>(load8<XT>(row, k, a.K)), top);
+  for (int m = 32; m; m /= 2)
+    top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
+  if ((tid & 63) == 0) part[tid >> 6] = top;
+  __syncthreads();
+  for (int w = 0; w < Q_WAVES; ++w)
+    top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(part[w])));
+  const float s = quant_scale(top), inv = quant_inv(s);
+  if (tid == 0) a.scales[r] = s;
+  int8_t *q = a.q + r * a.q_stride;
+  const int width = a.pad ? a.pad : a.K;
+  for (int k = 8 * tid; k < width; k += 8 * 64 * Q_WAVES)
+    store_q8(q, k, width, quantize8(to_f32<XT>(load8<XT>(row, k, a.K)), s, inv));
+}
+
+template <int XT>
+hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
+  const int units = (a.K + 7) / 8;
+  int L = 64;
+  while (L / 2 >= units) L /= 2;
+  auto grid = [&](int B) {
+    const int64_t rows = (int64_t)Q_WAVES * (64 / L) * B;
+    return dim3((uint32_t)((a.n + rows - 1) / rows));
+  };
+  const dim3 block(64 * Q_WAVES);
+  if (units <= 64) return launch(quantize_rows<XT, 1, 4>, grid(4), block, 0, stream, a, L);
+  if (units <= 128) return launch(quantize_rows<XT, 2, 2>, grid(2), block, 0, stream, a, L);
+  if (units <= 256) return launch(quantize_rows<XT, 4, 1>, grid(1), block, 0, stream, a, L);
+  if (units <= 512) return launch(quantize_rows<XT, 8, 1>, grid(1), block, 0, stream, a, L);
+  return launch(quantize_wide<XT>, dim3((uint32_t)a.n), block, 0, stream, a);
+}
+
+// ---- LayerNorm and ReLU of hidden rows ----
+// A wave to a row: mean, then variance of the centred values, both in fp32
+// from registers (C units of eight a lane; rows of up to 4096).
+template <int YT, int C>
+__device__ __forceinline__ void norm_row(const NormArgs &a, int64_t p, int lane) {
+  int32_t g = 0;
+  if (a.ids) g = clamp_idx(a.ids[clamp_idx(a.order[p], (int32_t)a.n)], a.G);
+  const float *row = a.x + p * a.H, *gm = a.gamma + (int64_t)g * a.H,
+              *bt = a.beta + (int64_t)g * a.H;
+  f8 x[C];
+  float s = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    x[c] = load8<T_F32>(row, 8 * (lane + 64 * c), a.H).v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += x[c][j];
+  }
+  for (int m = 32; m; m /= 2) s += __shfl_xor(s, m);
+  const float mean = s / a.H;
+  float var = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[c][j] = 8 * (lane + 64 * c) + j < a.H ? x[c][j] - mean : 0.f;
+      var += x[c][j] * x[c][j];
+    }
+  for (int m = 32; m; m /= 2) var += __shfl_xor(var, m);
+  const float rstd = ln_rstd(var / a.H + a.eps);
+  float top = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int k = 8 * (lane + 64 * c);
+    const f8 gg = load8<T_F32>(gm, k, a.H).v, bb = load8<T_F32>(bt, k, a.H).v;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float v = x[c][j] * rstd * gg[j] + bb[j];
+      x[c][j] = v < 0.f ? 0.f : v;  // a NaN stays one
+    }
+    top = max_abs8(x[c], top);
+  }
+  elem_t<YT> *y = (elem_t<YT> *)a.y + p * a.H;
+  if constexpr (YT == T_I8) {
+    for (int m = 32; m; m /= 2)
+      top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
+    const float sc = quant_scale(top), inv = quant_inv(sc);
+    if (lane == 0) a.scales[p] = sc;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      store_q8(y, 8 * (lane + 64 * c), a.H, quantize8(x[c], sc, inv));
+  } else {
+    typedef elem_t<YT> vec __attribute__((ext_vector_type(8)));
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int k = 8 * (lane + 64 * c);
+      const vec o = __builtin_convertvector(x[c], vec);
+      if (k + 8 <= a.H) {
+        __builtin_memcpy(y + k, &o, sizeof o);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (k + j < a.H) y[k + j] = o[j];
+      }
+    }
+  }
+}
+
+template <int YT, int C>
+__global__ __launch_bounds__(64 * Q_WAVES) void norm_rows(NormArgs a) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t n = a.n_in ? min((int64_t)max(*a.n_in, 0), a.n) : a.n;
+  for (int64_t p = (int64_t)blockIdx.x * Q_WAVES + wave; p < n; p += (int64_t)gridDim.x * Q_WAVES)
+    norm_row<YT, C>(a, p, lane);
+}
+
+template <int YT>
+hipError_t norm_t(const NormArgs &a, hipStream_t stream) {
+  const int64_t wgs = (a.n + Q_WAVES - 1) / Q_WAVES;
+  const dim3 grid((uint32_t)(wgs < (1 << 20) ? wgs : 1 << 20)), block(64 * Q_WAVES);
+  const int units = (a.H + 7) / 8;
+  if (units <= 64) return launch(norm_rows<YT, 1>, grid, block, 0, stream, a);
+  if (units <= 128) return launch(norm_rows<YT, 2>, grid, block, 0, stream, a);
+  if (units <= 256) return launch(norm_rows<YT, 4>, grid, block, 0, stream, a);
+  return launch(norm_rows<YT, 8>, grid, block, 0, stream, a);
+}
+
+// ---- rows in the order of their groups ----
+// A stable counting sort of the group ids.  Every tile of rows counts its
+// ids (group_count), and places its rows behind those of lower groups and of
+// earlier tiles (group_place); ids outside [0, G) form one more group, G, that
+// comes last.  In a tile every wave owns a run of consecutive rows and counters
+// of its own: the lanes of a step that hold the same id are found with one
+// ballot per bit of the id, so there are no atomics and the order is the
+// input's.  Reads the ids twice, writes the order once; bound by the latency of
+// the launches up to some 10^5 rows.
+constexpr int G_WAVES = 4;
+constexpr int G_STEPS = 16;                        // rows of a wave / 64
+constexpr int G_TILE = G_WAVES * G_STEPS * 64;     // rows of a tile
+
+__device__ __forceinline__ int32_t group_of(int32_t id, int32_t G) {
+  return (uint32_t)id < (uint32_t)G ? id : G;
+}
+
+// Lanes with this lane's id, of those with ok.
+__device__ __forceinline__ uint64_t same_id(int32_t id, int bits, bool ok) {
+  uint64_t m = __ballot(ok);
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot((id >> b) & 1);
+    m &= (id >> b) & 1 ? set : ~set;
+  }
+  return m;
+}
+
+// This wave's ids of its run, and their counts added to cnt[0 .. G].
+__device__ __forceinline__ void count_run(const GroupArgs &a, int64_t r0, int bits, int32_t *cnt,
+                                          int32_t (&id)[G_STEPS]) {
+  const int lane = threadIdx.x & 63;
+  const uint64_t lt = ((uint64_t)1 << lane) - 1;
+#pragma unroll
+  for (int s = 0; s < G_STEPS; ++s) {
+    const int64_t r = r0 + s * 64 + lane;
+    id[s] = r < a.n ? group_of(a.ids[r], a.G) : 0;
+  }
+#pragma unroll
+  for (int s = 0; s < G_STEPS; ++s) {
+    if (r0 + s * 64 >= a.n) break;
+    const bool ok = r0 + s * 64 + lane < a.n;
+    const uint64_t m = same_id(id[s], bits, ok);
+    if (ok && (m & lt) == 0) cnt[id[s]] += __popcll(m);
+  }
+}
+
+// counts[tile][0 .. G]
+__global__ __launch_bounds__(64 * G_WAVES) void group_count(GroupArgs a, int bits) {
+  extern __shared__ int32_t cnt[];  // [G_WAVES][G + 1]
+  const int tid = threadIdx.x, wave = tid >> 6, W = a.G + 1;
+  for (int i = tid; i < G_WAVES * W; i += 64 * G_WAVES) cnt[i] = 0;
+  __syncthreads();
+  int32_t id[G_STEPS];
+  count_run(a, (int64_t)blockIdx.x * G_TILE + wave * (G_STEPS * 64), bits, cnt + wave * W, id);
+  __syncthreads();
+  for (int g = tid; g < W; g += 64 * G_WAVES) {
+    int32_t c = 0;
+    for (int w = 0; w < G_WAVES; ++w) c += cnt[w * W + g];
+    a.counts[(int64_t)blockIdx.x * W + g] = c;
+  }
+}
+
+__global__ __launch_bounds__(64 * G_WAVES) void group_place(GroupArgs a, int bits, int tiles) {
+  extern __shared__ int32_t lds[];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, W = a.G + 1;
+  int32_t *cnt = lds;                   // [G_WAVES][W], then where a wave's rows go
+  int32_t *base = lds + G_WAVES * W;    // [W]
+  __shared__ int32_t wsum[G_WAVES];
+  const int tile = blockIdx.x;
+  for (int i = tid; i < G_WAVES * W; i += 64 * G_WAVES) cnt[i] = 0;
+  __syncthreads();
+  int32_t id[G_STEPS];
+  const int64_t r0 = (int64_t)tile * G_TILE + wave * (G_STEPS * 64);
+  count_run(a, r0, bits, cnt + wave * W, id);
+  __syncthreads();
+  // base[g] = rows of lower groups + rows of g in earlier tiles
+  int32_t carry = 0;
+  for (int g0 = 0; g0 < W; g0 += 64 * G_WAVES) {
+    const int g = g0 + tid;
+    int32_t all = 0, before = 0;
+    if (g < W) {
+      if (tiles == 1) {
+        for (int w = 0; w < G_WAVES; ++w) all += cnt[w * W + g];
+      } else {
+        for (int t = 0; t < tiles; ++t) {
+          const int32_t c = a.counts[(int64_t)t * W + g];
+          all += c;
+          if (t < tile) before += c;
+        }
+      }
+    }
+    int32_t inc = all;  // inclusive sum over the groups of this round
+    for (int m = 1; m < 64; m *= 2) {
+      const int32_t v = __shfl_up(inc, m);
+      if (lane >= m) inc += v;
+    }
+    if (lane == 63) wsum[wave] = inc;
+    __syncthreads();
+    int32_t add = carry;
+    for (int w = 0; w < wave; ++w) add += wsum[w];
+    if (g < W) {
+      const int32_t first = add + inc - all;
+      base[g] = first + before;
+      if (tile == 0) a.offsets[g] = first;
+    }
+    for (int w = 0; w < G_WAVES; ++w) carry += wsum[w];
+    __syncthreads();
+  }
+  for (int g = tid; g < W; g += 64 * G_WAVES) {
+    int32_t at = base[g];
+    for (int w = 0; w < G_WAVES; ++w) {
+      const int32_t c = cnt[w * W + g];
+      cnt[w * W + g] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  const uint64_t lt = ((uint64_t)1 << lane) - 1;
+  int32_t *mine = cnt + wave * W;
+#pragma unroll
+  for (int s = 0; s < G_STEPS; ++s) {
+    if (r0 + s * 64 >= a.n) break;
+    const bool ok = r0 + s * 64 + lane < a.n;
+    const uint64_t m = same_id(id[s], bits, ok);
+    const int32_t at = mine[id[s]];
+    if (ok) a.order[at + __popcll(m & lt)] = (int32_t)(r0 + s * 64 + lane);
+    if (ok && (m & lt) == 0) mine[id[s]] = at + __popcll(m);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantArgs &a, hipStream_t stream) {
+  if (a.x_type == T_F32) return quantize_t<T_F32>(a, stream);
+  if (a.x_type == T_BF16) return quantize_t<T_BF16>(a, stream);
+  return quantize_t<T_F16>(a, stream);
+}
+
+hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
+  if (a.y_type == T_I8) return norm_t<T_I8>(a, stream);
+  if (a.y_type == T_BF16) return norm_t<T_BF16>(a, stream);
+  return norm_t<T_F16>(a, stream);
+}
+
+size_t group_scratch_bytes(int64_t n, int32_t G) {
+  const int64_t tiles = (n + G_TILE - 1) / G_TILE;
+  return tiles > 1 ? (size_t)tiles * (G + 1) * 4 : 0;
+}
+
+hipError_t launch_group(const GroupArgs &a, hipStream_t stream) {
+  const int tiles = (int)((a.n + G_TILE - 1) / G_TILE);
+  int bits = 0;
+  while ((a.G >> bits) != 0) ++bits;  // ids 0 .. G
+  const size_t W = (size_t)a.G + 1;
+  const dim3 block(64 * G_WAVES);
+  if (tiles > 1) {
+    const hipError_t e = launch_lds(group_count, dim3(tiles), block, G_WAVES * W * 4, stream, a, bits);
+    if (e != hipSuccess) return e;
+  }
+  return launch_lds(group_place, dim3(tiles), block, (G_WAVES + 1) * W * 4, stream, a, bits, tiles);
+}
+
+}  // namespace gnn

@@ -26,6 +26,9 @@ GNN_E_HIP = -5
 GNN_E_UNSUPPORTED = -6
 GNN_FP32 = 0
 GNN_BF16 = 1
+GNN_F16 = 2
+GNN_INT8 = 3
+GNN_MLP_MAX_LAYERS = 8
 GNN_VALIDATE_INDICES = 1
 GNN_LITERAL_GATHER = 2
 GNN_FP32_MFMA = 4
@@ -41,7 +44,10 @@ EXPORTS = ("gnn_weight_count", "gnn_create", "gnn_infer", "gnn_infer_logits", "g
            "gnn_server_destroy", "gnn_set_workspace_limit",
            "gnn_embed_weight_count", "gnn_embed_create", "gnn_embed_apply", "gnn_embed_destroy",
            "gnn_frnn", "gnn_debug_shared", "gnn_debug_frnn", "gnn_debug_frnn_bytes",
-           "gnn_hbm_probe")
+           "gnn_hbm_probe", "gnn_quantize_rows", "gnn_group_workspace", "gnn_group_rows",
+           "gnn_linear_weight_count", "gnn_linear_create", "gnn_linear_workspace",
+           "gnn_linear_apply", "gnn_linear_destroy", "gnn_mlp_weight_count", "gnn_mlp_create",
+           "gnn_mlp_workspace", "gnn_mlp_apply", "gnn_mlp_destroy")
 STAGES = ("csr", "node_enc", "edge_enc", "edge_update", "aggregate", "node_update",
           "classifier", "total")
 
@@ -72,6 +78,32 @@ class gnn_filter_dims(ctypes.Structure):
 
 def make_filter_dims(in_features=3, hidden=64, ln_eps=1e-5) -> gnn_filter_dims:
     return gnn_filter_dims(ctypes.sizeof(gnn_filter_dims), in_features, hidden, ln_eps)
+
+
+class gnn_linear_dims(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("in_features", ctypes.c_int32),
+                ("out_features", ctypes.c_int32), ("n_groups", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
+def make_linear_dims(in_features, out_features, n_groups=1, dtype=GNN_BF16) -> gnn_linear_dims:
+    return gnn_linear_dims(ctypes.sizeof(gnn_linear_dims), in_features, out_features, n_groups,
+                           dtype)
+
+
+class gnn_mlp_dims(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("n_layers", ctypes.c_int32),
+                ("widths", ctypes.c_int32 * (GNN_MLP_MAX_LAYERS + 1)),
+                ("n_groups", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("ln_eps", ctypes.c_float)]
+
+
+def make_mlp_dims(widths, n_groups=1, dtype=GNN_BF16, ln_eps=1e-5) -> gnn_mlp_dims:
+    """widths: of the input, the hidden layers and the output."""
+    if not 2 <= len(widths) <= GNN_MLP_MAX_LAYERS + 1:
+        raise ValueError(f"2..{GNN_MLP_MAX_LAYERS + 1} widths, got {len(widths)}")
+    w = (ctypes.c_int32 * (GNN_MLP_MAX_LAYERS + 1))(*widths)
+    return gnn_mlp_dims(ctypes.sizeof(gnn_mlp_dims), len(widths) - 1, w, n_groups, dtype, ln_eps)
 
 
 class gnn_profile_stats(ctypes.Structure):
@@ -157,6 +189,25 @@ def _load():
     L.gnn_frnn.restype = ctypes.c_int
     L.gnn_frnn.argtypes = [vp, i64, i32, ctypes.c_float, vp, i64, ctypes.POINTER(ctypes.c_int64),
                            vp]
+    L.gnn_quantize_rows.restype = ctypes.c_int
+    L.gnn_quantize_rows.argtypes = [vp, i32, i64, i64, i32, vp, i64, vp, vp]
+    L.gnn_group_workspace.restype = ctypes.c_size_t
+    L.gnn_group_workspace.argtypes = [i64, i32]
+    L.gnn_group_rows.restype = ctypes.c_int
+    L.gnn_group_rows.argtypes = [vp, i64, i32, vp, vp, vp, i64, vp]
+    for name, dims in (("linear", gnn_linear_dims), ("mlp", gnn_mlp_dims)):
+        f = getattr(L, f"gnn_{name}_weight_count")
+        f.restype, f.argtypes = ctypes.c_size_t, [ctypes.POINTER(dims)]
+        f = getattr(L, f"gnn_{name}_create")
+        f.restype, f.argtypes = vp, [vp, ctypes.POINTER(dims)]
+        f = getattr(L, f"gnn_{name}_workspace")
+        f.restype, f.argtypes = ctypes.c_size_t, [vp, i32, i64]
+        f = getattr(L, f"gnn_{name}_destroy")
+        f.restype, f.argtypes = None, [vp]
+    L.gnn_linear_apply.restype = ctypes.c_int
+    L.gnn_linear_apply.argtypes = [vp, vp, i32, i64, vp, i64, vp, vp, vp, i32, i64, vp, i64, vp]
+    L.gnn_mlp_apply.restype = ctypes.c_int
+    L.gnn_mlp_apply.argtypes = [vp, vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, vp]
     L.gnn_server_create.restype = vp
     L.gnn_server_create.argtypes = [vp, ctypes.c_int]
     L.gnn_server_submit.restype = i64
@@ -459,6 +510,261 @@ def radius_graph(z: torch.Tensor, r2: float, stream=None) -> torch.Tensor:
         out = torch.empty(2 * max(cnt, 1), dtype=torch.int32, device=z.device)
         cnt = gnn_frnn(z, n, d, r2, out, cnt, stream)
     return out[:2 * cnt].view(2, cnt)
+
+
+# ---- linear layers of wide and per-region networks ----
+
+_TYPES = {torch.float32: GNN_FP32, torch.bfloat16: GNN_BF16, torch.float16: GNN_F16,
+          torch.int8: GNN_INT8}
+
+
+def _on(device, stream):
+    """Context in which what is allocated, and what runs, belongs to `stream` of
+    `device` (its current stream if None)."""
+    if stream is None:
+        return torch.cuda.device(device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return torch.cuda.stream(stream)
+
+
+def _rows(what: str, t: torch.Tensor, width=None, n=None, device=None):
+    """Checks a table of rows; (address, element type, stride in elements)."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise TypeError(f"{what}: expected a 2-D tensor")
+    if t.dtype not in _TYPES:
+        raise TypeError(f"{what}: rows of {t.dtype} are not supported")
+    if not t.is_cuda or (device is not None and t.device != device):
+        raise ValueError(f"{what}: expected a tensor on {device or 'the GPU'}, got {t.device}")
+    if width is not None and t.shape[1] != width:
+        raise ValueError(f"{what}: rows of {t.shape[1]}, expected {width}")
+    if n is not None and t.shape[0] != n:
+        raise ValueError(f"{what}: {t.shape[0]} rows, expected {n}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the elements of a row must be contiguous")
+    stride = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    if stride < t.shape[1]:
+        raise ValueError(f"{what}: rows overlap")
+    return t.data_ptr(), _TYPES[t.dtype], stride
+
+
+def _vector(what: str, t, dtype, n: int, device):
+    """Address of a contiguous vector of n elements, or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.shape != (n,):
+        raise TypeError(f"{what}: expected a {dtype} tensor of shape ({n},)")
+    if not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{what}: expected a contiguous tensor on {device}")
+    return t.data_ptr()
+
+
+def _scratch(nbytes: int, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _device(what: str, t) -> torch.device:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{what}: expected a tensor on the GPU")
+    return t.device
+
+
+def gnn_quantize_rows(x, x_type: int, x_stride: int, n_rows: int, width: int, q, q_stride: int,
+                      scales, stream=None) -> int:
+    """As the C call; addresses or contiguous tensors."""
+    return _check(lib.gnn_quantize_rows(_addr(x), x_type, x_stride, n_rows, width, _addr(q),
+                                        q_stride, _addr(scales), _stream(stream)))
+
+
+def quantize_rows(x: torch.Tensor, out=None, stream=None):
+    """(q, scales): the rows of x as int8 with one fp32 scale each; `out`: a pair
+    of tensors to fill."""
+    dev = _device("x", x)
+    with _on(dev, stream):
+        xa, xt, xs = _rows("x", x)
+        n, k = x.shape
+        q, s = out if out is not None else (torch.empty(n, k, dtype=torch.int8, device=dev),
+                                            torch.empty(n, dtype=torch.float32, device=dev))
+        qa, qt, qs = _rows("q", q, k, n, dev)
+        if qt != GNN_INT8:
+            raise TypeError("q: expected int8 rows")
+        gnn_quantize_rows(xa, xt, xs, n, k, qa, qs, _vector("scales", s, torch.float32, n, dev))
+    return q, s
+
+
+def gnn_group_workspace(n_rows: int, n_groups: int) -> int:
+    return int(lib.gnn_group_workspace(n_rows, n_groups))
+
+
+def gnn_group_rows(group_ids, n_rows: int, n_groups: int, offsets, order, workspace=None,
+                   workspace_bytes: int = 0, stream=None) -> int:
+    """As the C call; addresses or contiguous tensors."""
+    return _check(lib.gnn_group_rows(_addr(group_ids), n_rows, n_groups, _addr(offsets),
+                                     _addr(order), _addr(workspace), workspace_bytes,
+                                     _stream(stream)))
+
+
+def group_rows(group_ids: torch.Tensor, n_groups: int, stream=None):
+    """(offsets, order) of the rows by their int32 group ids; rows whose id is
+    outside [0, n_groups) come last and belong to no group."""
+    dev = _device("group_ids", group_ids)
+    n = group_ids.numel()
+    ids = _vector("group_ids", group_ids, torch.int32, n, dev)
+    with _on(dev, stream):
+        nb = gnn_group_workspace(n, n_groups)
+        ws = _scratch(nb, dev)
+        offsets = torch.empty(max(n_groups, 0) + 1, dtype=torch.int32, device=dev)
+        order = torch.empty(n, dtype=torch.int32, device=dev)
+        gnn_group_rows(ids, n, n_groups, offsets, order, ws, nb)
+    return offsets, order
+
+
+def gnn_linear_weight_count(dims: gnn_linear_dims) -> int:
+    return int(lib.gnn_linear_weight_count(ctypes.byref(dims)))
+
+
+def gnn_mlp_weight_count(dims: gnn_mlp_dims) -> int:
+    return int(lib.gnn_mlp_weight_count(ctypes.byref(dims)))
+
+
+def _create_from_blob(count, create, weights, dims, what: str) -> int:
+    n = int(count(ctypes.byref(dims)))
+    if n == 0:
+        raise GnnError(GNN_E_INVALID_ARG, gnn_last_error())
+    w = np.ascontiguousarray(weights, np.float32)
+    if w.size != n:
+        raise ValueError(f"{what} blob has {w.size} floats, dims need {n}")
+    h = create(w.ctypes.data, ctypes.byref(dims))
+    if not h:
+        raise GnnError(GNN_E_INVALID_ARG, gnn_last_error())
+    return h
+
+
+def gnn_linear_create(weights: np.ndarray, dims: gnn_linear_dims) -> int:
+    return _create_from_blob(lib.gnn_linear_weight_count, lib.gnn_linear_create, weights, dims,
+                             "linear")
+
+
+def gnn_linear_destroy(layer) -> None:
+    lib.gnn_linear_destroy(layer)
+
+
+def gnn_linear_workspace(layer, x_type: int, n_rows: int) -> int:
+    return int(lib.gnn_linear_workspace(layer, x_type, n_rows))
+
+
+def gnn_linear_apply(layer, x, x_type: int, x_stride: int, x_scales, n_rows: int, offsets, order,
+                     y, y_type: int, y_stride: int, workspace=None, workspace_bytes: int = 0,
+                     stream=None) -> int:
+    """As the C call; addresses or contiguous tensors."""
+    return _check(lib.gnn_linear_apply(layer, _addr(x), x_type, x_stride, _addr(x_scales), n_rows,
+                                       _addr(offsets), _addr(order), _addr(y), y_type, y_stride,
+                                       _addr(workspace), workspace_bytes, _stream(stream)))
+
+
+def gnn_mlp_create(weights: np.ndarray, dims: gnn_mlp_dims) -> int:
+    return _create_from_blob(lib.gnn_mlp_weight_count, lib.gnn_mlp_create, weights, dims, "MLP")
+
+
+def gnn_mlp_destroy(mlp) -> None:
+    lib.gnn_mlp_destroy(mlp)
+
+
+def gnn_mlp_workspace(mlp, x_type: int, n_rows: int) -> int:
+    return int(lib.gnn_mlp_workspace(mlp, x_type, n_rows))
+
+
+def gnn_mlp_apply(mlp, x, x_type: int, x_stride: int, group_ids, n_rows: int, y, y_type: int,
+                  y_stride: int, workspace=None, workspace_bytes: int = 0, stream=None) -> int:
+    """As the C call; addresses or contiguous tensors."""
+    return _check(lib.gnn_mlp_apply(mlp, _addr(x), x_type, x_stride, _addr(group_ids), n_rows,
+                                    _addr(y), y_type, y_stride, _addr(workspace), workspace_bytes,
+                                    _stream(stream)))
+
+
+class _RowsHandle:
+    """A handle that turns rows of one width into rows of another."""
+
+    _free = None
+    handle = None
+
+    def _out(self, n: int, width: int, x, out, out_dtype, grouped: bool):
+        if out is None:
+            if out_dtype is None:
+                out_dtype = x.dtype if x.dtype.is_floating_point else torch.float32
+            # rows of no group are not written: zeros in a new output
+            new = torch.zeros if grouped else torch.empty
+            out = new(n, width, dtype=out_dtype, device=self.device)
+        elif out_dtype is not None and out.dtype != out_dtype:
+            raise TypeError(f"out: expected {out_dtype}, got {out.dtype}")
+        return out, _rows("out", out, width, n, self.device)
+
+    def close(self):
+        if self.handle:
+            type(self)._free(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Linear(_RowsHandle):
+    """Owns one layer: ``Linear(w, dims)(x) -> y``, with ``offsets`` and ``order``
+    as ``group_rows`` gives them where the layer has several groups.  x: rows of
+    any float type, or int8 rows with their ``scales`` (GNN_INT8 layers).  Rows of
+    no group are left as they were in ``out``, zeros in a new output."""
+
+    _free = staticmethod(gnn_linear_destroy)
+
+    def __init__(self, weights: np.ndarray, dims: gnn_linear_dims):
+        self.dims = dims
+        self.handle = gnn_linear_create(weights, dims)
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def __call__(self, x: torch.Tensor, scales=None, offsets=None, order=None, out=None,
+                 out_dtype=None, stream=None) -> torch.Tensor:
+        d, dev = self.dims, self.device
+        with _on(dev, stream):
+            xa, xt, xs = _rows("x", x, d.in_features, None, dev)
+            n = x.shape[0]
+            sc = _vector("scales", scales, torch.float32, n, dev)
+            off = _vector("offsets", offsets, torch.int32, d.n_groups + 1, dev)
+            ordr = _vector("order", order, torch.int32, n, dev)
+            out, (ya, yt, ys) = self._out(n, d.out_features, x, out, out_dtype,
+                                          offsets is not None or order is not None)
+            nb = gnn_linear_workspace(self.handle, xt, n)
+            ws = _scratch(nb, dev)
+            gnn_linear_apply(self.handle, xa, xt, xs, sc, n, off, ordr, ya, yt, ys, ws, nb)
+        return out
+
+
+class Mlp(_RowsHandle):
+    """Owns one network of linear layers: ``Mlp(w, dims)(x, group_ids) -> y``.
+    Rows of no group are left as they were in ``out``, zeros in a new output."""
+
+    _free = staticmethod(gnn_mlp_destroy)
+
+    def __init__(self, weights: np.ndarray, dims: gnn_mlp_dims):
+        self.dims = dims
+        self.handle = gnn_mlp_create(weights, dims)
+        self.device = torch.device("cuda", torch.cuda.current_device())
+
+    def __call__(self, x: torch.Tensor, group_ids=None, out=None, out_dtype=None,
+                 stream=None) -> torch.Tensor:
+        d, dev = self.dims, self.device
+        with _on(dev, stream):
+            xa, xt, xs = _rows("x", x, d.widths[0], None, dev)
+            n = x.shape[0]
+            ids = _vector("group_ids", group_ids, torch.int32, n, dev)
+            out, (ya, yt, ys) = self._out(n, d.widths[d.n_layers], x, out, out_dtype,
+                                          group_ids is not None)
+            nb = gnn_mlp_workspace(self.handle, xt, n)
+            ws = _scratch(nb, dev)
+            gnn_mlp_apply(self.handle, xa, xt, xs, ids, n, ya, yt, ys, ws, nb)
+        return out
 
 
 def gnn_server_create(handle, n_instances: int):
