@@ -13,8 +13,9 @@
 namespace gnn {
 namespace {
 
-constexpr int WAVES = 4;
-constexpr int CHUNK = 4096;  // most bytes of a row staged at a time
+constexpr int WAVES = 8;
+constexpr int CHUNK = 4096;        // most bytes of a row staged at a time
+constexpr int HALF = 78 * 1024;    // LDS of a tile of more than 32 rows: two fit on a CU
 constexpr int LDS_PAD = 16;  // bytes between staged rows: 16-byte slots of 8 rows differ
 
 template <int WT>
@@ -103,18 +104,28 @@ __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *r
   }
 }
 
-template <int WT, int XT, bool QUANT>
+// MAXU: the most units that a staged row of the calling kernel can have.
+template <int WT, int XT, bool QUANT, int MAXU>
 __device__ __forceinline__ void stage(const LinearArgs &a, const int32_t *rows, float *scale,
                                       unsigned char *lds, int pitch, int PM, int k0, int kn) {
   const int units = (kn + 7) / 8;
-  if (units <= 64)
+  if (units <= 64) {
     stage_rows<WT, XT, QUANT, 1, 4>(a, rows, scale, lds, pitch, PM, k0, kn);
-  else if (units <= 128)
-    stage_rows<WT, XT, QUANT, 2, 2>(a, rows, scale, lds, pitch, PM, k0, kn);
-  else if (units <= 256)
-    stage_rows<WT, XT, QUANT, 4, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
-  else
-    stage_rows<WT, XT, QUANT, 8, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
+    return;
+  }
+  if constexpr (MAXU > 64) {
+    if (units <= 128) {
+      stage_rows<WT, XT, QUANT, 2, 2>(a, rows, scale, lds, pitch, PM, k0, kn);
+      return;
+    }
+  }
+  if constexpr (MAXU > 128) {
+    if (units <= 256) {
+      stage_rows<WT, XT, QUANT, 4, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
+      return;
+    }
+  }
+  if constexpr (MAXU > 256) stage_rows<WT, XT, QUANT, 8, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
 }
 
 template <int T>
@@ -132,13 +143,16 @@ __device__ __forceinline__ void store4(void *y, int64_t at, const f4 &v, int lef
 }
 
 // One row tile (PM = 32 RB rows of one group) by all waves: the rows are
-// staged once (chunk by chunk where they do not fit), the weights come from
-// the caches in fragment order, NBW blocks of 32 channels to a wave at a time.
-template <int WT, int XT, int RB, int NBW>
-__global__ __launch_bounds__(64 * WAVES, 2) void linear_panel(LinearArgs a) {
+// staged once (MULTI: chunk by chunk, where they do not fit), the weights come
+// from the caches in fragment order.  A wave takes RBW of the tile's RB row
+// blocks and one block of 32 channels at a time.
+template <int WT, int XT, int RB, int RBW, bool MULTI>
+__global__ __launch_bounds__(64 * WAVES, 4) void linear_panel(LinearArgs a) {
   constexpr int PM = 32 * RB;
+  constexpr int WR = RB / RBW, WN = WAVES / WR;  // waves by row blocks and by channel blocks
   typedef typename Mma<WT>::acc acc_t;
   constexpr bool QUANT = WT == T_I8 && XT != T_I8;
+  constexpr int MAXU = (RB > 1 ? HALF / PM - LDS_PAD : CHUNK) / (WT == T_I8 ? 8 : 16);
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int32_t rows[PM], yrows[PM];
   __shared__ float scale[PM];
@@ -156,86 +170,80 @@ __global__ __launch_bounds__(64 * WAVES, 2) void linear_panel(LinearArgs a) {
     if (WT == T_I8 && !QUANT) scale[tid] = a.xs[r];
   }
   const int pitch = a.chunk + LDS_PAD;
-  const int esz = WT == T_I8 ? 1 : 2;
+  constexpr int esz = WT == T_I8 ? 1 : 2;
   const int steps = a.chunk / 32;  // of a chunk
-  const int nchunk = (a.S + steps - 1) / steps;
-  const int ntile = (a.NB + WAVES * NBW - 1) / (WAVES * NBW);
+  const int nchunk = MULTI ? (a.S + steps - 1) / steps : 1;
+  const int ntile = (a.NB + WN - 1) / WN;
   const int col = lane & 31, hh = lane >> 5;
-  const unsigned char *xl = smem + col * pitch + hh * 16;
+  const int rb0 = (wave % WR) * RBW;
+  const unsigned char *xl = smem + (rb0 * 32 + col) * pitch + hh * 16;
   __syncthreads();
+  if constexpr (!MULTI) {
+    stage<WT, XT, QUANT, MAXU>(a, rows, scale, smem, pitch, PM, 0, a.K);
+    __syncthreads();
+  }
   for (int nt = split; nt < ntile; nt += a.nsplit) {
-    const int nb0 = (nt * WAVES + wave) * NBW;
-    const bool live = nb0 < a.NB;
-    acc_t acc[NBW][RB];
+    const int nb = nt * WN + wave / WR;
+    const bool live = nb < a.NB;
+    acc_t acc[RBW];
 #pragma unroll
-    for (int i = 0; i < NBW; ++i)
+    for (int r = 0; r < RBW; ++r)
 #pragma unroll
-      for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[i][r][v] = 0;
-    const i4 *wf[NBW];
-#pragma unroll
-    for (int i = 0; i < NBW; ++i)
-      wf[i] = (const i4 *)a.w + ((int64_t)t.g * a.NB + min(nb0 + i, a.NB - 1)) * a.S * 64 + lane;
+      for (int v = 0; v < 16; ++v) acc[r][v] = 0;
+    const i4 *wf = (const i4 *)a.w + ((int64_t)t.g * a.NB + min(nb, a.NB - 1)) * a.S * 64 + lane;
     for (int ch = 0; ch < nchunk; ++ch) {
-      if (nchunk > 1 || nt == split) {
-        if (nchunk > 1) __syncthreads();
+      if constexpr (MULTI) {
         const int k0 = ch * (a.chunk / esz);
-        stage<WT, XT, QUANT>(a, rows, scale, smem, pitch, PM, k0, min(a.K - k0, a.chunk / esz));
+        __syncthreads();
+        stage<WT, XT, false, MAXU>(a, rows, scale, smem, pitch, PM, k0, min(a.K - k0, a.chunk / esz));
         __syncthreads();
       }
-      if (live) {
-        const int s0 = ch * steps, s1 = min(steps, a.S - s0);
-        for (int s = 0; s < s1; s += 2) {
-          i4 w[2][NBW], x[2][RB];
+      if (!live) continue;
+      const int s1 = MULTI ? min(steps, a.S - ch * steps) : a.S;
+      const i4 *wc = MULTI ? wf + ch * steps * 64 : wf;
+      i4 w[2] = {wc[0], wc[64]};
+      for (int s = 0; s < s1; s += 2) {
+        const int sn = min(s + 2, s1 - 2);  // the next two steps' weights, in flight meanwhile
+        const i4 n0 = wc[sn * 64], n1 = wc[sn * 64 + 64];
 #pragma unroll
-          for (int d = 0; d < 2; ++d)
+        for (int d = 0; d < 2; ++d) {
+          i4 x[RBW];
 #pragma unroll
-            for (int i = 0; i < NBW; ++i) w[d][i] = wf[i][(s0 + s + d) * 64];
+          for (int r = 0; r < RBW; ++r)
+            x[r] = *(const i4 *)(xl + r * 32 * pitch + (s + d) * 32);
 #pragma unroll
-          for (int d = 0; d < 2; ++d)
-#pragma unroll
-            for (int r = 0; r < RB; ++r)
-              x[d][r] = *(const i4 *)(xl + r * 32 * pitch + (s + d) * 32);
-#pragma unroll
-          for (int d = 0; d < 2; ++d)
-#pragma unroll
-            for (int i = 0; i < NBW; ++i)
-#pragma unroll
-              for (int r = 0; r < RB; ++r) mma<WT>(acc[i][r], w[d][i], x[d][r]);
+          for (int r = 0; r < RBW; ++r) mma<WT>(acc[r], w[d], x[r]);
         }
+        w[0] = n0;
+        w[1] = n1;
       }
     }
     if (!live) continue;
 #pragma unroll
-    for (int i = 0; i < NBW; ++i) {
-      if (nb0 + i >= a.NB) break;
+    for (int q = 0; q < 4; ++q) {
+      const int f = nb * 32 + 8 * q + 4 * hh;
+      const int64_t fo = (int64_t)t.g * a.NB * 32 + f;
+      const f4 b = *(const f4 *)(a.bias + fo);
+      f4 ws = {1.f, 1.f, 1.f, 1.f};
+      if constexpr (WT == T_I8) ws = *(const f4 *)(a.ws + fo);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int f = (nb0 + i) * 32 + 8 * q + 4 * hh;
-        const int64_t fo = (int64_t)t.g * a.NB * 32 + f;
-        const f4 b = *(const f4 *)(a.bias + fo);
-        f4 ws = {1.f, 1.f, 1.f, 1.f};
-        if constexpr (WT == T_I8) ws = *(const f4 *)(a.ws + fo);
+      for (int r = 0; r < RBW; ++r) {
+        const int row = (rb0 + r) * 32 + col;
+        f4 v;
 #pragma unroll
-        for (int r = 0; r < RB; ++r) {
-          const int row = r * 32 + col;
-          f4 v;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            v[k] = (float)acc[i][r][4 * q + k];
-            if constexpr (WT == T_I8) v[k] *= scale[row] * ws[k];
-            v[k] += b[k];
-          }
-          if (row < nrow && f < a.N) {
-            const int64_t at = (int64_t)yrows[row] * a.y_stride + f;
-            if (a.y_type == T_F32)
-              store4<T_F32>(a.y, at, v, a.N - f);
-            else if (a.y_type == T_BF16)
-              store4<T_BF16>(a.y, at, v, a.N - f);
-            else
-              store4<T_F16>(a.y, at, v, a.N - f);
-          }
+        for (int k = 0; k < 4; ++k) {
+          v[k] = (float)acc[r][4 * q + k];
+          if constexpr (WT == T_I8) v[k] *= scale[row] * ws[k];
+          v[k] += b[k];
+        }
+        if (row < nrow && f < a.N) {
+          const int64_t at = (int64_t)yrows[row] * a.y_stride + f;
+          if (a.y_type == T_F32)
+            store4<T_F32>(a.y, at, v, a.N - f);
+          else if (a.y_type == T_BF16)
+            store4<T_BF16>(a.y, at, v, a.N - f);
+          else
+            store4<T_F16>(a.y, at, v, a.N - f);
         }
       }
     }
@@ -295,18 +303,37 @@ __global__ __launch_bounds__(256) void linear_layout(const float *__restrict__ b
   }
 }
 
-template <int WT, int XT, int RB>
-hipError_t panel(const LinearArgs &a, int64_t tiles, hipStream_t stream) {
+// What a launch of the row panels needs: RB row blocks to a tile, RBW to a
+// wave, rows staged whole or in chunks.
+struct Plan {
+  int RB, RBW;
+  bool multi;
+  int64_t tiles;
+};
+
+template <int WT, int XT, int RB, int RBW, bool MULTI>
+hipError_t panel(const LinearArgs &a, const Plan &p, hipStream_t stream) {
   const size_t lds = (size_t)32 * RB * (a.chunk + LDS_PAD);
-  return launch_lds(linear_panel<WT, XT, RB, 2>, dim3((uint32_t)(tiles * a.nsplit)),
+  return launch_lds(linear_panel<WT, XT, RB, RBW, MULTI>, dim3((uint32_t)(p.tiles * a.nsplit)),
                     dim3(64 * WAVES), lds, stream, a);
 }
 
 template <int WT, int XT>
-hipError_t panel_rows(const LinearArgs &a, int RB, int64_t tiles, hipStream_t stream) {
-  if (RB == 4) return panel<WT, XT, 4>(a, tiles, stream);
-  if (RB == 2) return panel<WT, XT, 2>(a, tiles, stream);
-  return panel<WT, XT, 1>(a, tiles, stream);
+hipError_t panel_rows(const LinearArgs &a, const Plan &p, hipStream_t stream) {
+  if (p.multi) {
+    if constexpr (WT != T_I8 || XT == T_I8) return panel<WT, XT, 1, 1, true>(a, p, stream);
+    return hipErrorInvalidValue;  // such rows are rounded beforehand
+  }
+  if (p.RB == 4) {
+    if (p.RBW == 4) return panel<WT, XT, 4, 4, false>(a, p, stream);
+    if (p.RBW == 2) return panel<WT, XT, 4, 2, false>(a, p, stream);
+    return panel<WT, XT, 4, 1, false>(a, p, stream);
+  }
+  if (p.RB == 2) {
+    if (p.RBW == 2) return panel<WT, XT, 2, 2, false>(a, p, stream);
+    return panel<WT, XT, 2, 1, false>(a, p, stream);
+  }
+  return panel<WT, XT, 1, 1, false>(a, p, stream);
 }
 
 }  // namespace
@@ -337,32 +364,41 @@ bool linear_needs_rows8(const LinearArgs &a) { return a.S * 32 > CHUNK; }
 
 hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
   LinearArgs a = args;
-  // The rows of a tile stay in LDS: 128 of them where they fit in half of it
-  // (two workgroups to a CU), fewer of wide ones and where there are few.
-  constexpr int HALF = 78 * 1024;
+  // The rows of a tile stay in LDS: 128 of them where two workgroups' fit on a
+  // CU, fewer of wide ones and where there are too few tiles to fill the CUs.
+  Plan p;
   const int row_bytes = a.S * 32;
-  a.chunk = row_bytes < CHUNK ? row_bytes : CHUNK;
-  int RB = 4;
-  while (RB > 1 && (32 * RB * (a.chunk + LDS_PAD) > HALF || a.n / a.G <= 16 * RB)) RB /= 2;
-  const int64_t PM = 32 * RB;
-  const int64_t tiles = a.off ? a.n / PM + a.G : (a.n + PM - 1) / PM;
-  const int ntile = (a.NB + 2 * WAVES - 1) / (2 * WAVES);
-  a.nsplit = (int)((2 * n_cu + tiles - 1) / tiles);
+  p.multi = row_bytes > CHUNK;
+  a.chunk = p.multi ? CHUNK / 2 : row_bytes;
+  auto tiles = [&](int RB) {
+    const int64_t PM = 32 * RB;
+    return a.off ? a.n / PM + a.G : (a.n + PM - 1) / PM;
+  };
+  p.RB = p.multi ? 1 : 4;
+  while (p.RB > 1 && (32 * p.RB * (a.chunk + LDS_PAD) > HALF || a.n / (32 * p.RB) < 2 * n_cu))
+    p.RB /= 2;
+  p.tiles = tiles(p.RB);
+  // Few channel blocks: the waves share out a tile's row blocks as well.
+  p.RBW = p.RB;
+  while (p.RBW > 1 && a.NB <= WAVES / (p.RB / p.RBW) / 2) p.RBW /= 2;
+  const int WN = WAVES / (p.RB / p.RBW);
+  const int ntile = (a.NB + WN - 1) / WN;
+  a.nsplit = (int)((2 * n_cu + p.tiles - 1) / p.tiles);
   if (a.nsplit > ntile) a.nsplit = ntile;
   if (a.w_type == T_I8) {
-    if (a.x_type == T_I8) return panel_rows<T_I8, T_I8>(a, RB, tiles, stream);
-    if (a.x_type == T_F32) return panel_rows<T_I8, T_F32>(a, RB, tiles, stream);
-    if (a.x_type == T_BF16) return panel_rows<T_I8, T_BF16>(a, RB, tiles, stream);
-    return panel_rows<T_I8, T_F16>(a, RB, tiles, stream);
+    if (a.x_type == T_I8) return panel_rows<T_I8, T_I8>(a, p, stream);
+    if (a.x_type == T_F32) return panel_rows<T_I8, T_F32>(a, p, stream);
+    if (a.x_type == T_BF16) return panel_rows<T_I8, T_BF16>(a, p, stream);
+    return panel_rows<T_I8, T_F16>(a, p, stream);
   }
   if (a.w_type == T_BF16) {
-    if (a.x_type == T_F32) return panel_rows<T_BF16, T_F32>(a, RB, tiles, stream);
-    if (a.x_type == T_BF16) return panel_rows<T_BF16, T_BF16>(a, RB, tiles, stream);
-    return panel_rows<T_BF16, T_F16>(a, RB, tiles, stream);
+    if (a.x_type == T_F32) return panel_rows<T_BF16, T_F32>(a, p, stream);
+    if (a.x_type == T_BF16) return panel_rows<T_BF16, T_BF16>(a, p, stream);
+    return panel_rows<T_BF16, T_F16>(a, p, stream);
   }
-  if (a.x_type == T_F32) return panel_rows<T_F16, T_F32>(a, RB, tiles, stream);
-  if (a.x_type == T_BF16) return panel_rows<T_F16, T_BF16>(a, RB, tiles, stream);
-  return panel_rows<T_F16, T_F16>(a, RB, tiles, stream);
+  if (a.x_type == T_F32) return panel_rows<T_F16, T_F32>(a, p, stream);
+  if (a.x_type == T_BF16) return panel_rows<T_F16, T_BF16>(a, p, stream);
+  return panel_rows<T_F16, T_F16>(a, p, stream);
 }
 
 }  // namespace gnn
