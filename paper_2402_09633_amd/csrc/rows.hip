@@ -190,11 +190,12 @@ hipError_t norm_t(const NormArgs &a, hipStream_t stream) {
 // comes last.  In a tile every wave owns a run of consecutive rows and counters
 // of its own: the lanes of a step that hold the same id are found with one
 // ballot per bit of the id, so there are no atomics and the order is the
-// input's.  Reads the ids twice, writes the order once; bound by the latency of
-// the launches up to some 10^5 rows.
-constexpr int G_WAVES = 4;
-constexpr int G_STEPS = 16;                        // rows of a wave / 64
-constexpr int G_TILE = G_WAVES * G_STEPS * 64;     // rows of a tile
+// input's.  Reads the ids twice, writes the order once.
+//
+// How the tiles' counts become places: with few of them (G + 1 times the tiles
+// at most GROUP_DIRECT) every tile sums them itself, a wave to a group; else
+// one more launch (group_scan) leaves each tile's place and the groups' totals.
+constexpr int64_t GROUP_DIRECT = 16384;
 
 __device__ __forceinline__ int32_t group_of(int32_t id, int32_t G) {
   return (uint32_t)id < (uint32_t)G ? id : G;
@@ -211,17 +212,18 @@ __device__ __forceinline__ uint64_t same_id(int32_t id, int bits, bool ok) {
 }
 
 // This wave's ids of its run, and their counts added to cnt[0 .. G].
+template <int STEPS>
 __device__ __forceinline__ void count_run(const GroupArgs &a, int64_t r0, int bits, int32_t *cnt,
-                                          int32_t (&id)[G_STEPS]) {
+                                          int32_t (&id)[STEPS]) {
   const int lane = threadIdx.x & 63;
   const uint64_t lt = ((uint64_t)1 << lane) - 1;
 #pragma unroll
-  for (int s = 0; s < G_STEPS; ++s) {
+  for (int s = 0; s < STEPS; ++s) {
     const int64_t r = r0 + s * 64 + lane;
     id[s] = r < a.n ? group_of(a.ids[r], a.G) : 0;
   }
 #pragma unroll
-  for (int s = 0; s < G_STEPS; ++s) {
+  for (int s = 0; s < STEPS; ++s) {
     if (r0 + s * 64 >= a.n) break;
     const bool ok = r0 + s * 64 + lane < a.n;
     const uint64_t m = same_id(id[s], bits, ok);
@@ -229,49 +231,95 @@ __device__ __forceinline__ void count_run(const GroupArgs &a, int64_t r0, int bi
   }
 }
 
-// counts[tile][0 .. G]
-__global__ __launch_bounds__(64 * G_WAVES) void group_count(GroupArgs a, int bits) {
-  extern __shared__ int32_t cnt[];  // [G_WAVES][G + 1]
+__device__ __forceinline__ int32_t wave_sum(int32_t v) {
+  for (int m = 32; m; m /= 2) v += __shfl_xor(v, m);
+  return v;
+}
+
+// counts[0 .. G][tile]
+template <int WAVES, int STEPS>
+__global__ __launch_bounds__(64 * WAVES) void group_count(GroupArgs a, int bits) {
+  extern __shared__ int32_t cnt[];  // [WAVES][G + 1]
   const int tid = threadIdx.x, wave = tid >> 6, W = a.G + 1;
-  for (int i = tid; i < G_WAVES * W; i += 64 * G_WAVES) cnt[i] = 0;
+  for (int i = tid; i < WAVES * W; i += 64 * WAVES) cnt[i] = 0;
   __syncthreads();
-  int32_t id[G_STEPS];
-  count_run(a, (int64_t)blockIdx.x * G_TILE + wave * (G_STEPS * 64), bits, cnt + wave * W, id);
+  int32_t id[STEPS];
+  count_run(a, ((int64_t)blockIdx.x * WAVES + wave) * (STEPS * 64), bits, cnt + wave * W, id);
   __syncthreads();
-  for (int g = tid; g < W; g += 64 * G_WAVES) {
+  for (int g = tid; g < W; g += 64 * WAVES) {
     int32_t c = 0;
-    for (int w = 0; w < G_WAVES; ++w) c += cnt[w * W + g];
-    a.counts[(int64_t)blockIdx.x * W + g] = c;
+    for (int w = 0; w < WAVES; ++w) c += cnt[w * W + g];
+    a.counts[(int64_t)g * gridDim.x + blockIdx.x] = c;
   }
 }
 
-__global__ __launch_bounds__(64 * G_WAVES) void group_place(GroupArgs a, int bits, int tiles) {
+// counts[g][tile] -> the sum over the tiles before; counts[G + 1][g] = the sum
+// over all.  A wave to a group.
+__global__ __launch_bounds__(256) void group_scan(int32_t *counts, int W, int tiles) {
+  const int lane = threadIdx.x & 63, g = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (g >= W) return;
+  int32_t *c = counts + (int64_t)g * tiles, carry = 0;
+  for (int t0 = 0; t0 < tiles; t0 += 64) {
+    const int32_t v = t0 + lane < tiles ? c[t0 + lane] : 0;
+    int32_t inc = v;
+    for (int m = 1; m < 64; m *= 2) {
+      const int32_t u = __shfl_up(inc, m);
+      if (lane >= m) inc += u;
+    }
+    if (t0 + lane < tiles) c[t0 + lane] = carry + inc - v;
+    carry += __shfl(inc, 63);
+  }
+  if (lane == 0) counts[(int64_t)W * tiles + g] = carry;
+}
+
+template <int WAVES, int STEPS>
+__global__ __launch_bounds__(64 * WAVES) void group_place(GroupArgs a, int bits, int tiles,
+                                                          bool scanned) {
   extern __shared__ int32_t lds[];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, W = a.G + 1;
-  int32_t *cnt = lds;                   // [G_WAVES][W], then where a wave's rows go
-  int32_t *base = lds + G_WAVES * W;    // [W]
-  __shared__ int32_t wsum[G_WAVES];
+  int32_t *cnt = lds;               // [WAVES][W]: counts, then where a wave's rows go
+  int32_t *total = cnt + WAVES * W;  // [W] rows of a group
+  int32_t *before = total + W;       // [W] those of earlier tiles
+  __shared__ int32_t wsum[WAVES];
   const int tile = blockIdx.x;
-  for (int i = tid; i < G_WAVES * W; i += 64 * G_WAVES) cnt[i] = 0;
+  for (int i = tid; i < WAVES * W; i += 64 * WAVES) cnt[i] = 0;
   __syncthreads();
-  int32_t id[G_STEPS];
-  const int64_t r0 = (int64_t)tile * G_TILE + wave * (G_STEPS * 64);
+  int32_t id[STEPS];
+  const int64_t r0 = ((int64_t)tile * WAVES + wave) * (STEPS * 64);
   count_run(a, r0, bits, cnt + wave * W, id);
+  if (scanned) {
+    for (int g = tid; g < W; g += 64 * WAVES) {
+      total[g] = a.counts[(int64_t)W * tiles + g];
+      before[g] = a.counts[(int64_t)g * tiles + tile];
+    }
+  } else if (tiles > 1) {
+    for (int g = wave; g < W; g += WAVES) {
+      int32_t all = 0, prev = 0;
+      for (int t = lane; t < tiles; t += 64) {
+        const int32_t c = a.counts[(int64_t)g * tiles + t];
+        all += c;
+        if (t < tile) prev += c;
+      }
+      all = wave_sum(all);
+      prev = wave_sum(prev);
+      if (lane == 0) {
+        total[g] = all;
+        before[g] = prev;
+      }
+    }
+  }
   __syncthreads();
-  // base[g] = rows of lower groups + rows of g in earlier tiles
+  // a wave's first place in group g: behind the lower groups, the earlier
+  // tiles and the earlier waves
   int32_t carry = 0;
-  for (int g0 = 0; g0 < W; g0 += 64 * G_WAVES) {
+  for (int g0 = 0; g0 < W; g0 += 64 * WAVES) {
     const int g = g0 + tid;
-    int32_t all = 0, before = 0;
+    int32_t all = 0;
     if (g < W) {
-      if (tiles == 1) {
-        for (int w = 0; w < G_WAVES; ++w) all += cnt[w * W + g];
+      if (tiles > 1) {
+        all = total[g];
       } else {
-        for (int t = 0; t < tiles; ++t) {
-          const int32_t c = a.counts[(int64_t)t * W + g];
-          all += c;
-          if (t < tile) before += c;
-        }
+        for (int w = 0; w < WAVES; ++w) all += cnt[w * W + g];
       }
     }
     int32_t inc = all;  // inclusive sum over the groups of this round
@@ -279,31 +327,29 @@ __global__ __launch_bounds__(64 * G_WAVES) void group_place(GroupArgs a, int bit
       const int32_t v = __shfl_up(inc, m);
       if (lane >= m) inc += v;
     }
+    if (g0 > 0) __syncthreads();
     if (lane == 63) wsum[wave] = inc;
     __syncthreads();
-    int32_t add = carry;
-    for (int w = 0; w < wave; ++w) add += wsum[w];
-    if (g < W) {
-      const int32_t first = add + inc - all;
-      base[g] = first + before;
-      if (tile == 0) a.offsets[g] = first;
+    int32_t first = carry + inc - all;
+    for (int w = 0; w < WAVES; ++w) {
+      first += w < wave ? wsum[w] : 0;
+      carry += wsum[w];
     }
-    for (int w = 0; w < G_WAVES; ++w) carry += wsum[w];
-    __syncthreads();
-  }
-  for (int g = tid; g < W; g += 64 * G_WAVES) {
-    int32_t at = base[g];
-    for (int w = 0; w < G_WAVES; ++w) {
-      const int32_t c = cnt[w * W + g];
-      cnt[w * W + g] = at;
-      at += c;
+    if (g < W) {
+      if (tile == 0) a.offsets[g] = first;
+      int32_t at = first + (tiles > 1 ? before[g] : 0);
+      for (int w = 0; w < WAVES; ++w) {
+        const int32_t c = cnt[w * W + g];
+        cnt[w * W + g] = at;
+        at += c;
+      }
     }
   }
   __syncthreads();
   const uint64_t lt = ((uint64_t)1 << lane) - 1;
   int32_t *mine = cnt + wave * W;
 #pragma unroll
-  for (int s = 0; s < G_STEPS; ++s) {
+  for (int s = 0; s < STEPS; ++s) {
     if (r0 + s * 64 >= a.n) break;
     const bool ok = r0 + s * 64 + lane < a.n;
     const uint64_t m = same_id(id[s], bits, ok);
@@ -311,6 +357,32 @@ __global__ __launch_bounds__(64 * G_WAVES) void group_place(GroupArgs a, int bit
     if (ok) a.order[at + __popcll(m & lt)] = (int32_t)(r0 + s * 64 + lane);
     if (ok && (m & lt) == 0) mine[id[s]] = at + __popcll(m);
   }
+}
+
+// Rows of a tile: one tile of up to 8192 rows, tiles of 4096 beyond (4 waves
+// with longer runs where 16 waves' counters would not fit in 64 KiB of LDS).
+constexpr int G_TILE = 4096, G_WIDE = 900;
+
+int64_t group_tiles(int64_t n, int32_t G) {
+  return n <= (G < G_WIDE ? 2 * G_TILE : G_TILE) ? 1 : (n + G_TILE - 1) / G_TILE;
+}
+
+template <int WAVES, int STEPS>
+hipError_t group_t(const GroupArgs &a, int tiles, hipStream_t stream) {
+  int bits = 0;
+  while ((a.G >> bits) != 0) ++bits;  // ids 0 .. G
+  const int W = a.G + 1;
+  const dim3 block(64 * WAVES);
+  const bool scanned = (int64_t)tiles * W > GROUP_DIRECT && tiles > 1;
+  hipError_t e = hipSuccess;
+  if (tiles > 1)
+    e = launch_lds(group_count<WAVES, STEPS>, dim3(tiles), block, (size_t)WAVES * W * 4, stream, a,
+                   bits);
+  if (e == hipSuccess && scanned)
+    e = launch(group_scan, dim3((W + 3) / 4), dim3(256), 0, stream, a.counts, W, tiles);
+  if (e != hipSuccess) return e;
+  return launch_lds(group_place<WAVES, STEPS>, dim3(tiles), block, (size_t)(WAVES + 2) * W * 4,
+                    stream, a, bits, tiles, scanned);
 }
 
 }  // namespace
@@ -328,21 +400,16 @@ hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {
 }
 
 size_t group_scratch_bytes(int64_t n, int32_t G) {
-  const int64_t tiles = (n + G_TILE - 1) / G_TILE;
-  return tiles > 1 ? (size_t)tiles * (G + 1) * 4 : 0;
+  const int64_t tiles = group_tiles(n, G);
+  return tiles > 1 ? (size_t)(tiles + 1) * (G + 1) * 4 : 0;
 }
 
 hipError_t launch_group(const GroupArgs &a, hipStream_t stream) {
-  const int tiles = (int)((a.n + G_TILE - 1) / G_TILE);
-  int bits = 0;
-  while ((a.G >> bits) != 0) ++bits;  // ids 0 .. G
-  const size_t W = (size_t)a.G + 1;
-  const dim3 block(64 * G_WAVES);
-  if (tiles > 1) {
-    const hipError_t e = launch_lds(group_count, dim3(tiles), block, G_WAVES * W * 4, stream, a, bits);
-    if (e != hipSuccess) return e;
-  }
-  return launch_lds(group_place, dim3(tiles), block, (G_WAVES + 1) * W * 4, stream, a, bits, tiles);
+  const int tiles = (int)group_tiles(a.n, a.G);
+  if (a.G >= G_WIDE) return group_t<4, G_TILE / 256>(a, tiles, stream);
+  if (tiles > 1) return group_t<16, G_TILE / 1024>(a, tiles, stream);
+  if (a.n <= 2048) return group_t<16, 2>(a, 1, stream);
+  return group_t<16, 2 * G_TILE / 1024>(a, 1, stream);
 }
 
 }  // namespace gnn

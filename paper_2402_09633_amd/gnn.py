@@ -520,9 +520,7 @@ _TYPES = {torch.float32: GNN_FP32, torch.bfloat16: GNN_BF16, torch.float16: GNN_
 
 def _on(device, stream):
     """Context in which what is allocated, and what runs, belongs to `stream` of
-    `device` (its current stream if None)."""
-    if stream is None:
-        return torch.cuda.device(device)
+    `device`."""
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
     return torch.cuda.stream(stream)
@@ -532,20 +530,24 @@ def _rows(what: str, t: torch.Tensor, width=None, n=None, device=None):
     """Checks a table of rows; (address, element type, stride in elements)."""
     if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise TypeError(f"{what}: expected a 2-D tensor")
-    if t.dtype not in _TYPES:
+    kind = _TYPES.get(t.dtype)
+    if kind is None:
         raise TypeError(f"{what}: rows of {t.dtype} are not supported")
-    if not t.is_cuda or (device is not None and t.device != device):
-        raise ValueError(f"{what}: expected a tensor on {device or 'the GPU'}, got {t.device}")
-    if width is not None and t.shape[1] != width:
-        raise ValueError(f"{what}: rows of {t.shape[1]}, expected {width}")
-    if n is not None and t.shape[0] != n:
-        raise ValueError(f"{what}: {t.shape[0]} rows, expected {n}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if t.device != device:
+        raise ValueError(f"{what}: expected a tensor on {device}, got {t.device}")
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if width is not None and cols != width:
+        raise ValueError(f"{what}: rows of {cols}, expected {width}")
+    if n is not None and rows != n:
+        raise ValueError(f"{what}: {rows} rows, expected {n}")
+    if step != 1 and cols > 1:
         raise ValueError(f"{what}: the elements of a row must be contiguous")
-    stride = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    if stride < t.shape[1]:
-        raise ValueError(f"{what}: rows overlap")
-    return t.data_ptr(), _TYPES[t.dtype], stride
+    if stride < cols:
+        if rows > 1:
+            raise ValueError(f"{what}: rows overlap")
+        stride = cols
+    return t.data_ptr(), kind, stride
 
 
 def _vector(what: str, t, dtype, n: int, device):
@@ -576,19 +578,28 @@ def gnn_quantize_rows(x, x_type: int, x_stride: int, n_rows: int, width: int, q,
                                         q_stride, _addr(scales), _stream(stream)))
 
 
+# The current stream's handle, without the stream object around it (a call costs
+# a third of the time that current_stream() does).
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def quantize_rows(x: torch.Tensor, out=None, stream=None):
     """(q, scales): the rows of x as int8 with one fp32 scale each; `out`: a pair
     of tensors to fill."""
     dev = _device("x", x)
-    with _on(dev, stream):
-        xa, xt, xs = _rows("x", x)
-        n, k = x.shape
-        q, s = out if out is not None else (torch.empty(n, k, dtype=torch.int8, device=dev),
-                                            torch.empty(n, dtype=torch.float32, device=dev))
-        qa, qt, qs = _rows("q", q, k, n, dev)
-        if qt != GNN_INT8:
-            raise TypeError("q: expected int8 rows")
-        gnn_quantize_rows(xa, xt, xs, n, k, qa, qs, _vector("scales", s, torch.float32, n, dev))
+    if stream is not None or dev.index != torch.cuda.current_device():
+        with _on(dev, torch.cuda.current_stream(dev) if stream is None else stream):
+            return quantize_rows(x, out)
+    xa, xt, xs = _rows("x", x, None, None, dev)
+    n, k = x.shape
+    q, s = out if out is not None else (torch.empty(n, k, dtype=torch.int8, device=dev),
+                                        torch.empty(n, dtype=torch.float32, device=dev))
+    qa, qt, qs = _rows("q", q, k, n, dev)
+    if qt != GNN_INT8:
+        raise TypeError("q: expected int8 rows")
+    _check(lib.gnn_quantize_rows(xa, xt, xs, n, k, qa, qs,
+                                 _vector("scales", s, torch.float32, n, dev),
+                                 _raw_stream(dev.index)))
     return q, s
 
 
@@ -608,14 +619,17 @@ def group_rows(group_ids: torch.Tensor, n_groups: int, stream=None):
     """(offsets, order) of the rows by their int32 group ids; rows whose id is
     outside [0, n_groups) come last and belong to no group."""
     dev = _device("group_ids", group_ids)
+    if stream is not None or dev.index != torch.cuda.current_device():
+        with _on(dev, torch.cuda.current_stream(dev) if stream is None else stream):
+            return group_rows(group_ids, n_groups)
     n = group_ids.numel()
     ids = _vector("group_ids", group_ids, torch.int32, n, dev)
-    with _on(dev, stream):
-        nb = gnn_group_workspace(n, n_groups)
-        ws = _scratch(nb, dev)
-        offsets = torch.empty(max(n_groups, 0) + 1, dtype=torch.int32, device=dev)
-        order = torch.empty(n, dtype=torch.int32, device=dev)
-        gnn_group_rows(ids, n, n_groups, offsets, order, ws, nb)
+    nb = gnn_group_workspace(n, n_groups)
+    ws = _scratch(nb, dev)
+    offsets = torch.empty(max(n_groups, 0) + 1, dtype=torch.int32, device=dev)
+    order = torch.empty(n, dtype=torch.int32, device=dev)
+    _check(lib.gnn_group_rows(ids, n, n_groups, offsets.data_ptr(), order.data_ptr(),
+                              _addr(ws), nb, _raw_stream(dev.index)))
     return offsets, order
 
 
@@ -727,17 +741,20 @@ class Linear(_RowsHandle):
     def __call__(self, x: torch.Tensor, scales=None, offsets=None, order=None, out=None,
                  out_dtype=None, stream=None) -> torch.Tensor:
         d, dev = self.dims, self.device
-        with _on(dev, stream):
-            xa, xt, xs = _rows("x", x, d.in_features, None, dev)
-            n = x.shape[0]
-            sc = _vector("scales", scales, torch.float32, n, dev)
-            off = _vector("offsets", offsets, torch.int32, d.n_groups + 1, dev)
-            ordr = _vector("order", order, torch.int32, n, dev)
-            out, (ya, yt, ys) = self._out(n, d.out_features, x, out, out_dtype,
-                                          offsets is not None or order is not None)
-            nb = gnn_linear_workspace(self.handle, xt, n)
-            ws = _scratch(nb, dev)
-            gnn_linear_apply(self.handle, xa, xt, xs, sc, n, off, ordr, ya, yt, ys, ws, nb)
+        if stream is not None:
+            with _on(dev, stream):
+                return self(x, scales, offsets, order, out, out_dtype)
+        xa, xt, xs = _rows("x", x, d.in_features, None, dev)
+        n = x.shape[0]
+        sc = _vector("scales", scales, torch.float32, n, dev)
+        off = _vector("offsets", offsets, torch.int32, d.n_groups + 1, dev)
+        ordr = _vector("order", order, torch.int32, n, dev)
+        out, (ya, yt, ys) = self._out(n, d.out_features, x, out, out_dtype,
+                                      off is not None or ordr is not None)
+        nb = lib.gnn_linear_workspace(self.handle, xt, n)
+        ws = _scratch(nb, dev)
+        _check(lib.gnn_linear_apply(self.handle, xa, xt, xs, sc, n, off, ordr, ya, yt, ys,
+                                    _addr(ws), nb, _raw_stream(dev.index)))
         return out
 
 
@@ -755,15 +772,17 @@ class Mlp(_RowsHandle):
     def __call__(self, x: torch.Tensor, group_ids=None, out=None, out_dtype=None,
                  stream=None) -> torch.Tensor:
         d, dev = self.dims, self.device
-        with _on(dev, stream):
-            xa, xt, xs = _rows("x", x, d.widths[0], None, dev)
-            n = x.shape[0]
-            ids = _vector("group_ids", group_ids, torch.int32, n, dev)
-            out, (ya, yt, ys) = self._out(n, d.widths[d.n_layers], x, out, out_dtype,
-                                          group_ids is not None)
-            nb = gnn_mlp_workspace(self.handle, xt, n)
-            ws = _scratch(nb, dev)
-            gnn_mlp_apply(self.handle, xa, xt, xs, ids, n, ya, yt, ys, ws, nb)
+        if stream is not None:
+            with _on(dev, stream):
+                return self(x, group_ids, out, out_dtype)
+        xa, xt, xs = _rows("x", x, d.widths[0], None, dev)
+        n = x.shape[0]
+        ids = _vector("group_ids", group_ids, torch.int32, n, dev)
+        out, (ya, yt, ys) = self._out(n, d.widths[d.n_layers], x, out, out_dtype, ids is not None)
+        nb = lib.gnn_mlp_workspace(self.handle, xt, n)
+        ws = _scratch(nb, dev)
+        _check(lib.gnn_mlp_apply(self.handle, xa, xt, xs, ids, n, ya, yt, ys, _addr(ws), nb,
+                                 _raw_stream(dev.index)))
         return out
 
 
