@@ -27,17 +27,18 @@ struct Mma<T_I8> {
   typedef i16v acc;
 };
 
-// 32 output channels x 32 rows over 32 bytes of a row: lane l supplies 16
-// bytes of channel l % 32 and of row l % 32 from byte 16 (l / 32) on.
+// 32 rows x 32 output channels over 32 bytes of a row: lane l supplies 16
+// bytes of row l % 32 and of channel l % 32 from byte 16 (l / 32) on, and holds
+// channel l % 32 of the rows 8 (v / 4) + 4 (l / 32) + v % 4, v = 0 .. 15.
 template <int WT>
-__device__ __forceinline__ void mma(typename Mma<WT>::acc &c, const i4 &w, const i4 &x) {
+__device__ __forceinline__ void mma(typename Mma<WT>::acc &c, const i4 &x, const i4 &w) {
   if constexpr (WT == T_I8)
-    c = __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, w, c, 0, 0, 0);
   else if constexpr (WT == T_BF16)
-    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, w),
-                                                __builtin_bit_cast(bf8, x), c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, x),
+                                                __builtin_bit_cast(bf8, w), c, 0, 0, 0);
   else
-    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, w), __builtin_bit_cast(h8, x),
+    c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, x), __builtin_bit_cast(h8, w),
                                                c, 0, 0, 0);
 }
 
@@ -70,16 +71,16 @@ __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *r
 #pragma unroll
     for (int b = 0; b < B; ++b) {
       const int rr = r + b * WAVES * per;
-      float s = 0.f, inv = 0.f;
+      Quant z;
       if constexpr (QUANT) {
-        float top = 0.f;
+        uint32_t bits = 0;
 #pragma unroll
-        for (int c = 0; c < C; ++c) top = max_abs8(to_f32<XT>(raw[b][c]), top);
+        for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[b][c], bits);
+        float top = top_of<XT>(bits);
         for (int m = L / 2; m; m /= 2)
           top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
-        s = quant_scale(top);
-        inv = quant_inv(s);
-        if (u0 == 0 && rr < PM) scale[rr] = s;
+        z = quant_of<XT>(top);
+        if (u0 == 0 && rr < PM) scale[rr] = z.s;
       }
 #pragma unroll
       for (int c = 0; c < C; ++c) {
@@ -88,7 +89,7 @@ __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *r
         if constexpr (XT == WT)
           q = __builtin_bit_cast(unit, raw[b][c].v);
         else if constexpr (WT == T_I8)
-          q = quantize8(to_f32<XT>(raw[b][c]), s, inv);
+          q = quantize8<XT>(to_f32<XT>(raw[b][c]), z);
         else if constexpr (WT == T_BF16)
           q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[b][c]), bf8));
         else
@@ -128,17 +129,50 @@ __device__ __forceinline__ void stage(const LinearArgs &a, const int32_t *rows, 
   if constexpr (MAXU > 256) stage_rows<WT, XT, QUANT, 8, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
 }
 
-template <int T>
-__device__ __forceinline__ void store4(void *y, int64_t at, const f4 &v, int left) {
-  typedef elem_t<T> vec __attribute__((ext_vector_type(4)));
-  elem_t<T> *p = (elem_t<T> *)y + at;
-  const vec o = __builtin_convertvector(v, vec);
-  if (left >= 4) {
-    __builtin_memcpy(p, &o, sizeof o);
-  } else {
+// Stores one block of 32 rows x 32 channels (v in the accumulators' order).
+// fp32 rows are stored 32 lanes to a row's 128 bytes.  Of 16-bit rows, two
+// neighbouring lanes exchange halves, so that the even lane stores both
+// channels of one row and the odd lane both of the next: 64 bytes of a row to
+// a store of 16 lanes.  row_at: element offsets of the block's rows in y;
+// left: how many of them there are; ch: this lane's channel.  FULL: 32 rows,
+// 32 channels.
+template <int T, bool FULL>
+__device__ __forceinline__ void store_block(const LinearArgs &a, const f16v &v,
+                                            const int64_t *row_at, int left, int ch) {
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  // the row comparisons are made here each time: kept over the channel loop,
+  // their masks would not fit in the scalar registers
+  if constexpr (!FULL) asm volatile("" : "+v"(left));
+  if constexpr (T == T_F32) {
+    float *y = (float *)a.y + ch;
 #pragma unroll
-    for (int t = 0; t < 3; ++t)
-      if (t < left) p[t] = o[t];
+    for (int i = 0; i < 16; ++i) {
+      const int r = 8 * (i / 4) + 4 * hh + i % 4;
+      if (FULL || (r < left && ch < a.N)) y[row_at[r]] = v[i];
+    }
+  } else {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef elem_t<T> vec __attribute__((ext_vector_type(2)));
+    const int odd = lane & 1;
+    // bytes of (neighbour, mine): the even lane takes the first row's two
+    // halves in channel order, the odd lane the second row's
+    const uint32_t sel = odd ? 0x03020706u : 0x05040100u;
+    const int c0 = ch - odd;
+    elem_t<T> *y = (elem_t<T> *)a.y + c0;
+    row_at += 4 * hh + odd;
+    left -= 4 * hh + odd;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const uint32_t mine =
+          __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{v[i], v[i + 1]}, vec));
+      const uint32_t other = __builtin_amdgcn_mov_dpp(mine, 0xb1, 0xf, 0xf, true);  // lane ^ 1
+      const uint32_t out = __builtin_amdgcn_perm(other, mine, sel);
+      const int r = 8 * (i / 4) + i % 4;
+      if (FULL || (r < left && c0 + 1 < a.N))
+        __builtin_memcpy(y + row_at[r], &out, 4);
+      else if (r < left && c0 < a.N)
+        y[row_at[r]] = __builtin_bit_cast(vec, out)[0];
+    }
   }
 }
 
@@ -154,7 +188,8 @@ __global__ __launch_bounds__(64 * WAVES, 4) void linear_panel(LinearArgs a) {
   constexpr bool QUANT = WT == T_I8 && XT != T_I8;
   constexpr int MAXU = (RB > 1 ? HALF / PM - LDS_PAD : CHUNK) / (WT == T_I8 ? 8 : 16);
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ int32_t rows[PM], yrows[PM];
+  __shared__ int32_t rows[PM];
+  __shared__ int64_t row_at[PM];  // where a row lies in y
   __shared__ float scale[PM];
   const int bid = xcd_remap(blockIdx.x, gridDim.x);
   const int tile = bid / a.nsplit, split = bid % a.nsplit;
@@ -166,7 +201,7 @@ __global__ __launch_bounds__(64 * WAVES, 4) void linear_panel(LinearArgs a) {
     const int p = t.r0 + min(tid, nrow - 1);
     const int r = a.order ? clamp_idx(a.order[p], a.n) : p;
     rows[tid] = r;
-    yrows[tid] = a.y_order ? clamp_idx(a.y_order[p], a.n) : p;
+    row_at[tid] = (a.y_order ? clamp_idx(a.y_order[p], a.n) : p) * a.y_stride;
     if (WT == T_I8 && !QUANT) scale[tid] = a.xs[r];
   }
   const int pitch = a.chunk + LDS_PAD;
@@ -212,40 +247,42 @@ __global__ __launch_bounds__(64 * WAVES, 4) void linear_panel(LinearArgs a) {
           for (int r = 0; r < RBW; ++r)
             x[r] = *(const i4 *)(xl + r * 32 * pitch + (s + d) * 32);
 #pragma unroll
-          for (int r = 0; r < RBW; ++r) mma<WT>(acc[r], w[d], x[r]);
+          for (int r = 0; r < RBW; ++r) mma<WT>(acc[r], x[r], w[d]);
         }
         w[0] = n0;
         w[1] = n1;
       }
     }
     if (!live) continue;
+    const int ch = nb * 32 + col;
+    const float bias = a.bias[(int64_t)t.g * a.NB * 32 + ch];
+    const float ws = WT == T_I8 ? a.ws[(int64_t)t.g * a.NB * 32 + ch] : 1.f;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int f = nb * 32 + 8 * q + 4 * hh;
-      const int64_t fo = (int64_t)t.g * a.NB * 32 + f;
-      const f4 b = *(const f4 *)(a.bias + fo);
-      f4 ws = {1.f, 1.f, 1.f, 1.f};
-      if constexpr (WT == T_I8) ws = *(const f4 *)(a.ws + fo);
+    for (int r = 0; r < RBW; ++r) {
+      const int r0 = (rb0 + r) * 32;
+      if (r0 >= nrow) break;
+      f16v v;
 #pragma unroll
-      for (int r = 0; r < RBW; ++r) {
-        const int row = (rb0 + r) * 32 + col;
-        f4 v;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          v[k] = (float)acc[r][4 * q + k];
-          if constexpr (WT == T_I8) v[k] *= scale[row] * ws[k];
-          v[k] += b[k];
-        }
-        if (row < nrow && f < a.N) {
-          const int64_t at = (int64_t)yrows[row] * a.y_stride + f;
-          if (a.y_type == T_F32)
-            store4<T_F32>(a.y, at, v, a.N - f);
-          else if (a.y_type == T_BF16)
-            store4<T_BF16>(a.y, at, v, a.N - f);
-          else
-            store4<T_F16>(a.y, at, v, a.N - f);
-        }
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (WT == T_I8)
+          v[i] = __builtin_fmaf((float)acc[r][i] * ws, scale[r0 + 8 * (i / 4) + 4 * hh + i % 4],
+                                bias);
+        else
+          v[i] = acc[r][i] + bias;
       }
+      auto store = [&](auto type) {
+        constexpr int T = decltype(type)::value;
+        if (nrow - r0 >= 32 && nb * 32 + 32 <= a.N)
+          store_block<T, true>(a, v, row_at + r0, 32, ch);
+        else
+          store_block<T, false>(a, v, row_at + r0, nrow - r0, ch);
+      };
+      if (a.y_type == T_F32)
+        store(std::integral_constant<int, T_F32>());
+      else if (a.y_type == T_BF16)
+        store(std::integral_constant<int, T_BF16>());
+      else
+        store(std::integral_constant<int, T_F16>());
     }
   }
 }
@@ -260,7 +297,7 @@ __global__ __launch_bounds__(256) void linear_layout(const float *__restrict__ b
   const float *bs = W + (int64_t)a.N * a.K;
   const int row = tid / 8, part = tid % 8;
   const int n = nb * 32 + row;
-  __shared__ float sc[32];
+  __shared__ float sc[32];  // largest absolute value of a channel
   if constexpr (WT == T_I8) {
     uint32_t top = 0;
     if (n < a.N)
@@ -268,8 +305,8 @@ __global__ __launch_bounds__(256) void linear_layout(const float *__restrict__ b
         top = max(top, __float_as_uint(W[(int64_t)n * a.K + k]) & 0x7fffffffu);
     for (int m = 4; m; m /= 2) top = max(top, (uint32_t)__shfl_xor((int)top, m));
     if (part == 0) {
-      sc[row] = quant_scale(__uint_as_float(top));
-      ws[((int64_t)g * a.NB + nb) * 32 + row] = sc[row];
+      sc[row] = __uint_as_float(top);
+      ws[((int64_t)g * a.NB + nb) * 32 + row] = quant_scale(sc[row]);
     }
     __syncthreads();
   }
@@ -291,8 +328,8 @@ __global__ __launch_bounds__(256) void linear_layout(const float *__restrict__ b
       }
     u4 q;
     if constexpr (WT == T_I8) {
-      const float sch = sc[ch], inv = quant_inv(sch);
-      const u2 lo = quantize8(v[0], sch, inv), hi = quantize8(v[PER / 8 - 1], sch, inv);
+      const Quant z = quant_of<T_F32>(sc[ch]);
+      const u2 lo = quantize8<T_F32>(v[0], z), hi = quantize8<T_F32>(v[PER / 8 - 1], z);
       q = u4{lo[0], lo[1], hi[0], hi[1]};
     } else if constexpr (WT == T_BF16) {
       q = __builtin_bit_cast(u4, __builtin_convertvector(v[0], bf8));

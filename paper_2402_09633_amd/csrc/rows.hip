@@ -39,18 +39,19 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L
 #pragma unroll
   for (int b = 0; b < B; ++b) {
     const int64_t r = r0 + (int64_t)b * per;
-    float top = 0.f;
+    uint32_t bits = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) top = max_abs8(to_f32<XT>(raw[b][c]), top);
+    for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[b][c], bits);
+    float top = top_of<XT>(bits);
     for (int m = L / 2; m; m /= 2)
       top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
-    const float s = quant_scale(top), inv = quant_inv(s);
+    const Quant z = quant_of<XT>(top);
     if (r >= a.n) continue;
-    if (u0 == 0) a.scales[r] = s;
+    if (u0 == 0) a.scales[r] = z.s;
     int8_t *q = a.q + r * a.q_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      store_q8(q, 8 * (u0 + 64 * c), width, quantize8(to_f32<XT>(raw[b][c]), s, inv));
+      store_q8(q, 8 * (u0 + 64 * c), width, quantize8<XT>(to_f32<XT>(raw[b][c]), z));
     for (int u = u0 + L * C; 8 * u < width; u += L) store_q8(q, 8 * u, width, u2{0u, 0u});
   }
 }
@@ -63,21 +64,22 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
   const int tid = threadIdx.x;
   const int64_t r = blockIdx.x;
   const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
-  float top = 0.f;
+  uint32_t bits = 0;
   for (int k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
-    top = max_abs8(to_f32<XT>(load8<XT>(row, k, a.K)), top);
+    bits = max_bits<XT>(load8<XT>(row, k, a.K), bits);
+  float top = top_of<XT>(bits);
   for (int m = 32; m; m /= 2)
     top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
   if ((tid & 63) == 0) part[tid >> 6] = top;
   __syncthreads();
   for (int w = 0; w < Q_WAVES; ++w)
     top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(part[w])));
-  const float s = quant_scale(top), inv = quant_inv(s);
-  if (tid == 0) a.scales[r] = s;
+  const Quant z = quant_of<XT>(top);
+  if (tid == 0) a.scales[r] = z.s;
   int8_t *q = a.q + r * a.q_stride;
   const int width = a.pad ? a.pad : a.K;
   for (int k = 8 * tid; k < width; k += 8 * 64 * Q_WAVES)
-    store_q8(q, k, width, quantize8(to_f32<XT>(load8<XT>(row, k, a.K)), s, inv));
+    store_q8(q, k, width, quantize8<XT>(to_f32<XT>(load8<XT>(row, k, a.K)), z));
 }
 
 template <int XT>
@@ -126,7 +128,7 @@ __device__ __forceinline__ void norm_row(const NormArgs &a, int64_t p, int lane)
     }
   for (int m = 32; m; m /= 2) var += __shfl_xor(var, m);
   const float rstd = ln_rstd(var / a.H + a.eps);
-  float top = 0.f;
+  uint32_t bits = 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int k = 8 * (lane + 64 * c);
@@ -136,17 +138,18 @@ __device__ __forceinline__ void norm_row(const NormArgs &a, int64_t p, int lane)
       const float v = x[c][j] * rstd * gg[j] + bb[j];
       x[c][j] = v < 0.f ? 0.f : v;  // a NaN stays one
     }
-    top = max_abs8(x[c], top);
+    bits = max_bits<T_F32>(Raw8<T_F32>{x[c]}, bits);
   }
   elem_t<YT> *y = (elem_t<YT> *)a.y + p * a.H;
   if constexpr (YT == T_I8) {
+    float top = top_of<T_F32>(bits);
     for (int m = 32; m; m /= 2)
       top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
-    const float sc = quant_scale(top), inv = quant_inv(sc);
-    if (lane == 0) a.scales[p] = sc;
+    const Quant z = quant_of<T_F32>(top);
+    if (lane == 0) a.scales[p] = z.s;
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      store_q8(y, 8 * (lane + 64 * c), a.H, quantize8(x[c], sc, inv));
+      store_q8(y, 8 * (lane + 64 * c), a.H, quantize8<T_F32>(x[c], z));
   } else {
     typedef elem_t<YT> vec __attribute__((ext_vector_type(8)));
 #pragma unroll

@@ -72,12 +72,34 @@ __device__ __forceinline__ f8 to_f32(const Raw8<T> &r) {
 // smallest normal number (such a row counts as zero), NaN where the row holds
 // an infinity or a NaN (its values are then 0, and what is computed from them
 // NaN).
-__device__ __forceinline__ float max_abs8(const f8 &x, float m) {
-  // the bits of |x| order as x does, infinities and NaN above all numbers
+// The bits of |x| order as |x| does, infinities and NaN above all numbers: the
+// largest of eight is taken as whole numbers, of 16-bit types two at a time.
+typedef uint16_t s2 __attribute__((ext_vector_type(2)));
+template <int T>
+__device__ __forceinline__ uint32_t max_bits(const Raw8<T> &r, uint32_t m) {
+  if constexpr (T == T_F32) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    m = __uint_as_float(max(__float_as_uint(m), __float_as_uint(x[j]) & 0x7fffffffu));
+    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(r.v[j]) & 0x7fffffffu);
+  } else {
+    const u4 w = __builtin_bit_cast(u4, r.v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      m = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
+                                           __builtin_bit_cast(s2, m),
+                                           __builtin_bit_cast(s2, w[j] & 0x7fff7fffu)));
+  }
   return m;
+}
+
+// The value that max_bits found.
+template <int T>
+__device__ __forceinline__ float top_of(uint32_t m) {
+  if constexpr (T == T_F32) {
+    return __uint_as_float(m);
+  } else {
+    const uint16_t h = (uint16_t)max(m & 0xffffu, m >> 16);
+    return (float)__builtin_bit_cast(elem_t<T>, h);
+  }
 }
 
 __device__ __forceinline__ float quant_scale(float top) {
@@ -86,13 +108,55 @@ __device__ __forceinline__ float quant_scale(float top) {
   return s < 1.17549435e-38f ? 0.f : s;
 }
 
-// The factor that quantize8 multiplies by: 1 / s, 0 where the values are 0.
-__device__ __forceinline__ float quant_inv(float s) { return s > 0.f ? 1.f / s : 0.f; }
+// What a row of type T is multiplied by, so that one fused multiply-add rounds
+// x / s exactly (adding 1.5 * 2^23 rounds to a whole number, ties to even, whose
+// two's complement is the sum's low byte).
+//
+// 16-bit types.  With c = top / 127 and s = c (1 + d), |d| <= 2^-24, a quotient
+// x / c is exactly half way between two whole numbers, or at least 1 / (2 * 2047
+// * 127) > 1.9e-6 of itself away from there (x and top are whole multiples of
+// one number, below 2^11 but for powers of two).  In the second case x / s and
+// x * f, for f within 2^-23 of 1 / c, lie on the same side.  In the first the
+// sign of d says where x / s lies, and f is taken on that side of 1 / c.  Where
+// d = 0 the quotient is a true tie: such rows (s is a 16-bit number, or nearly)
+// are rounded by quant_exact.
+//
+// fp32.  Two factors, one step below and above 1 / s, round alike unless x / s
+// is next to a half; then quant_exact decides.
+struct Quant {
+  float s, lo, hi;
+  bool zero, tie;
+};
 
-// t = x * inv is within 1.5 * 2^-24 * 127 < 1.2e-5 of x / s.  Where its
-// distance from the nearest whole number is not within that of a half, the
-// nearest whole number is the one of x / s.  Otherwise x - t s decides, which
-// is exact in fp32 (a multiple of the smaller of ulp(x) and ulp(s), below s).
+__device__ __forceinline__ float step_up(float x, int by) {  // x > 0
+  return __uint_as_float(__float_as_uint(x) + (uint32_t)by);
+}
+
+template <int T>
+__device__ __forceinline__ Quant quant_of(float top) {
+  Quant q;
+  q.s = quant_scale(top);
+  q.zero = !(q.s > 0.f);
+  q.lo = q.hi = 0.f;
+  q.tie = false;
+  if (q.zero) return q;
+  if constexpr (T == T_F32) {
+    const float inv = 1.f / q.s;
+    q.lo = step_up(inv, -1);
+    q.hi = step_up(inv, 1);
+  } else {
+    const float d = __builtin_fmaf(q.s, 127.f, -top);
+    const float f = 127.f / top, e = __builtin_fmaf(f, top, -127.f);
+    q.lo = d > 0.f ? (e >= 0.f ? step_up(f, -1) : f) : (e <= 0.f ? step_up(f, 1) : f);
+    q.tie = d == 0.f;
+  }
+  return q;
+}
+
+// Nearest whole number to x / s.  t = x / s is off by less than 2e-5 before its
+// rounding, so the whole number next to it on the other side is the only other
+// candidate; x - t s decides, which is exact in fp32 (a multiple of the smaller
+// of ulp(x) and ulp(s), below s).
 __device__ __forceinline__ float quant_exact(float x, float s, float inv) {
   float t = rintf(x * inv);
   const float r2 = 2.f * __builtin_fmaf(-t, s, x);
@@ -102,21 +166,10 @@ __device__ __forceinline__ float quant_exact(float x, float s, float inv) {
   return t;
 }
 
-// Eight values to bytes.  Adding 1.5 * 2^23 rounds to a whole number (to
-// nearest, ties to even) whose two's complement is the sum's low byte.
-__device__ __forceinline__ u2 quantize8(const f8 &x, float s, float inv) {
-  constexpr float MAGIC = 12582912.f;
-  float t[8], far = 0.f;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    t[j] = __builtin_fmaf(x[j], inv, MAGIC);
-    const float r = __builtin_fmaf(x[j], inv, -(t[j] - MAGIC));
-    far = fmaxf(far, fabsf(r));
-  }
-  if (far > 0.5f - 2e-5f) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = quant_exact(x[j], s, inv) + MAGIC;
-  }
+constexpr float ROUND_MAGIC = 12582912.f;
+
+// The low bytes of eight sums.
+__device__ __forceinline__ u2 pack_bytes(const float (&t)[8]) {
   u2 q;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -124,9 +177,31 @@ __device__ __forceinline__ u2 quantize8(const f8 &x, float s, float inv) {
                                               __float_as_uint(t[4 * h]), 0x0c0c0400u);
     const uint32_t hi = __builtin_amdgcn_perm(__float_as_uint(t[4 * h + 3]),
                                               __float_as_uint(t[4 * h + 2]), 0x04000c0cu);
-    q[h] = inv == 0.f ? 0u : lo | hi;
+    q[h] = lo | hi;
   }
   return q;
+}
+
+template <int T>
+__device__ __forceinline__ u2 quantize8(const f8 &x, const Quant &z) {
+  float t[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) t[j] = __builtin_fmaf(x[j], z.lo, ROUND_MAGIC);
+  u2 q = pack_bytes(t);
+  bool exact = z.tie;
+  if constexpr (T == T_F32) {
+    float u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) u[j] = __builtin_fmaf(x[j], z.hi, ROUND_MAGIC);
+    const u2 p = pack_bytes(u);
+    exact = p[0] != q[0] || p[1] != q[1];
+  }
+  if (exact) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = quant_exact(x[j], z.s, z.lo) + ROUND_MAGIC;
+    q = pack_bytes(t);
+  }
+  return z.zero ? u2{0u, 0u} : q;
 }
 
 // launch() with more than 64 KiB of dynamic LDS allowed.
