@@ -43,90 +43,86 @@ __device__ __forceinline__ void mma(typename Mma<WT>::acc &c, const i4 &x, const
 }
 
 // Stages PM rows of a tile in LDS as the products read them, bytes
-// [0, chunk) of a row from element k0 on.  A wave takes 64 / L rows at a
-// time, L lanes to a row, C units of eight elements to a lane; with QUANT the
-// row's scale is formed from the same registers.  B such passes are loaded
-// before the first is stored.
-template <int WT, int XT, bool QUANT, int C, int B>
+// [0, chunk) of a row from element k0 on.  L lanes hold a row, C units of eight
+// elements each (unit u0 + L c), so that a wave takes 64 / L rows at a time:
+// with QUANT the row's scale is formed from the same registers, and what it
+// costs is shared by the rows that the lanes work on at once.  FULL: kn = 8 L C.
+template <int WT, int XT, bool QUANT, int C, bool FULL>
 __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *rows, float *scale,
-                                           unsigned char *lds, int pitch, int PM, int k0, int kn) {
+                                           unsigned char *lds, int pitch, int PM, int k0, int kn,
+                                           int L) {
   typedef typename std::conditional<WT == T_I8, u2, u4>::type unit;
-  const int units = (kn + 7) / 8;
-  int L = 64;
-  if (C == 1)
-    while (L / 2 >= units) L /= 2;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = 64 / L;
   const int sub = lane / L, u0 = lane % L;
   const int cap = (int)(pitch - LDS_PAD) / (int)sizeof(unit);  // units a staged row holds
-  for (int r = wave * per + sub; r < PM; r += WAVES * per * B) {
-    Raw8<XT> raw[B][C];
+  for (int r = wave * per + sub; r < PM; r += WAVES * per) {
+    Raw8<XT> raw[C];
+    const elem_t<XT> *row = (const elem_t<XT> *)a.x + (int64_t)rows[r] * a.x_stride + k0;
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int rr = min(r + b * WAVES * per, PM - 1);
-      const elem_t<XT> *row = (const elem_t<XT> *)a.x + (int64_t)rows[rr] * a.x_stride + k0;
+    for (int c = 0; c < C; ++c)
+      raw[c] = FULL ? load8_full<XT>(row, 8 * (u0 + L * c)) : load8<XT>(row, 8 * (u0 + L * c), kn);
+    Quant z;
+    if constexpr (QUANT) {
+      uint32_t bits = 0;
 #pragma unroll
-      for (int c = 0; c < C; ++c) raw[b][c] = load8<XT>(row, 8 * (u0 + 64 * c), kn);
+      for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[c], bits);
+      z = quant_of<XT>(lanes_max(top_of<XT>(bits), L));
+      if (u0 == 0) scale[r] = z.s;
     }
+    unsigned char *out = lds + r * pitch;
 #pragma unroll
-    for (int b = 0; b < B; ++b) {
-      const int rr = r + b * WAVES * per;
-      Quant z;
-      if constexpr (QUANT) {
-        uint32_t bits = 0;
-#pragma unroll
-        for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[b][c], bits);
-        float top = top_of<XT>(bits);
-        for (int m = L / 2; m; m /= 2)
-          top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
-        z = quant_of<XT>(top);
-        if (u0 == 0 && rr < PM) scale[rr] = z.s;
-      }
-#pragma unroll
-      for (int c = 0; c < C; ++c) {
-        const int u = u0 + 64 * c;
-        unit q;
-        if constexpr (XT == WT)
-          q = __builtin_bit_cast(unit, raw[b][c].v);
-        else if constexpr (WT == T_I8)
-          q = quantize8<XT>(to_f32<XT>(raw[b][c]), z);
-        else if constexpr (WT == T_BF16)
-          q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[b][c]), bf8));
-        else
-          q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[b][c]), h8));
-        if (rr < PM && u < cap) *(unit *)(lds + rr * pitch + u * (int)sizeof(unit)) = q;
-      }
+    for (int c = 0; c < C; ++c) {
+      const int u = u0 + L * c;
+      unit q;
+      if constexpr (XT == WT)
+        q = __builtin_bit_cast(unit, raw[c].v);
+      else if constexpr (WT == T_I8)
+        q = quantize8<XT>(to_f32<XT>(raw[c]), z);
+      else if constexpr (WT == T_BF16)
+        q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[c]), bf8));
+      else
+        q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[c]), h8));
+      if (FULL || u < cap) *(unit *)(out + u * (int)sizeof(unit)) = q;
     }
     // units past the last lane's: zeros up to the staged width
-    for (int b = 0; b < B; ++b)
-      if (r + b * WAVES * per < PM)
-        for (int u = u0 + L * C; u < cap; u += L)
-          *(unit *)(lds + (r + b * WAVES * per) * pitch + u * (int)sizeof(unit)) = unit{};
+    for (int u = u0 + L * C; u < cap; u += L) *(unit *)(out + u * (int)sizeof(unit)) = unit{};
   }
 }
 
-// MAXU: the most units that a staged row of the calling kernel can have.
+// Lanes to a row and units to a lane: 16 lanes where eight units each are
+// enough (a row's loads then span whole cache lines, and four rows share the
+// instructions that form their scales), more for wider rows, fewer for rows of
+// less than 16 units.  MAXU: the most units that a staged row of the calling
+// kernel can have.
 template <int WT, int XT, bool QUANT, int MAXU>
 __device__ __forceinline__ void stage(const LinearArgs &a, const int32_t *rows, float *scale,
                                       unsigned char *lds, int pitch, int PM, int k0, int kn) {
   const int units = (kn + 7) / 8;
-  if (units <= 64) {
-    stage_rows<WT, XT, QUANT, 1, 4>(a, rows, scale, lds, pitch, PM, k0, kn);
-    return;
+  int L = 16;
+  while (L / 2 >= units) L /= 2;
+  while (8 * L < units) L *= 2;
+  const int C = (units + L - 1) / L;
+  auto go = [&](auto n) {
+    constexpr int CC = decltype(n)::value;
+    if (kn == 8 * CC * L)
+      stage_rows<WT, XT, QUANT, CC, true>(a, rows, scale, lds, pitch, PM, k0, kn, L);
+    else
+      stage_rows<WT, XT, QUANT, CC, false>(a, rows, scale, lds, pitch, PM, k0, kn, L);
+  };
+  if (C <= 1) {
+    go(std::integral_constant<int, 1>());
+  } else if (C <= 2) {
+    go(std::integral_constant<int, 2>());
+  } else if (C <= 3) {
+    go(std::integral_constant<int, 3>());
+  } else if (C <= 4) {
+    go(std::integral_constant<int, 4>());
+  } else if (C <= 6) {
+    if constexpr (MAXU > 64) go(std::integral_constant<int, 6>());
+  } else {
+    if constexpr (MAXU > 96) go(std::integral_constant<int, 8>());
   }
-  if constexpr (MAXU > 64) {
-    if (units <= 128) {
-      stage_rows<WT, XT, QUANT, 2, 2>(a, rows, scale, lds, pitch, PM, k0, kn);
-      return;
-    }
-  }
-  if constexpr (MAXU > 128) {
-    if (units <= 256) {
-      stage_rows<WT, XT, QUANT, 4, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
-      return;
-    }
-  }
-  if constexpr (MAXU > 256) stage_rows<WT, XT, QUANT, 8, 1>(a, rows, scale, lds, pitch, PM, k0, kn);
 }
 
 // Stores one block of 32 rows x 32 channels (v in the accumulators' order).

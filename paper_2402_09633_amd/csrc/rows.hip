@@ -1,5 +1,7 @@
 // Row operators that feed the linear layers (linear.hip): rows rounded to 8
 // bits with a scale each, and rows put in the order of their groups.
+#include <type_traits>
+
 #include "rows_common.h"
 
 namespace gnn {
@@ -7,9 +9,8 @@ namespace {
 
 // ---- rows to 8 bits ----
 // One pass over the rows: L lanes hold a row (C units of eight elements
-// each), form its largest absolute value and round the values they hold.  B
-// rows are loaded before the first is reduced, so that a wave keeps several
-// loads in flight.  Bound by memory: x is read and q written once.
+// each), form its largest absolute value and round the values they hold.
+// Bound by memory: x is read and q written once.
 constexpr int Q_WAVES = 4;
 
 __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q) {
@@ -22,38 +23,33 @@ __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q)
   }
 }
 
-template <int XT, int C, int B>
+template <int XT, int C, bool FULL>
 __global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = 64 / L, sub = lane / L, u0 = lane % L;
-  const int64_t r0 = ((int64_t)blockIdx.x * Q_WAVES + wave) * per * B + sub;
+  const int64_t r = ((int64_t)blockIdx.x * Q_WAVES + wave) * per + sub;
+  if (r >= a.n) return;
   const int width = a.pad ? a.pad : a.K;
-  Raw8<XT> raw[B][C];
+  const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
+  Raw8<XT> raw[C];
 #pragma unroll
-  for (int b = 0; b < B; ++b) {
-    const int64_t r = min(r0 + (int64_t)b * per, a.n - 1);
-    const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
+  for (int c = 0; c < C; ++c)
+    raw[c] = FULL ? load8_full<XT>(row, 8 * (u0 + L * c)) : load8<XT>(row, 8 * (u0 + L * c), a.K);
+  uint32_t bits = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) raw[b][c] = load8<XT>(row, 8 * (u0 + 64 * c), a.K);
+  for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[c], bits);
+  const Quant z = quant_of<XT>(lanes_max(top_of<XT>(bits), L));
+  if (u0 == 0) a.scales[r] = z.s;
+  int8_t *q = a.q + r * a.q_stride;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const u2 v = quantize8<XT>(to_f32<XT>(raw[c]), z);
+    if (FULL)
+      __builtin_memcpy(q + 8 * (u0 + L * c), &v, 8);
+    else
+      store_q8(q, 8 * (u0 + L * c), width, v);
   }
-#pragma unroll
-  for (int b = 0; b < B; ++b) {
-    const int64_t r = r0 + (int64_t)b * per;
-    uint32_t bits = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[b][c], bits);
-    float top = top_of<XT>(bits);
-    for (int m = L / 2; m; m /= 2)
-      top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
-    const Quant z = quant_of<XT>(top);
-    if (r >= a.n) continue;
-    if (u0 == 0) a.scales[r] = z.s;
-    int8_t *q = a.q + r * a.q_stride;
-#pragma unroll
-    for (int c = 0; c < C; ++c)
-      store_q8(q, 8 * (u0 + 64 * c), width, quantize8<XT>(to_f32<XT>(raw[b][c]), z));
-    for (int u = u0 + L * C; 8 * u < width; u += L) store_q8(q, 8 * u, width, u2{0u, 0u});
-  }
+  for (int u = u0 + L * C; 8 * u < width; u += L) store_q8(q, 8 * u, width, u2{0u, 0u});
 }
 
 // Rows too wide for a wave's registers: one workgroup to a row, which is read
@@ -68,8 +64,7 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
   for (int k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
     bits = max_bits<XT>(load8<XT>(row, k, a.K), bits);
   float top = top_of<XT>(bits);
-  for (int m = 32; m; m /= 2)
-    top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
+  top = lanes_max(top, 64);
   if ((tid & 63) == 0) part[tid >> 6] = top;
   __syncthreads();
   for (int w = 0; w < Q_WAVES; ++w)
@@ -85,18 +80,25 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
 template <int XT>
 hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
   const int units = (a.K + 7) / 8;
-  int L = 64;
-  while (L / 2 >= units) L /= 2;
-  auto grid = [&](int B) {
-    const int64_t rows = (int64_t)Q_WAVES * (64 / L) * B;
-    return dim3((uint32_t)((a.n + rows - 1) / rows));
-  };
   const dim3 block(64 * Q_WAVES);
-  if (units <= 64) return launch(quantize_rows<XT, 1, 4>, grid(4), block, 0, stream, a, L);
-  if (units <= 128) return launch(quantize_rows<XT, 2, 2>, grid(2), block, 0, stream, a, L);
-  if (units <= 256) return launch(quantize_rows<XT, 4, 1>, grid(1), block, 0, stream, a, L);
-  if (units <= 512) return launch(quantize_rows<XT, 8, 1>, grid(1), block, 0, stream, a, L);
-  return launch(quantize_wide<XT>, dim3((uint32_t)a.n), block, 0, stream, a);
+  if (units > 512) return launch(quantize_wide<XT>, dim3((uint32_t)a.n), block, 0, stream, a);
+  int L = 16;
+  while (L / 2 >= units) L /= 2;
+  while (8 * L < units) L *= 2;
+  const int C = (units + L - 1) / L;
+  const int64_t rows = (int64_t)Q_WAVES * (64 / L);
+  const dim3 grid((uint32_t)((a.n + rows - 1) / rows));
+  auto go = [&](auto n) {
+    constexpr int CC = decltype(n)::value;
+    if (a.K == 8 * CC * L) return launch(quantize_rows<XT, CC, true>, grid, block, 0, stream, a, L);
+    return launch(quantize_rows<XT, CC, false>, grid, block, 0, stream, a, L);
+  };
+  if (C <= 1) return go(std::integral_constant<int, 1>());
+  if (C <= 2) return go(std::integral_constant<int, 2>());
+  if (C <= 3) return go(std::integral_constant<int, 3>());
+  if (C <= 4) return go(std::integral_constant<int, 4>());
+  if (C <= 6) return go(std::integral_constant<int, 6>());
+  return go(std::integral_constant<int, 8>());
 }
 
 // ---- LayerNorm and ReLU of hidden rows ----
@@ -142,10 +144,7 @@ __device__ __forceinline__ void norm_row(const NormArgs &a, int64_t p, int lane)
   }
   elem_t<YT> *y = (elem_t<YT> *)a.y + p * a.H;
   if constexpr (YT == T_I8) {
-    float top = top_of<T_F32>(bits);
-    for (int m = 32; m; m /= 2)
-      top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(__shfl_xor(top, m))));
-    const Quant z = quant_of<T_F32>(top);
+    const Quant z = quant_of<T_F32>(lanes_max(top_of<T_F32>(bits), 64));
     if (lane == 0) a.scales[p] = z.s;
 #pragma unroll
     for (int c = 0; c < C; ++c)

@@ -60,6 +60,14 @@ __device__ __forceinline__ Raw8<T> load8(const elem_t<T> *row, int k, int K) {
   return r;
 }
 
+// load8 where the row is known to hold all eight.
+template <int T>
+__device__ __forceinline__ Raw8<T> load8_full(const elem_t<T> *row, int k) {
+  Raw8<T> r;
+  __builtin_memcpy(&r.v, row + k, sizeof r.v);
+  return r;
+}
+
 template <int T>
 __device__ __forceinline__ f8 to_f32(const Raw8<T> &r) {
   if constexpr (T == T_F32) return r.v;
@@ -100,6 +108,19 @@ __device__ __forceinline__ float top_of(uint32_t m) {
     const uint16_t h = (uint16_t)max(m & 0xffffu, m >> 16);
     return (float)__builtin_bit_cast(elem_t<T>, h);
   }
+}
+
+// The largest value of L = 2^i neighbouring lanes, in all of them.
+__device__ __forceinline__ float lanes_max(float v, int L) {
+  uint32_t m = __float_as_uint(v);
+  auto step = [&](uint32_t o) { m = max(m, o); };
+  if (L >= 2) step(__builtin_amdgcn_mov_dpp(m, 0xb1, 0xf, 0xf, true));   // lane ^ 1
+  if (L >= 4) step(__builtin_amdgcn_mov_dpp(m, 0x4e, 0xf, 0xf, true));   // lane ^ 2
+  if (L >= 8) step(__builtin_amdgcn_mov_dpp(m, 0x141, 0xf, 0xf, true));  // 7 - lane of 8
+  if (L >= 16) step(__builtin_amdgcn_mov_dpp(m, 0x140, 0xf, 0xf, true)); // 15 - lane of 16
+  if (L >= 32) step((uint32_t)__shfl_xor((int)m, 16));
+  if (L >= 64) step((uint32_t)__shfl_xor((int)m, 32));
+  return __uint_as_float(m);
 }
 
 __device__ __forceinline__ float quant_scale(float top) {
