@@ -414,9 +414,20 @@ size_t linear_frag_bytes(int32_t K, int32_t N, int32_t G, int w_type);
 // Lays out `blob` (device fp32, per group W [N][K] and b [N]).
 hipError_t launch_linear_layout(const float *blob, const LinearArgs &a, void *w, float *ws,
                                 float *bias, hipStream_t stream);
-// Whether rows of this width are too wide to be rounded to 8 bits while they
-// are staged.
-bool linear_needs_rows8(const LinearArgs &a);
+// Whether a call of n rows takes rows of x_type as they are.  If not, they are
+// given to it in the weights' type (8 bits: rounded, with scales) in rows of
+// 32 S bytes, zeros behind the last element.
+bool linear_takes(const LinearArgs &a, int x_type, int64_t n, int n_cu);
+// Such rows of 16 bits, or of 8 bits that are there already.
+struct ConvertArgs {
+  const void *x = nullptr;
+  int32_t x_type = 0, y_type = 0;
+  int64_t x_stride = 0;  // elements
+  int64_t n = 0;
+  int32_t K = 0, pad = 0;  // elements of a row of x and of y
+  void *y = nullptr;
+};
+hipError_t launch_convert(const ConvertArgs &a, hipStream_t stream);
 hipError_t launch_linear(const LinearArgs &a, int n_cu, hipStream_t stream);
 
 // flag <- 1 if any of the 2*n_edges indices lies outside [0, n_nodes).

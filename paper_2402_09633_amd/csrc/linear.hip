@@ -42,51 +42,64 @@ __device__ __forceinline__ void mma(typename Mma<WT>::acc &c, const i4 &x, const
                                                c, 0, 0, 0);
 }
 
-// Stages PM rows of a tile in LDS as the products read them, bytes
+// Stages the n rows of a tile in LDS as the products read them, bytes
 // [0, chunk) of a row from element k0 on.  L lanes hold a row, C units of eight
 // elements each (unit u0 + L c), so that a wave takes 64 / L rows at a time:
 // with QUANT the row's scale is formed from the same registers, and what it
-// costs is shared by the rows that the lanes work on at once.  FULL: kn = 8 L C.
-template <int WT, int XT, bool QUANT, int C, bool FULL>
+// costs is shared by the rows that the lanes work on at once.  B such passes are
+// loaded before the first is used.
+template <int WT, int XT, bool QUANT, int C, int B, int NW>
 __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *rows, float *scale,
-                                           unsigned char *lds, int pitch, int PM, int k0, int kn,
+                                           unsigned char *lds, int pitch, int n, int k0, int kn,
                                            int L) {
+  const bool full = kn == 8 * L * C;
+  constexpr int SURE = C >= 6 ? C - 2 : C - 1;  // units of a lane that end inside the row
   typedef typename std::conditional<WT == T_I8, u2, u4>::type unit;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int per = 64 / L;
   const int sub = lane / L, u0 = lane % L;
   const int cap = (int)(pitch - LDS_PAD) / (int)sizeof(unit);  // units a staged row holds
-  for (int r = wave * per + sub; r < PM; r += WAVES * per) {
-    Raw8<XT> raw[C];
-    const elem_t<XT> *row = (const elem_t<XT> *)a.x + (int64_t)rows[r] * a.x_stride + k0;
+  for (int rb = wave * per + sub; rb < n; rb += NW * per * B) {
+    Raw8<XT> raw[B][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-      raw[c] = FULL ? load8_full<XT>(row, 8 * (u0 + L * c)) : load8<XT>(row, 8 * (u0 + L * c), kn);
-    Quant z;
-    if constexpr (QUANT) {
-      uint32_t bits = 0;
+    for (int b = 0; b < B; ++b) {
+      const int r = min(rb + b * NW * per, n - 1);
+      const elem_t<XT> *row = (const elem_t<XT> *)a.x + (int64_t)rows[r] * a.x_stride + k0;
 #pragma unroll
-      for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[c], bits);
-      z = quant_of<XT>(lanes_max(top_of<XT>(bits), L));
-      if (u0 == 0) scale[r] = z.s;
+      for (int c = 0; c < C; ++c)
+        raw[b][c] = c < SURE || full ? load8<XT>(row, 8 * (u0 + L * c))
+                                     : load8_end<XT>(row, 8 * (u0 + L * c), kn);
     }
-    unsigned char *out = lds + r * pitch;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const int u = u0 + L * c;
-      unit q;
-      if constexpr (XT == WT)
-        q = __builtin_bit_cast(unit, raw[c].v);
-      else if constexpr (WT == T_I8)
-        q = quantize8<XT>(to_f32<XT>(raw[c]), z);
-      else if constexpr (WT == T_BF16)
-        q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[c]), bf8));
-      else
-        q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[c]), h8));
-      if (FULL || u < cap) *(unit *)(out + u * (int)sizeof(unit)) = q;
+    for (int b = 0; b < B; ++b) {
+      const int r = rb + b * NW * per;
+      if (r >= n) break;
+      Quant z;
+      if constexpr (QUANT) {
+        uint32_t bits = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[b][c], bits);
+        z = quant_of<XT>(lanes_max(top_of<XT>(bits), L));
+        if (u0 == 0) scale[r] = z.s;
+      }
+      unsigned char *out = lds + r * pitch;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const int u = u0 + L * c;
+        unit q;
+        if constexpr (XT == WT)
+          q = __builtin_bit_cast(unit, raw[b][c].v);
+        else if constexpr (WT == T_I8)
+          q = quantize8<XT>(to_f32<XT>(raw[b][c]), z);
+        else if constexpr (WT == T_BF16)
+          q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[b][c]), bf8));
+        else
+          q = __builtin_bit_cast(unit, __builtin_convertvector(to_f32<XT>(raw[b][c]), h8));
+        if (full || u < cap) *(unit *)(out + u * (int)sizeof(unit)) = q;
+      }
+      // units past the last lane's: zeros up to the staged width
+      for (int u = u0 + L * C; u < cap; u += L) *(unit *)(out + u * (int)sizeof(unit)) = unit{};
     }
-    // units past the last lane's: zeros up to the staged width
-    for (int u = u0 + L * C; u < cap; u += L) *(unit *)(out + u * (int)sizeof(unit)) = unit{};
   }
 }
 
@@ -94,21 +107,23 @@ __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *r
 // enough (a row's loads then span whole cache lines, and four rows share the
 // instructions that form their scales), more for wider rows, fewer for rows of
 // less than 16 units.  MAXU: the most units that a staged row of the calling
-// kernel can have.
-template <int WT, int XT, bool QUANT, int MAXU>
+// kernel can have; RB: its tiles' row blocks.
+template <int WT, int XT, bool QUANT, int MAXU, int RB, int NW>
 __device__ __forceinline__ void stage(const LinearArgs &a, const int32_t *rows, float *scale,
-                                      unsigned char *lds, int pitch, int PM, int k0, int kn) {
+                                      unsigned char *lds, int pitch, int n, int k0, int kn) {
   const int units = (kn + 7) / 8;
   int L = 16;
   while (L / 2 >= units) L /= 2;
   while (8 * L < units) L *= 2;
   const int C = (units + L - 1) / L;
-  auto go = [&](auto n) {
-    constexpr int CC = decltype(n)::value;
-    if (kn == 8 * CC * L)
-      stage_rows<WT, XT, QUANT, CC, true>(a, rows, scale, lds, pitch, PM, k0, kn, L);
-    else
-      stage_rows<WT, XT, QUANT, CC, false>(a, rows, scale, lds, pitch, PM, k0, kn, L);
+  auto go = [&](auto nc) {
+    constexpr int CC = decltype(nc)::value;
+    // passes in flight: the tile's (at 16 lanes to a row), or as many as 64
+    // registers hold
+    constexpr int fit = 64 / (CC * (XT == T_F32 ? 8 : XT == T_I8 ? 2 : 4));
+    constexpr int all = RB * 8 / NW;
+    constexpr int B = all < fit ? all : fit >= 4 ? 4 : fit >= 2 ? 2 : 1;
+    stage_rows<WT, XT, QUANT, CC, B, NW>(a, rows, scale, lds, pitch, n, k0, kn, L);
   };
   if (C <= 1) {
     go(std::integral_constant<int, 1>());
@@ -172,14 +187,47 @@ __device__ __forceinline__ void store_block(const LinearArgs &a, const f16v &v,
   }
 }
 
+// The epilogue of one block: scales and bias, rounding, store.
+template <int WT>
+__device__ __forceinline__ void finish_block(const LinearArgs &a,
+                                             const typename Mma<WT>::acc &acc, const float *scale,
+                                             const int64_t *row_at, int left, int ch, float ws,
+                                             float bias) {
+  const int hh = (threadIdx.x & 63) >> 5;
+  f16v v;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    if constexpr (WT == T_I8)
+      v[i] = __builtin_fmaf((float)acc[i] * ws, scale[8 * (i / 4) + 4 * hh + i % 4], bias);
+    else
+      v[i] = acc[i] + bias;
+  }
+  auto store = [&](auto type) {
+    constexpr int T = decltype(type)::value;
+    if (left >= 32 && (ch | 31) < a.N)
+      store_block<T, true>(a, v, row_at, 32, ch);
+    else
+      store_block<T, false>(a, v, row_at, left, ch);
+  };
+  if (a.y_type == T_F32)
+    store(std::integral_constant<int, T_F32>());
+  else if (a.y_type == T_BF16)
+    store(std::integral_constant<int, T_BF16>());
+  else
+    store(std::integral_constant<int, T_F16>());
+}
+
 // One row tile (PM = 32 RB rows of one group) by all waves: the rows are
 // staged once (MULTI: chunk by chunk, where they do not fit), the weights come
-// from the caches in fragment order.  A wave takes RBW of the tile's RB row
-// blocks and one block of 32 channels at a time.
-template <int WT, int XT, int RB, int RBW, bool MULTI>
-__global__ __launch_bounds__(64 * WAVES, 4) void linear_panel(LinearArgs a) {
-  constexpr int PM = 32 * RB;
-  constexpr int WR = RB / RBW, WN = WAVES / WR;  // waves by row blocks and by channel blocks
+// from the caches in fragment order, RING steps of them in flight.  A wave takes
+// the tile's RB row blocks and one block of 32 channels at a time.  WK waves share the steps of a block (few rows: a call is then bound by how long
+// the weights take, and all waves fetch them); their sums are added in LDS, in
+// the waves' order.
+template <int WT, int XT, int RB, int WK, int NW, bool MULTI>
+__global__ __launch_bounds__(64 * NW, RB > 1 ? 4 : 2) void linear_panel(LinearArgs a) {
+  constexpr int PM = 32 * RB, RING = RB == 1 ? 8 : 4;
+  constexpr int WN = NW / WK;  // channel blocks at a time
+  static_assert(WK == 1 || (RB == 1 && WK == NW), "one block to a workgroup");
   typedef typename Mma<WT>::acc acc_t;
   constexpr bool QUANT = WT == T_I8 && XT != T_I8;
   constexpr int MAXU = (RB > 1 ? HALF / PM - LDS_PAD : CHUNK) / (WT == T_I8 ? 8 : 16);
@@ -193,60 +241,110 @@ __global__ __launch_bounds__(64 * WAVES, 4) void linear_panel(LinearArgs a) {
   if (t.r0 >= t.r1) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int nrow = min(PM, t.r1 - t.r0);
-  if (tid < PM) {
-    const int p = t.r0 + min(tid, nrow - 1);
-    const int r = a.order ? clamp_idx(a.order[p], a.n) : p;
-    rows[tid] = r;
-    row_at[tid] = (a.y_order ? clamp_idx(a.y_order[p], a.n) : p) * a.y_stride;
-    if (WT == T_I8 && !QUANT) scale[tid] = a.xs[r];
-  }
   const int pitch = a.chunk + LDS_PAD;
   constexpr int esz = WT == T_I8 ? 1 : 2;
   const int steps = a.chunk / 32;  // of a chunk
   const int nchunk = MULTI ? (a.S + steps - 1) / steps : 1;
   const int ntile = (a.NB + WN - 1) / WN;
   const int col = lane & 31, hh = lane >> 5;
-  const int rb0 = (wave % WR) * RBW;
-  const unsigned char *xl = smem + (rb0 * 32 + col) * pitch + hh * 16;
+  const int wk = WK > 1 ? wave : 0;
+  const unsigned char *xl = smem + col * pitch + hh * 16;
+  i4 w[RING];
+  auto block_of = [&](int nt) { return nt * WN + (WK > 1 ? 0 : wave); };
+  auto weights_of = [&](int nb) {
+    return (const i4 *)a.w + ((int64_t)t.g * a.NB + min(nb, a.NB - 1)) * a.S * 64 + lane;
+  };
+  // this wave's steps of a chunk of n
+  auto first = [&](int n) { return WK > 1 ? n * wk / WK : 0; };
+  auto fill = [&](const i4 *wf, int s0, int s1) {
+#pragma unroll
+    for (int d = 0; d < RING; ++d) w[d] = wf[max(min(s0 + d, s1 - 1), 0) * 64];
+  };
+  const int n0 = MULTI ? min(steps, a.S) : a.S;
+  fill(weights_of(block_of(split)), first(n0), WK > 1 ? n0 * (wk + 1) / WK : n0);
+  if (tid < nrow) {
+    const int p = t.r0 + tid;
+    const int r = a.order ? clamp_idx(a.order[p], a.n) : p;
+    rows[tid] = r;
+    row_at[tid] = (a.y_order ? clamp_idx(a.y_order[p], a.n) : p) * a.y_stride;
+    if (WT == T_I8 && !QUANT) scale[tid] = a.xs[r];
+  }
   __syncthreads();
   if constexpr (!MULTI) {
-    stage<WT, XT, QUANT, MAXU>(a, rows, scale, smem, pitch, PM, 0, a.K);
+    stage<WT, XT, QUANT, MAXU, RB, NW>(a, rows, scale, smem, pitch, nrow, 0, a.K);
     __syncthreads();
   }
   for (int nt = split; nt < ntile; nt += a.nsplit) {
-    const int nb = nt * WN + wave / WR;
+    const int nb = block_of(nt);
     const bool live = nb < a.NB;
-    acc_t acc[RBW];
+    acc_t acc[RB];
 #pragma unroll
-    for (int r = 0; r < RBW; ++r)
+    for (int r = 0; r < RB; ++r)
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[r][v] = 0;
-    const i4 *wf = (const i4 *)a.w + ((int64_t)t.g * a.NB + min(nb, a.NB - 1)) * a.S * 64 + lane;
+    const i4 *wf = weights_of(nb);
     for (int ch = 0; ch < nchunk; ++ch) {
+      const int n = MULTI ? min(steps, a.S - ch * steps) : a.S;
+      const int s0 = first(n), s1 = WK > 1 ? n * (wk + 1) / WK : n;
+      const i4 *wc = MULTI ? wf + ch * steps * 64 : wf;
+      if (ch > 0 || (RB == 1 && nt > split)) fill(wc, s0, s1);
       if constexpr (MULTI) {
         const int k0 = ch * (a.chunk / esz);
         __syncthreads();
-        stage<WT, XT, false, MAXU>(a, rows, scale, smem, pitch, PM, k0, min(a.K - k0, a.chunk / esz));
+        stage<WT, XT, false, MAXU, RB, NW>(a, rows, scale, smem, pitch, nrow, k0,
+                                   min(a.K - k0, a.chunk / esz));
         __syncthreads();
       }
       if (!live) continue;
-      const int s1 = MULTI ? min(steps, a.S - ch * steps) : a.S;
-      const i4 *wc = MULTI ? wf + ch * steps * 64 : wf;
-      i4 w[2] = {wc[0], wc[64]};
-      for (int s = 0; s < s1; s += 2) {
-        const int sn = min(s + 2, s1 - 2);  // the next two steps' weights, in flight meanwhile
-        const i4 n0 = wc[sn * 64], n1 = wc[sn * 64 + 64];
+      auto step = [&](int s, int d) {
+        i4 x[RB];
 #pragma unroll
-        for (int d = 0; d < 2; ++d) {
-          i4 x[RBW];
+        for (int r = 0; r < RB; ++r) x[r] = *(const i4 *)(xl + r * 32 * pitch + (s + d) * 32);
 #pragma unroll
-          for (int r = 0; r < RBW; ++r)
-            x[r] = *(const i4 *)(xl + r * 32 * pitch + (s + d) * 32);
+        for (int r = 0; r < RB; ++r) mma<WT>(acc[r], x[r], w[d]);
+      };
+      if constexpr (RB > 1) {
+        // a row's steps are a multiple of RING: behind the last come the next
+        // block's first ones, ahead of this block's stores (loads and stores are
+        // counted together, in order)
+        const i4 *wn = nt + a.nsplit < ntile ? weights_of(block_of(nt + a.nsplit)) : nullptr;
+        for (int s = 0; s < s1; s += RING) {
+          const i4 *wl = s + RING < s1 ? wc + (s + RING) * 64 : wn;
 #pragma unroll
-          for (int r = 0; r < RBW; ++r) mma<WT>(acc[r], x[r], w[d]);
+          for (int d = 0; d < RING; ++d) {
+            step(s, d);
+            if (wl) w[d] = wl[d * 64];
+          }
         }
-        w[0] = n0;
-        w[1] = n1;
+      } else {
+        for (int s = s0; s < s1; s += RING) {
+#pragma unroll
+          for (int d = 0; d < RING; ++d) {
+            if (s + d >= s1) break;
+            step(s, d);
+            w[d] = wc[min(s + d + RING, s1 - 1) * 64];
+          }
+        }
+      }
+    }
+    if constexpr (WK > 1) {
+      // the staged rows have been read: their place takes the waves' sums
+      typedef decltype(acc[0][0] + acc[0][0]) val;
+      typedef val val4 __attribute__((ext_vector_type(4)));
+      val4 *part = (val4 *)smem;  // [wave][v / 4][lane]
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        part[(wave * 4 + q) * 64 + lane] =
+            val4{acc[0][4 * q], acc[0][4 * q + 1], acc[0][4 * q + 2], acc[0][4 * q + 3]};
+      __syncthreads();
+      if (wave > 0) return;  // one block to a workgroup: nothing is left
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        val4 sum = part[q * 64 + lane];
+        for (int k = 1; k < WK; ++k) sum += part[(k * 4 + q) * 64 + lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[0][4 * q + j] = sum[j];
       }
     }
     if (!live) continue;
@@ -254,31 +352,151 @@ __global__ __launch_bounds__(64 * WAVES, 4) void linear_panel(LinearArgs a) {
     const float bias = a.bias[(int64_t)t.g * a.NB * 32 + ch];
     const float ws = WT == T_I8 ? a.ws[(int64_t)t.g * a.NB * 32 + ch] : 1.f;
 #pragma unroll
-    for (int r = 0; r < RBW; ++r) {
-      const int r0 = (rb0 + r) * 32;
+    for (int r = 0; r < RB; ++r) {
+      const int r0 = r * 32;
       if (r0 >= nrow) break;
-      f16v v;
+      finish_block<WT>(a, acc[r], scale + r0, row_at + r0, nrow - r0, ch, ws, bias);
+    }
+  }
+}
+
+// ---- tiles for wide layers ----
+// Where a row does not fit beside its neighbours in LDS, the matrix cores bound
+// the layer, and every byte has to be used often once it is on the CU: tiles of
+// 64 TR rows x 256 channels, eight waves of 32 TR x 64.  The rows (already in
+// the weights' type, whole steps of 32 bytes) go through LDS, 128 bytes of each
+// at a time and two such stages in turn; a wave's weights come from the caches
+// into registers, in fragment order.  While a stage is multiplied, the next one's
+// weights and the rows of the one after it are in flight.
+constexpr int T_STEPS = 4;                // steps of 32 bytes in a stage
+constexpr int T_BYTES = 32 * T_STEPS;     // of a row
+constexpr int T_CH = 8;                   // channel blocks of a tile
+
+template <int WT, int TR>
+__global__ __launch_bounds__(64 * WAVES, 2) void linear_tiled(LinearArgs a) {
+  constexpr int PM = 64 * TR;             // rows of a tile
+  constexpr int LOADS = PM / (8 * WAVES);  // 16-byte loads of a lane a stage
+  typedef typename Mma<WT>::acc acc_t;
+  __shared__ __align__(16) unsigned char xs[2][PM * T_BYTES];
+  __shared__ int64_t row_at[PM];
+  __shared__ float scale[PM];
+  const int ntile = (a.NB + T_CH - 1) / T_CH;
+  const int bid = xcd_remap(blockIdx.x, gridDim.x);
+  // eight row tiles side by side go through the channels together, so that they
+  // share the weights in an XCD's cache, and the channels the rows
+  const int tiles = gridDim.x / ntile, band = 8 * ntile;
+  const int b0 = bid / band * 8, wide = min(8, tiles - b0);
+  const int tile = b0 + bid % band % wide, nt = bid % band / wide;
+  const TileRows t = find_tile(a.off, a.G, a.n, tile, PM);
+  if (t.r0 >= t.r1) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int nrow = min(PM, t.r1 - t.r0);
+  auto row_of = [&](int i) {
+    const int p = t.r0 + min(i, nrow - 1);
+    return a.order ? clamp_idx(a.order[p], a.n) : p;
+  };
+  for (int i = tid; i < PM; i += 64 * WAVES) {
+    const int p = t.r0 + min(i, nrow - 1);
+    row_at[i] = (a.y_order ? clamp_idx(a.y_order[p], a.n) : p) * a.y_stride;
+    if (WT == T_I8) scale[i] = a.xs[row_of(i)];
+  }
+  // A wave's load takes 8 rows of 128 bytes; the 16-byte chunk c of row r lies
+  // at place c ^ (r % 8), so that the lanes of a product's read (32 rows, one
+  // chunk) meet every bank alike.
+  const int c = (lane & 7) ^ (lane >> 3);
+  constexpr int esz = WT == T_I8 ? 1 : 2;
+  const unsigned char *src[LOADS];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if constexpr (WT == T_I8)
-          v[i] = __builtin_fmaf((float)acc[r][i] * ws, scale[r0 + 8 * (i / 4) + 4 * hh + i % 4],
-                                bias);
-        else
-          v[i] = acc[r][i] + bias;
-      }
-      auto store = [&](auto type) {
-        constexpr int T = decltype(type)::value;
-        if (nrow - r0 >= 32 && nb * 32 + 32 <= a.N)
-          store_block<T, true>(a, v, row_at + r0, 32, ch);
-        else
-          store_block<T, false>(a, v, row_at + r0, nrow - r0, ch);
-      };
-      if (a.y_type == T_F32)
-        store(std::integral_constant<int, T_F32>());
-      else if (a.y_type == T_BF16)
-        store(std::integral_constant<int, T_BF16>());
-      else
-        store(std::integral_constant<int, T_F16>());
+  for (int i = 0; i < LOADS; ++i)
+    src[i] = (const unsigned char *)a.x +
+             (int64_t)row_of((i * WAVES + wave) * 8 + (lane >> 3)) * a.x_stride * esz;
+  const int bytes = a.K * esz;  // whole chunks of 16; zeros behind them
+  auto load = [&](i4(&r)[LOADS], int st) {
+    const int at = st * T_BYTES + c * 16;
+    const int from = at < bytes ? at : 0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) __builtin_memcpy(&r[i], src[i] + from, 16);
+  };
+  auto put = [&](const i4(&r)[LOADS], int buf, int st) {
+    const bool in = st * T_BYTES + c * 16 < bytes;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+      *(i4 *)(xs[buf] + (i * WAVES + wave) * 1024 + lane * 16) = in ? r[i] : i4{0, 0, 0, 0};
+  };
+  const int wr = wave & 1, wc = wave >> 1;
+  const int nb0 = nt * T_CH + wc * 2;
+  const i4 *wf[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    wf[i] = (const i4 *)a.w + ((int64_t)t.g * a.NB + min(nb0 + i, a.NB - 1)) * a.S * 64 + lane;
+  i4 w[T_STEPS][2];
+  auto weights = [&](int s, int st) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) w[s][i] = wf[i][min(st * T_STEPS + s, a.S - 1) * 64];
+  };
+  acc_t acc[2][TR];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < TR; ++r)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][r][v] = 0;
+  const int col = lane & 31, hh = lane >> 5;
+  // A step's products, with the next step's rows on their way from LDS, and
+  // behind them the same step's weights of the next stage.
+  auto multiply = [&](int buf, int st) {
+    const unsigned char *x0 = xs[buf] + (wr * TR * 32 + col) * T_BYTES;
+    i4 x[2][TR];
+    auto read = [&](int s) {
+#pragma unroll
+      for (int r = 0; r < TR; ++r)
+        x[s & 1][r] = *(const i4 *)(x0 + r * 32 * T_BYTES + (((2 * s + hh) ^ (col & 7)) * 16));
+    };
+    read(0);
+#pragma unroll
+    for (int s = 0; s < T_STEPS; ++s) {
+      if (s + 1 < T_STEPS) read(s + 1);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int r = 0; r < TR; ++r) mma<WT>(acc[i][r], x[s & 1][r], w[s][i]);
+      weights(s, st + 1);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  const int stages = a.S / T_STEPS;
+  i4 rows[LOADS];
+  load(rows, 0);
+#pragma unroll
+  for (int s = 0; s < T_STEPS; ++s) weights(s, 0);
+  put(rows, 0, 0);
+  load(rows, 1);
+  __syncthreads();
+  int st = 0;
+  for (; st + 1 < stages; st += 2) {
+    put(rows, 1, st + 1);
+    load(rows, st + 2);
+    multiply(0, st);
+    __syncthreads();
+    put(rows, 0, st + 2);
+    load(rows, st + 3);
+    multiply(1, st + 1);
+    __syncthreads();
+  }
+  if (st < stages) {
+    multiply(0, st);
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (nb0 + i >= a.NB) break;
+    const int ch = (nb0 + i) * 32 + col;
+    const float bias = a.bias[(int64_t)t.g * a.NB * 32 + ch];
+    const float ws = WT == T_I8 ? a.ws[(int64_t)t.g * a.NB * 32 + ch] : 1.f;
+#pragma unroll
+    for (int r = 0; r < TR; ++r) {
+      const int r0 = (wr * TR + r) * 32;
+      if (r0 >= nrow) break;
+      finish_block<WT>(a, acc[i][r], scale + r0, row_at + r0, nrow - r0, ch, ws, bias);
     }
   }
 }
@@ -336,44 +554,56 @@ __global__ __launch_bounds__(256) void linear_layout(const float *__restrict__ b
   }
 }
 
-// What a launch of the row panels needs: RB row blocks to a tile, RBW to a
-// wave, rows staged whole or in chunks.
+// What a launch of the row panels needs: RB row blocks to a tile, NW waves, rows
+// staged whole or in chunks (multi).
 struct Plan {
-  int RB, RBW;
-  bool multi;
+  int RB, NW;
+  bool multi, split;  // split: the waves share a block's steps
   int64_t tiles;
 };
 
-template <int WT, int XT, int RB, int RBW, bool MULTI>
+template <int WT, int XT, int RB, int WK, int NW, bool MULTI>
 hipError_t panel(const LinearArgs &a, const Plan &p, hipStream_t stream) {
-  const size_t lds = (size_t)32 * RB * (a.chunk + LDS_PAD);
-  return launch_lds(linear_panel<WT, XT, RB, RBW, MULTI>, dim3((uint32_t)(p.tiles * a.nsplit)),
-                    dim3(64 * WAVES), lds, stream, a);
+  size_t lds = (size_t)32 * RB * (a.chunk + LDS_PAD);
+  if (WK > 1 && lds < 4096 * NW) lds = 4096 * NW;
+  return launch_lds(linear_panel<WT, XT, RB, WK, NW, MULTI>,
+                    dim3((uint32_t)(p.tiles * a.nsplit)), dim3(64 * NW), lds, stream, a);
 }
 
 template <int WT, int XT>
 hipError_t panel_rows(const LinearArgs &a, const Plan &p, hipStream_t stream) {
   if (p.multi) {
-    if constexpr (WT != T_I8 || XT == T_I8) return panel<WT, XT, 1, 1, true>(a, p, stream);
+    if constexpr (WT != T_I8 || XT == T_I8) {
+      if (p.split) return panel<WT, XT, 1, 8, 8, true>(a, p, stream);
+      return panel<WT, XT, 1, 1, 8, true>(a, p, stream);
+    }
     return hipErrorInvalidValue;  // such rows are rounded beforehand
   }
   if (p.RB == 4) {
-    if (p.RBW == 4) return panel<WT, XT, 4, 4, false>(a, p, stream);
-    if (p.RBW == 2) return panel<WT, XT, 4, 2, false>(a, p, stream);
-    return panel<WT, XT, 4, 1, false>(a, p, stream);
+    if (p.NW == 8) return panel<WT, XT, 4, 1, 8, false>(a, p, stream);
+    return panel<WT, XT, 4, 1, 4, false>(a, p, stream);
   }
   if (p.RB == 2) {
-    if (p.RBW == 2) return panel<WT, XT, 2, 2, false>(a, p, stream);
-    return panel<WT, XT, 2, 1, false>(a, p, stream);
+    if (p.NW == 8) return panel<WT, XT, 2, 1, 8, false>(a, p, stream);
+    return panel<WT, XT, 2, 1, 4, false>(a, p, stream);
   }
-  return panel<WT, XT, 1, 1, false>(a, p, stream);
+  if (p.split) return panel<WT, XT, 1, 8, 8, false>(a, p, stream);
+  return panel<WT, XT, 1, 1, 8, false>(a, p, stream);
+}
+
+template <int WT>
+hipError_t tiled(const LinearArgs &a, int TR, hipStream_t stream) {
+  const int64_t PM = 64 * TR, tiles = a.off ? a.n / PM + a.G : (a.n + PM - 1) / PM;
+  const dim3 grid((uint32_t)(tiles * ((a.NB + T_CH - 1) / T_CH))), block(64 * WAVES);
+  if (TR == 4) return launch(linear_tiled<WT, 4>, grid, block, 0, stream, a);
+  return launch(linear_tiled<WT, 2>, grid, block, 0, stream, a);
 }
 
 }  // namespace
 
 int32_t linear_steps(int32_t K, int w_type) {
-  const int per = w_type == T_I8 ? 64 : 32;  // elements of two steps
-  return 2 * ((K + per - 1) / per);
+  const int per = w_type == T_I8 ? 128 : 64;  // elements of four steps
+  return 4 * ((K + per - 1) / per);
 }
 
 size_t linear_frag_bytes(int32_t K, int32_t N, int32_t G, int w_type) {
@@ -393,12 +623,47 @@ hipError_t launch_linear_layout(const float *blob, const LinearArgs &a, void *w,
                 bias);
 }
 
-bool linear_needs_rows8(const LinearArgs &a) { return a.S * 32 > CHUNK; }
+// Whether the tiles for wide layers take a call of n rows, and with how many
+// row blocks to a wave (0: the row panels do).  Measured (panels : tiles, us):
+//  - rows up to 1 KB: 100000 x 512 -> 512 bf16 87 : 88, 300000 x 128 -> 128 bf16
+//    42 : 54; past it 100000 x 640 -> 640 159 : 129, 1024 -> 256 107 : 74,
+//    2048 -> 512 367 : 247
+//  - 8-bit layers whose rows come as floats pay for a pass over the rows first:
+//    100000 x 1024 -> 1024 195 : 241, 2048 -> 512 242 : 269, but 30000 x 1024 ->
+//    2048 128 : 110
+//  - few tiles leave CUs idle: 1000 x 4096 -> 512 bf16 30 : 62, 300 x 4096 -> 4096
+//    43 : 63, 4000 x 2048 -> 2048 69 : 42; 32 groups of 312 rows x 1024 -> 1024
+//    43 : 47, of 937 118 : 99
+//  - 256 rows to a tile where that gives every CU one: 16384 x 4096 -> 4096 8-bit
+//    288, with 128 rows 321; 2048 x 4096 -> 4096 55 and 39
+int tiled_rows(const LinearArgs &a, int x_type, int64_t n, int n_cu) {
+  const int ntile = (a.NB + T_CH - 1) / T_CH;
+  const bool rounds = a.w_type == T_I8 && x_type != T_I8;
+  if (a.S * 32 < (rounds ? 1024 : 1025) || a.NB <= (rounds ? 32 : 4)) return 0;
+  if (n / a.G < 512 || n / 128 * ntile < n_cu / 2) return 0;
+  return n / 256 * ntile >= n_cu ? 4 : 2;
+}
+
+bool linear_takes(const LinearArgs &a, int x_type, int64_t n, int n_cu) {
+  if (tiled_rows(a, x_type, n, n_cu))
+    return x_type == a.w_type && a.K * type_bytes(a.w_type) % 16 == 0;
+  if (a.w_type == T_I8) return x_type == T_I8 || a.S * 32 <= CHUNK;
+  return x_type == T_F32 || x_type == a.w_type;
+}
 
 hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
   LinearArgs a = args;
+  if (const int TR = tiled_rows(a, a.x_type, a.n, n_cu)) {
+    if (a.w_type == T_I8) return tiled<T_I8>(a, TR, stream);
+    if (a.w_type == T_BF16) return tiled<T_BF16>(a, TR, stream);
+    return tiled<T_F16>(a, TR, stream);
+  }
   // The rows of a tile stay in LDS: 128 of them where two workgroups' fit on a
   // CU, fewer of wide ones and where there are too few tiles to fill the CUs.
+  // Layers of up to four channel blocks keep four waves busy: smaller workgroups,
+  // and more of them to a CU (300000 x 128 -> 128 bf16 37 us with four waves, 44
+  // with eight; 1000513 x 384 -> 128 f16 272 and 298).  Wider ones take eight
+  // (300000 x 512 -> 512 8-bit 187 us, 201 with four waves and 64 rows).
   Plan p;
   const int row_bytes = a.S * 32;
   p.multi = row_bytes > CHUNK;
@@ -407,17 +672,20 @@ hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
     const int64_t PM = 32 * RB;
     return a.off ? a.n / PM + a.G : (a.n + PM - 1) / PM;
   };
+  p.NW = a.NB <= 4 ? 4 : WAVES;
+  const int room = p.NW == WAVES ? HALF : HALF / 2;
   p.RB = p.multi ? 1 : 4;
-  while (p.RB > 1 && (32 * p.RB * (a.chunk + LDS_PAD) > HALF || a.n / (32 * p.RB) < 2 * n_cu))
+  while (p.RB > 1 && (32 * p.RB * (a.chunk + LDS_PAD) > (p.RB == 4 ? room : HALF) ||
+                      a.n / (32 * p.RB) < 2 * n_cu))
     p.RB /= 2;
+  if (p.RB == 1) p.NW = WAVES;
   p.tiles = tiles(p.RB);
-  // Few channel blocks: the waves share out a tile's row blocks as well.
-  p.RBW = p.RB;
-  while (p.RBW > 1 && a.NB <= WAVES / (p.RB / p.RBW) / 2) p.RBW /= 2;
-  const int WN = WAVES / (p.RB / p.RBW);
+  // So few blocks that the CUs are not filled: all waves to each.
+  p.split = p.RB == 1 && p.tiles * a.NB <= 4 * n_cu && a.S >= 2 * WAVES;
+  const int WN = p.split ? 1 : p.NW;
   const int ntile = (a.NB + WN - 1) / WN;
   a.nsplit = (int)((2 * n_cu + p.tiles - 1) / p.tiles);
-  if (a.nsplit > ntile) a.nsplit = ntile;
+  if (a.nsplit > ntile || p.split) a.nsplit = ntile;
   if (a.w_type == T_I8) {
     if (a.x_type == T_I8) return panel_rows<T_I8, T_I8>(a, p, stream);
     if (a.x_type == T_F32) return panel_rows<T_I8, T_F32>(a, p, stream);
@@ -426,11 +694,9 @@ hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
   }
   if (a.w_type == T_BF16) {
     if (a.x_type == T_F32) return panel_rows<T_BF16, T_F32>(a, p, stream);
-    if (a.x_type == T_BF16) return panel_rows<T_BF16, T_BF16>(a, p, stream);
-    return panel_rows<T_BF16, T_F16>(a, p, stream);
+    return panel_rows<T_BF16, T_BF16>(a, p, stream);
   }
   if (a.x_type == T_F32) return panel_rows<T_F16, T_F32>(a, p, stream);
-  if (a.x_type == T_BF16) return panel_rows<T_F16, T_BF16>(a, p, stream);
   return panel_rows<T_F16, T_F16>(a, p, stream);
 }
 

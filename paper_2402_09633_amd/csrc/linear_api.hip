@@ -108,33 +108,48 @@ int check_linear_dims(const gnn_linear_dims *d) {
   return GNN_OK;
 }
 
-// Scratch of a call: 8-bit rows and their scales, where the rows come as
-// floats and are too wide to be rounded while they are staged.
+// Scratch of a call: its rows in the form that the kernels take, and 8-bit
+// rows' scales, where they do not take the caller's.
 size_t linear_scratch(const gnn_linear *l, int x_type, int64_t n_rows) {
-  if (l->dims.dtype != GNN_INT8 || x_type == GNN_INT8) return 0;
-  if (!linear_needs_rows8(l->tmpl)) return 0;
-  return up256((size_t)n_rows * l->tmpl.S * 32) + up256((size_t)n_rows * 4);
+  if (linear_takes(l->tmpl, x_type, n_rows, l->n_cu)) return 0;
+  const bool round8 = l->dims.dtype == GNN_INT8 && x_type != GNN_INT8;
+  return up256((size_t)n_rows * l->tmpl.S * 32) + (round8 ? up256((size_t)n_rows * 4) : 0);
 }
 
 // The launches of a layer; everything has been checked.
 int run_linear(const gnn_linear *l, LinearArgs a, unsigned char *ws, hipStream_t stream) {
-  const size_t need = linear_scratch(l, a.x_type, a.n);
-  if (need) {
-    QuantArgs q;
-    q.x = a.x;
-    q.x_type = a.x_type;
-    q.x_stride = a.x_stride;
-    q.n = a.n;
-    q.K = a.K;
-    q.q = (int8_t *)ws;
-    q.q_stride = q.pad = a.S * 32;
-    q.scales = (float *)(ws + up256((size_t)a.n * a.S * 32));
-    const int rc = launched(launch_quantize(q, stream), "row rounding");
+  if (!linear_takes(a, a.x_type, a.n, l->n_cu)) {
+    hipError_t e;
+    const int pad = a.S * 32 / type_bytes(a.w_type);
+    if (a.w_type == GNN_INT8 && a.x_type != GNN_INT8) {
+      QuantArgs q;
+      q.x = a.x;
+      q.x_type = a.x_type;
+      q.x_stride = a.x_stride;
+      q.n = a.n;
+      q.K = a.K;
+      q.q = (int8_t *)ws;
+      q.q_stride = q.pad = pad;
+      q.scales = (float *)(ws + up256((size_t)a.n * a.S * 32));
+      a.xs = q.scales;
+      e = launch_quantize(q, stream);
+    } else {
+      ConvertArgs c;
+      c.x = a.x;
+      c.x_type = a.x_type;
+      c.y_type = a.w_type;
+      c.x_stride = a.x_stride;
+      c.n = a.n;
+      c.K = a.K;
+      c.pad = pad;
+      c.y = ws;
+      e = launch_convert(c, stream);
+    }
+    const int rc = launched(e, "row conversion");
     if (rc) return rc;
-    a.x = q.q;
-    a.x_type = GNN_INT8;
-    a.x_stride = q.q_stride;
-    a.xs = q.scales;
+    a.x = ws;
+    a.x_type = a.w_type;
+    a.x_stride = pad;
   }
   return launched(launch_linear(a, l->n_cu, stream), "linear layer");
 }

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L
   Raw8<XT> raw[C];
 #pragma unroll
   for (int c = 0; c < C; ++c)
-    raw[c] = FULL ? load8_full<XT>(row, 8 * (u0 + L * c)) : load8<XT>(row, 8 * (u0 + L * c), a.K);
+    raw[c] = FULL ? load8<XT>(row, 8 * (u0 + L * c)) : load8_end<XT>(row, 8 * (u0 + L * c), a.K);
   uint32_t bits = 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) bits = max_bits<XT>(raw[c], bits);
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
   const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
   uint32_t bits = 0;
   for (int k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
-    bits = max_bits<XT>(load8<XT>(row, k, a.K), bits);
+    bits = max_bits<XT>(load8_end<XT>(row, k, a.K), bits);
   float top = top_of<XT>(bits);
   top = lanes_max(top, 64);
   if ((tid & 63) == 0) part[tid >> 6] = top;
@@ -74,7 +74,7 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
   int8_t *q = a.q + r * a.q_stride;
   const int width = a.pad ? a.pad : a.K;
   for (int k = 8 * tid; k < width; k += 8 * 64 * Q_WAVES)
-    store_q8(q, k, width, quantize8<XT>(to_f32<XT>(load8<XT>(row, k, a.K)), z));
+    store_q8(q, k, width, quantize8<XT>(to_f32<XT>(load8_end<XT>(row, k, a.K)), z));
 }
 
 template <int XT>
@@ -101,6 +101,38 @@ hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
   return go(std::integral_constant<int, 8>());
 }
 
+// ---- rows in another type ----
+// A thread to eight elements; zeros from K up to the padded width.
+template <int XT, int YT>
+__global__ __launch_bounds__(256) void convert_rows(ConvertArgs a) {
+  const int units = a.pad / 8;
+  const int64_t all = a.n * units;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all;
+       i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / units;
+    const int k = (int)(i - r * units) * 8;
+    const Raw8<XT> x = load8_end<XT>((const elem_t<XT> *)a.x + r * a.x_stride, k, a.K);
+    Raw8<YT> y;
+    if constexpr (XT == YT)
+      y = x;
+    else
+      y.v = __builtin_convertvector(to_f32<XT>(x), typename Raw8<YT>::vec);
+    __builtin_memcpy((elem_t<YT> *)a.y + i * 8, &y.v, sizeof y.v);
+  }
+}
+
+template <int XT>
+hipError_t convert_t(const ConvertArgs &a, hipStream_t stream) {
+  const int64_t wgs = (a.n * (a.pad / 8) + 255) / 256;
+  const dim3 grid((uint32_t)(wgs < (1 << 20) ? wgs : 1 << 20)), block(256);
+  if constexpr (XT == T_I8) {
+    return launch(convert_rows<T_I8, T_I8>, grid, block, 0, stream, a);
+  } else {
+    if (a.y_type == T_BF16) return launch(convert_rows<XT, T_BF16>, grid, block, 0, stream, a);
+    return launch(convert_rows<XT, T_F16>, grid, block, 0, stream, a);
+  }
+}
+
 // ---- LayerNorm and ReLU of hidden rows ----
 // A wave to a row: mean, then variance of the centred values, both in fp32
 // from registers (C units of eight a lane; rows of up to 4096).
@@ -114,7 +146,7 @@ __device__ __forceinline__ void norm_row(const NormArgs &a, int64_t p, int lane)
   float s = 0.f;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    x[c] = load8<T_F32>(row, 8 * (lane + 64 * c), a.H).v;
+    x[c] = load8_end<T_F32>(row, 8 * (lane + 64 * c), a.H).v;
 #pragma unroll
     for (int j = 0; j < 8; ++j) s += x[c][j];
   }
@@ -134,7 +166,7 @@ __device__ __forceinline__ void norm_row(const NormArgs &a, int64_t p, int lane)
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int k = 8 * (lane + 64 * c);
-    const f8 gg = load8<T_F32>(gm, k, a.H).v, bb = load8<T_F32>(bt, k, a.H).v;
+    const f8 gg = load8_end<T_F32>(gm, k, a.H).v, bb = load8_end<T_F32>(bt, k, a.H).v;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const float v = x[c][j] * rstd * gg[j] + bb[j];
@@ -393,6 +425,13 @@ hipError_t launch_quantize(const QuantArgs &a, hipStream_t stream) {
   if (a.x_type == T_F32) return quantize_t<T_F32>(a, stream);
   if (a.x_type == T_BF16) return quantize_t<T_BF16>(a, stream);
   return quantize_t<T_F16>(a, stream);
+}
+
+hipError_t launch_convert(const ConvertArgs &a, hipStream_t stream) {
+  if (a.x_type == T_F32) return convert_t<T_F32>(a, stream);
+  if (a.x_type == T_BF16) return convert_t<T_BF16>(a, stream);
+  if (a.x_type == T_F16) return convert_t<T_F16>(a, stream);
+  return convert_t<T_I8>(a, stream);
 }
 
 hipError_t launch_norm(const NormArgs &a, hipStream_t stream) {

@@ -47,24 +47,55 @@ struct Raw8 {
   vec v;
 };
 
-// Elements k .. k + 7 of a row of K; zeros from K on, which is not read past.
+// Elements k .. k + 7 of a row.
 template <int T>
-__device__ __forceinline__ Raw8<T> load8(const elem_t<T> *row, int k, int K) {
+__device__ __forceinline__ Raw8<T> load8(const elem_t<T> *row, int k) {
   Raw8<T> r;
-  if (k + 8 <= K) {
-    __builtin_memcpy(&r.v, row + k, sizeof r.v);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r.v[j] = k + j < K ? row[k + j] : (elem_t<T>)0;
-  }
+  __builtin_memcpy(&r.v, row + k, sizeof r.v);
   return r;
 }
 
-// load8 where the row is known to hold all eight.
+// The same of a row of K, with zeros from K on, which is not read past: from K
+// >= 8 on, the row's last eight elements moved down by as many as lie before k.
 template <int T>
-__device__ __forceinline__ Raw8<T> load8_full(const elem_t<T> *row, int k) {
-  Raw8<T> r;
-  __builtin_memcpy(&r.v, row + k, sizeof r.v);
+__device__ __forceinline__ Raw8<T> load8_end(const elem_t<T> *row, int k, int K) {
+  if (K < 8) {  // the same for all lanes
+    Raw8<T> r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r.v[j] = k + j < K ? row[k + j] : (elem_t<T>)0;
+    return r;
+  }
+  const int at = min(k, K - 8), d = min(k - at, 8);
+  Raw8<T> r = load8<T>(row, at);
+  if constexpr (T == T_I8) {
+    const uint64_t v = __builtin_bit_cast(uint64_t, r.v);
+    const uint64_t m = d < 8 ? v >> (8 * d) : 0;
+    r.v = __builtin_bit_cast(typename Raw8<T>::vec, m);
+  } else {
+    if constexpr (T == T_F32) {
+#pragma unroll
+      for (int b = 1; b <= 8; b *= 2)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float up = j + b < 8 ? r.v[j + b] : 0.f;
+          r.v[j] = d & b ? up : r.v[j];
+        }
+    } else {
+      u4 w = __builtin_bit_cast(u4, r.v);
+#pragma unroll
+      for (int b = 1; b <= 4; b *= 2)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t up = j + b < 4 ? w[j + b] : 0u;
+          w[j] = d & (2 * b) ? up : w[j];
+        }
+      const uint32_t odd = 16 * (d & 1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        w[j] = (uint32_t)((((uint64_t)(j < 3 ? w[j + 1] : 0u) << 32) | w[j]) >> odd);
+      r.v = __builtin_bit_cast(typename Raw8<T>::vec, w);
+    }
+  }
   return r;
 }
 
@@ -139,11 +170,14 @@ __device__ __forceinline__ float quant_scale(float top) {
 // one number, below 2^11 but for powers of two).  In the second case x / s and
 // x * f, for f within 2^-23 of 1 / c, lie on the same side.  In the first the
 // sign of d says where x / s lies, and f is taken on that side of 1 / c.  Where
-// d = 0 the quotient is a true tie: such rows (s is a 16-bit number, or nearly)
-// are rounded by quant_exact.
+// d = 0 the quotient is a true tie: the whole numbers that a factor below and
+// one above 1 / c lead to are then its neighbours, and half their sum rounds to
+// the even one (without a tie they are the same).
 //
-// fp32.  Two factors, one step below and above 1 / s, round alike unless x / s
-// is next to a half; then quant_exact decides.
+// fp32.  Factors one step below and above 1 / s round alike unless x / s is next
+// to a half.  Then half the sum h of what they lead to is that half, and x - h s
+// says on which side x / s lies (exact in fp32: a multiple of the smaller of
+// ulp(x) and ulp(s), below s).
 struct Quant {
   float s, lo, hi;
   bool zero, tie;
@@ -158,9 +192,7 @@ __device__ __forceinline__ Quant quant_of(float top) {
   Quant q;
   q.s = quant_scale(top);
   q.zero = !(q.s > 0.f);
-  q.lo = q.hi = 0.f;
   q.tie = false;
-  if (q.zero) return q;
   if constexpr (T == T_F32) {
     const float inv = 1.f / q.s;
     q.lo = step_up(inv, -1);
@@ -168,23 +200,12 @@ __device__ __forceinline__ Quant quant_of(float top) {
   } else {
     const float d = __builtin_fmaf(q.s, 127.f, -top);
     const float f = 127.f / top, e = __builtin_fmaf(f, top, -127.f);
-    q.lo = d > 0.f ? (e >= 0.f ? step_up(f, -1) : f) : (e <= 0.f ? step_up(f, 1) : f);
+    const float below = e >= 0.f ? step_up(f, -1) : f, above = e <= 0.f ? step_up(f, 1) : f;
+    q.lo = d >= 0.f ? below : above;
+    q.hi = above;
     q.tie = d == 0.f;
   }
   return q;
-}
-
-// Nearest whole number to x / s.  t = x / s is off by less than 2e-5 before its
-// rounding, so the whole number next to it on the other side is the only other
-// candidate; x - t s decides, which is exact in fp32 (a multiple of the smaller
-// of ulp(x) and ulp(s), below s).
-__device__ __forceinline__ float quant_exact(float x, float s, float inv) {
-  float t = rintf(x * inv);
-  const float r2 = 2.f * __builtin_fmaf(-t, s, x);
-  const float dir = r2 > 0.f ? 1.f : -1.f;
-  const bool odd = t - 2.f * truncf(0.5f * t) != 0.f;
-  if (fabsf(r2) > s || (fabsf(r2) == s && odd)) t += dir;
-  return t;
 }
 
 constexpr float ROUND_MAGIC = 12582912.f;
@@ -209,20 +230,33 @@ __device__ __forceinline__ u2 quantize8(const f8 &x, const Quant &z) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) t[j] = __builtin_fmaf(x[j], z.lo, ROUND_MAGIC);
   u2 q = pack_bytes(t);
-  bool exact = z.tie;
   if constexpr (T == T_F32) {
     float u[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) u[j] = __builtin_fmaf(x[j], z.hi, ROUND_MAGIC);
     const u2 p = pack_bytes(u);
-    exact = p[0] != q[0] || p[1] != q[1];
-  }
-  if (exact) {
+    if (((p[0] ^ q[0]) | (p[1] ^ q[1])) != 0 || z.zero) {
+      asm volatile("");  // a branch, not selected values: it is hardly ever taken
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = quant_exact(x[j], z.s, z.lo) + ROUND_MAGIC;
+      for (int j = 0; j < 8; ++j) {
+        const float h = 0.5f * ((t[j] - ROUND_MAGIC) + (u[j] - ROUND_MAGIC));
+        const float r = __builtin_fmaf(-h, z.s, x[j]);
+        t[j] = (h + (r == 0.f ? 0.f : __builtin_copysignf(0.25f, r))) + ROUND_MAGIC;
+      }
+      q = pack_bytes(t);
+      if (z.zero) q = u2{0u, 0u};
+    }
+  } else if (z.tie || z.zero) {
+    asm volatile("");
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float u = __builtin_fmaf(x[j], z.hi, ROUND_MAGIC);
+      t[j] = 0.5f * ((t[j] - ROUND_MAGIC) + (u - ROUND_MAGIC)) + ROUND_MAGIC;
+    }
     q = pack_bytes(t);
+    if (z.zero) q = u2{0u, 0u};
   }
-  return z.zero ? u2{0u, 0u} : q;
+  return q;
 }
 
 // launch() with more than 64 KiB of dynamic LDS allowed.
@@ -253,21 +287,24 @@ __device__ __forceinline__ TileRows find_tile(const int32_t *__restrict__ off, i
                                               int32_t n_rows, int32_t tile, int32_t PM) {
   if (!off) return TileRows{0, tile * PM, n_rows};
   const int lane = threadIdx.x & 63;
-  auto at = [&](int32_t g) { return min(max(off[g], 0), n_rows); };
-  int32_t base = 0, step = (G + 63) / 64;
+  auto at = [&](int32_t g) { return min(max(off[min(g, G)], 0), n_rows); };
+  int32_t base = 0;
+  const int32_t step = (G + 63) / 64;
   if (step > 1) {
     const int32_t g = lane * step;
-    const uint64_t m = __ballot(g < G && at(min(g, G - 1)) / PM + g <= tile);
+    const uint64_t m = __ballot(g < G && at(g) / PM + g <= tile);
     base = (max((int)__popcll(m), 1) - 1) * step;
   }
   // the last of up to 64 groups from base on whose first number is <= tile
   const int32_t g = base + lane;
   const bool in = lane < (step > 1 ? step : 64) && g < G;
-  const uint64_t m = __ballot(in && at(min(g, G - 1)) / PM + g <= tile);
+  const int32_t first = at(g), end = at(g + 1);
+  const uint64_t m = __ballot(in && first / PM + g <= tile);
   const int32_t n = __popcll(m);
   if (n == 0) return TileRows{0, 0, 0};
   const int32_t gg = base + n - 1;
-  const int32_t lo = at(gg), hi = at(gg + 1);
+  const int32_t lo = __builtin_amdgcn_readlane(first, n - 1),
+                hi = __builtin_amdgcn_readlane(end, n - 1);
   const int64_t r0 = lo + (int64_t)(tile - (lo / PM + gg)) * PM;
   if (r0 < lo || r0 >= hi) return TileRows{gg, 0, 0};
   return TileRows{gg, (int32_t)r0, hi};
