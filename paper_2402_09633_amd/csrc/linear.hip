@@ -48,11 +48,16 @@ __device__ __forceinline__ void mma(typename Mma<WT>::acc &c, const i4 &x, const
 // with QUANT the row's scale is formed from the same registers, and what it
 // costs is shared by the rows that the lanes work on at once.  B such passes are
 // loaded before the first is used.
-template <int WT, int XT, bool QUANT, int C, int B, int NW>
+template <int WT, int XT, bool QUANT, int C, int B, int NW, int RB>
 __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *rows, float *scale,
                                            unsigned char *lds, int pitch, int n, int k0, int kn,
                                            int L) {
   const bool full = kn == 8 * L * C;
+  // Rows of large calls pass the caches by, so that the weights stay there (300000
+  // x 512 -> 512 8-bit 187 us -> 174); fp32 rows, which take two loads to a cache
+  // line, do not (1000513 x 384 -> 128: 358 and 382), nor those of small calls,
+  // where several workgroups read a row (64 x 1024 -> 1024, 64 groups: 16.5, 18.3).
+  constexpr bool ONCE = XT != T_F32 && RB > 1;
   constexpr int SURE = C >= 6 ? C - 2 : C - 1;  // units of a lane that end inside the row
   typedef typename std::conditional<WT == T_I8, u2, u4>::type unit;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -67,8 +72,8 @@ __device__ __forceinline__ void stage_rows(const LinearArgs &a, const int32_t *r
       const elem_t<XT> *row = (const elem_t<XT> *)a.x + (int64_t)rows[r] * a.x_stride + k0;
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        raw[b][c] = c < SURE || full ? load8<XT>(row, 8 * (u0 + L * c))
-                                     : load8_end<XT>(row, 8 * (u0 + L * c), kn);
+        raw[b][c] = c < SURE || full ? load8<XT, ONCE>(row, 8 * (u0 + L * c))
+                                     : load8_end<XT, ONCE>(row, 8 * (u0 + L * c), kn);
     }
 #pragma unroll
     for (int b = 0; b < B; ++b) {
@@ -123,7 +128,7 @@ __device__ __forceinline__ void stage(const LinearArgs &a, const int32_t *rows, 
     constexpr int fit = 64 / (CC * (XT == T_F32 ? 8 : XT == T_I8 ? 2 : 4));
     constexpr int all = RB * 8 / NW;
     constexpr int B = all < fit ? all : fit >= 4 ? 4 : fit >= 2 ? 2 : 1;
-    stage_rows<WT, XT, QUANT, CC, B, NW>(a, rows, scale, lds, pitch, n, k0, kn, L);
+    stage_rows<WT, XT, QUANT, CC, B, NW, RB>(a, rows, scale, lds, pitch, n, k0, kn, L);
   };
   if (C <= 1) {
     go(std::integral_constant<int, 1>());
@@ -283,6 +288,8 @@ __global__ __launch_bounds__(64 * NW, RB > 1 ? 4 : 2) void linear_panel(LinearAr
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[r][v] = 0;
     const i4 *wf = weights_of(nb);
+    const int64_t cw = ((int64_t)t.g * a.NB + min(nb, a.NB - 1)) * 32 + col;
+    const float bias = a.bias[cw], ws = WT == T_I8 ? a.ws[cw] : 1.f;
     for (int ch = 0; ch < nchunk; ++ch) {
       const int n = MULTI ? min(steps, a.S - ch * steps) : a.S;
       const int s0 = first(n), s1 = WK > 1 ? n * (wk + 1) / WK : n;
@@ -349,8 +356,6 @@ __global__ __launch_bounds__(64 * NW, RB > 1 ? 4 : 2) void linear_panel(LinearAr
     }
     if (!live) continue;
     const int ch = nb * 32 + col;
-    const float bias = a.bias[(int64_t)t.g * a.NB * 32 + ch];
-    const float ws = WT == T_I8 ? a.ws[(int64_t)t.g * a.NB * 32 + ch] : 1.f;
 #pragma unroll
     for (int r = 0; r < RB; ++r) {
       const int r0 = r * 32;

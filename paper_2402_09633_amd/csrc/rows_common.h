@@ -47,17 +47,22 @@ struct Raw8 {
   vec v;
 };
 
-// Elements k .. k + 7 of a row.
-template <int T>
+// Elements k .. k + 7 of a row.  ONCE: they are not read again, and need no
+// place in the caches.
+template <int T, bool ONCE = false>
 __device__ __forceinline__ Raw8<T> load8(const elem_t<T> *row, int k) {
+  typedef typename Raw8<T>::vec loose __attribute__((aligned(sizeof(elem_t<T>))));
   Raw8<T> r;
-  __builtin_memcpy(&r.v, row + k, sizeof r.v);
+  if constexpr (ONCE)
+    r.v = __builtin_nontemporal_load((const loose *)(row + k));
+  else
+    r.v = *(const loose *)(row + k);
   return r;
 }
 
 // The same of a row of K, with zeros from K on, which is not read past: from K
 // >= 8 on, the row's last eight elements moved down by as many as lie before k.
-template <int T>
+template <int T, bool ONCE = false>
 __device__ __forceinline__ Raw8<T> load8_end(const elem_t<T> *row, int k, int K) {
   if (K < 8) {  // the same for all lanes
     Raw8<T> r;
@@ -66,7 +71,7 @@ __device__ __forceinline__ Raw8<T> load8_end(const elem_t<T> *row, int k, int K)
     return r;
   }
   const int at = min(k, K - 8), d = min(k - at, 8);
-  Raw8<T> r = load8<T>(row, at);
+  Raw8<T> r = load8<T, ONCE>(row, at);
   if constexpr (T == T_I8) {
     const uint64_t v = __builtin_bit_cast(uint64_t, r.v);
     const uint64_t m = d < 8 ? v >> (8 * d) : 0;

@@ -735,21 +735,22 @@ class Linear(_RowsHandle):
 
     def __init__(self, weights: np.ndarray, dims: gnn_linear_dims):
         self.dims = dims
+        self.widths = (int(dims.in_features), int(dims.out_features), int(dims.n_groups))
         self.handle = gnn_linear_create(weights, dims)
         self.device = torch.device("cuda", torch.cuda.current_device())
 
     def __call__(self, x: torch.Tensor, scales=None, offsets=None, order=None, out=None,
                  out_dtype=None, stream=None) -> torch.Tensor:
-        d, dev = self.dims, self.device
+        (k, n_out, groups), dev = self.widths, self.device
         if stream is not None:
             with _on(dev, stream):
                 return self(x, scales, offsets, order, out, out_dtype)
-        xa, xt, xs = _rows("x", x, d.in_features, None, dev)
+        xa, xt, xs = _rows("x", x, k, None, dev)
         n = x.shape[0]
         sc = _vector("scales", scales, torch.float32, n, dev)
-        off = _vector("offsets", offsets, torch.int32, d.n_groups + 1, dev)
+        off = _vector("offsets", offsets, torch.int32, groups + 1, dev)
         ordr = _vector("order", order, torch.int32, n, dev)
-        out, (ya, yt, ys) = self._out(n, d.out_features, x, out, out_dtype,
+        out, (ya, yt, ys) = self._out(n, n_out, x, out, out_dtype,
                                       off is not None or ordr is not None)
         nb = lib.gnn_linear_workspace(self.handle, xt, n)
         ws = _scratch(nb, dev)
