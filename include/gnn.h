@@ -320,7 +320,7 @@ int gnn_frnn(const float *z, int64_t n_nodes, int32_t dim, float r2, int32_t *ed
  * Tables of rows are device memory: a pointer, an element type and a stride in
  * elements from one row to the next (>= the row's width; the gap between rows
  * is neither read nor written).  Pointers need the alignment of their elements
- * only.  Up to 2^30 rows.  All calls are asynchronous on `stream` and allocate
+ * only.  Up to 2^28 rows.  All calls are asynchronous on `stream` and allocate
  * nothing; scratch is the caller's (device memory aligned to 256 bytes, which
  * the call may overwrite until the stream has passed it; each call in flight
  * needs its own), so calls may overlap and may be captured into graphs.
@@ -334,7 +334,7 @@ int gnn_frnn(const float *z, int64_t n_nodes, int32_t dim, float r2, int32_t *ed
  * zeros; a row with an infinity or a NaN gets scale NaN and zeros, so that its
  * products are NaN and no other row's are touched.  x_type GNN_FP32, GNN_BF16
  * or GNN_F16.  Runs on the current device.  GNN_E_INVALID_ARG for bad counts,
- * types, strides or pointers; GNN_E_UNSUPPORTED above 2^30 rows. */
+ * types, strides or pointers; GNN_E_UNSUPPORTED above 2^28 rows. */
 int gnn_quantize_rows(const void *x, int32_t x_type, int64_t x_stride, int64_t n_rows,
                       int32_t width, int8_t *q, int64_t q_stride, float *scales,
                       hipStream_t stream);

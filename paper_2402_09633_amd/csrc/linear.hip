@@ -685,8 +685,9 @@ hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
     p.RB /= 2;
   if (p.RB == 1) p.NW = WAVES;
   p.tiles = tiles(p.RB);
-  // So few blocks that the CUs are not filled: all waves to each.
-  p.split = p.RB == 1 && p.tiles * a.NB <= 4 * n_cu && a.S >= 2 * WAVES;
+  // So few blocks that the CUs are not filled, or one to a tile: all waves to each
+  // (64 x 4096 -> 4096 8-bit 31 us without, 15 with).
+  p.split = p.RB == 1 && (p.tiles * a.NB <= 4 * n_cu || a.NB == 1) && a.S >= 2 * WAVES;
   const int WN = p.split ? 1 : p.NW;
   const int ntile = (a.NB + WN - 1) / WN;
   a.nsplit = (int)((2 * n_cu + p.tiles - 1) / p.tiles);

@@ -16,7 +16,7 @@ using namespace gnn;
 namespace {
 
 constexpr int MAX_WIDTH = 16384, MAX_HIDDEN = 4096, MAX_GROUPS = 4096;
-constexpr int64_t MAX_ROWS = (int64_t)1 << 30;
+constexpr int64_t MAX_ROWS = (int64_t)1 << 28;
 constexpr int64_t MAX_STRIDE = (int64_t)1 << 31;
 
 int bad(int code, const char *fmt, ...) {
@@ -40,7 +40,7 @@ bool float_type(int t) { return t == GNN_FP32 || t == GNN_BF16 || t == GNN_F16; 
 
 int check_rows(int64_t n_rows) {
   if (n_rows < 0) return bad(GNN_E_INVALID_ARG, "negative row count");
-  if (n_rows > MAX_ROWS) return bad(GNN_E_UNSUPPORTED, "more than 2^30 rows");
+  if (n_rows > MAX_ROWS) return bad(GNN_E_UNSUPPORTED, "more than 2^28 rows");
   return GNN_OK;
 }
 
@@ -377,7 +377,12 @@ MlpScratch mlp_scratch(const gnn_mlp *m, int x_type, int64_t n) {
   s.pre = take((size_t)n * widest * 4);
   s.act = take((size_t)n * widest * (d.dtype == GNN_INT8 ? 1 : 2));
   s.scales = take(d.dtype == GNN_INT8 ? (size_t)n * 4 : 0);
-  s.linear = take(linear_scratch(m->layer[0], x_type, n));
+  size_t linear = 0;  // the layers take turns
+  for (int i = 0; i < d.n_layers; ++i) {
+    const size_t b = linear_scratch(m->layer[i], i == 0 ? x_type : d.dtype, n);
+    if (b > linear) linear = b;
+  }
+  s.linear = take(linear);
   return s;
 }
 

@@ -52,36 +52,39 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L
   for (int u = u0 + L * C; 8 * u < width; u += L) store_q8(q, 8 * u, width, u2{0u, 0u});
 }
 
-// Rows too wide for a wave's registers: one workgroup to a row, which is read
+// Rows too wide for a wave's registers: a workgroup to a row, which is read
 // twice (the second time from the caches).
 template <int XT>
 __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
   __shared__ float part[Q_WAVES];
   const int tid = threadIdx.x;
-  const int64_t r = blockIdx.x;
-  const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
-  uint32_t bits = 0;
-  for (int k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
-    bits = max_bits<XT>(load8_end<XT>(row, k, a.K), bits);
-  float top = top_of<XT>(bits);
-  top = lanes_max(top, 64);
-  if ((tid & 63) == 0) part[tid >> 6] = top;
-  __syncthreads();
-  for (int w = 0; w < Q_WAVES; ++w)
-    top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(part[w])));
-  const Quant z = quant_of<XT>(top);
-  if (tid == 0) a.scales[r] = z.s;
-  int8_t *q = a.q + r * a.q_stride;
   const int width = a.pad ? a.pad : a.K;
-  for (int k = 8 * tid; k < width; k += 8 * 64 * Q_WAVES)
-    store_q8(q, k, width, quantize8<XT>(to_f32<XT>(load8_end<XT>(row, k, a.K)), z));
+  for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x) {
+    const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
+    uint32_t bits = 0;
+    for (int k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
+      bits = max_bits<XT>(load8_end<XT>(row, k, a.K), bits);
+    float top = lanes_max(top_of<XT>(bits), 64);
+    __syncthreads();  // part has been read for the row before
+    if ((tid & 63) == 0) part[tid >> 6] = top;
+    __syncthreads();
+    for (int w = 0; w < Q_WAVES; ++w)
+      top = __uint_as_float(max(__float_as_uint(top), __float_as_uint(part[w])));
+    const Quant z = quant_of<XT>(top);
+    if (tid == 0) a.scales[r] = z.s;
+    int8_t *q = a.q + r * a.q_stride;
+    for (int k = 8 * tid; k < width; k += 8 * 64 * Q_WAVES)
+      store_q8(q, k, width, quantize8<XT>(to_f32<XT>(load8_end<XT>(row, k, a.K)), z));
+  }
 }
 
 template <int XT>
 hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
   const int units = (a.K + 7) / 8;
   const dim3 block(64 * Q_WAVES);
-  if (units > 512) return launch(quantize_wide<XT>, dim3((uint32_t)a.n), block, 0, stream, a);
+  if (units > 512)
+    return launch(quantize_wide<XT>, dim3((uint32_t)(a.n < (1 << 20) ? a.n : 1 << 20)), block, 0,
+                  stream, a);
   int L = 16;
   while (L / 2 >= units) L /= 2;
   while (8 * L < units) L *= 2;

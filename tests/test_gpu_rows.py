@@ -179,6 +179,64 @@ def test_linear_more_tiles_than_cus(G):
             _check(_np(_layer(G, w, b, kind)(x)), _np(x), w[0], b[0], kind, "bf16")
 
 
+# Sizes that the tiles for wide layers take: 128 and 256 rows to a tile, widths
+# that are whole chunks of 16 bytes, and others, whose rows are copied first.
+@pytest.mark.parametrize("kind,xt,m,k,n", [
+    ("bf16", "bf16", 4100, 640, 1100), ("bf16", "bf16", 4100, 643, 1100),
+    ("f16", "f16", 14_001, 520, 1400), ("f16", "f32", 4100, 650, 1030),
+    ("bf16", "f16", 4100, 520, 1027), ("i8", "bf16", 4100, 1000, 1100),
+    ("i8", "f32", 14_001, 901, 1300), ("i8", "i8", 4100, 1040, 1100),
+    ("i8", "i8", 4100, 1101, 1100), ("bf16", "bf16", 2000, 2056, 2100)])
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+def test_linear_tiles(G, kind, xt, m, k, n, out):
+    print(f"tiles {kind} {m}x{k}->{n} x {xt} y {out}", flush=True)
+    w, b = _weights(1, n, k, m + k)
+    layer = _layer(G, w, b, kind)
+    x = _x(m, k, "f32" if xt == "i8" else xt, k, k + 3, 1)
+    scales = None
+    xs = _np(x)
+    if xt == "i8":
+        table = torch.full((m * (k + 3) + 1,), 77, dtype=torch.int8, device="cuda")
+        q = table[1:].view(m, k + 3)[:, :k]
+        x, scales = G.quantize_rows(x, out=(q, torch.empty(m, device="cuda")))
+    table = torch.full((m, n + 5), 7.0, dtype=T[out], device="cuda")
+    y = layer(x, scales=scales, out=table[:, 2:n + 2])
+    _check(_np(y), xs, w[0], b[0], kind, out, f"{xt} {out}")
+    assert (table[:, :2] == 7).all() and (table[:, n + 2:] == 7).all()
+
+
+@pytest.mark.parametrize("kind", ["i8", "bf16", "f16"])
+@pytest.mark.parametrize("m,k,n,g,ordered", [(6000, 1032, 1100, 3, True), (9000, 1001, 1064, 5, False),
+                                             (17_000, 904, 1100, 7, True)])
+def test_grouped_tiles(G, kind, m, k, n, g, ordered):
+    print(f"grouped tiles {kind} {m}x{k}->{n} {g} groups", flush=True)
+    rng = np.random.default_rng(m)
+    sizes = _sizes("ragged", g, m - 50, rng)
+    w, b = _weights(g, n, k, g)
+    x = _x(m, k, "bf16" if kind == "i8" else kind, g)
+    off = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int32) + 20  # 20 rows before, 30 behind
+    order = rng.permutation(m).astype(np.int32) if ordered else np.arange(m, dtype=np.int32)
+    out = torch.full((m, n), 7.0, device="cuda")
+    y = _np(_layer(G, w, b, kind)(x, offsets=torch.as_tensor(off).cuda(),
+                                  order=torch.as_tensor(order).cuda() if ordered else None, out=out))
+    xs = _np(x)
+    for i in range(g):
+        rows = order[off[i]:off[i + 1]][:400]  # enough of each group
+        if len(rows):
+            _check(y[rows], xs[rows], w[i], b[i], kind, "f32", f"group {i}")
+    rest = np.concatenate([order[:off[0]], order[off[-1]:]])
+    assert len(rest) == 50 and (y[rest] == 7.0).all()
+
+
+@pytest.mark.parametrize("m,k", [(3000, 4096), (3000, 2100), (40, 16384)])
+def test_linear_one_block_of_channels(G, m, k):
+    w, b = _weights(1, 20, k, 1)
+    for kind in ("i8", "bf16"):
+        x = _x(m, k, "bf16", 4)
+        _check(_np(_layer(G, w, b, kind)(x, out_dtype=torch.float32)), _np(x), w[0], b[0], kind,
+               "f32")
+
+
 @pytest.mark.parametrize("m,k,n", [(1, 64, 32), (77, 100, 50), (500, 387, 130), (3, 6001, 20),
                                    (2500, 1024, 640)])
 def test_linear_given_8_bit_rows(G, m, k, n):
@@ -509,6 +567,19 @@ def test_grouped_mlp_equals_one_network_per_group(G):
         rows = torch.as_tensor(np.nonzero(ids == j)[0]).cuda()
         assert torch.equal(one(x[rows], out_dtype=torch.float32), y[rows])
     assert (_np(y)[(ids < 0) | (ids >= g)] == 4.0).all()
+
+
+def test_mlp_with_wide_hidden_layers(G):
+    # a hidden layer that the tiles take, with rows that have to be copied first
+    widths, m = [20, 1101, 1100, 4], 4100
+    x = _x(m, 20, "f32", 5)
+    mlp, layers = _mlp(G, widths, 1, "bf16", 3)
+    ref, bound = _mlp_ref(_np(x), layers, 0, "bf16")
+    assert (np.abs(_np(mlp(x)) - ref) <= R.stored(ref, bound, "f32")).all()
+    # sums of 8-bit products are exact: a small call, which the row panels take,
+    # gives the same bits
+    mlp, layers = _mlp(G, widths, 1, "i8", 3)
+    assert torch.equal(mlp(x)[:300], mlp(x[:300]))
 
 
 def test_one_layer_mlp_is_a_linear_layer(G):
