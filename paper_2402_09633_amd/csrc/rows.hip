@@ -230,7 +230,7 @@ hipError_t norm_t(const NormArgs &a, hipStream_t stream) {
 // input's.  Reads the ids twice, writes the order once.
 //
 // How the tiles' counts become places: with few of them (G + 1 times the tiles
-// at most GROUP_DIRECT) every tile sums them itself, a wave to a group; else
+// at most GROUP_DIRECT) every tile sums them itself; else
 // one more launch (group_scan) leaves each tile's place and the groups' totals.
 constexpr int64_t GROUP_DIRECT = 16384;
 
@@ -266,11 +266,6 @@ __device__ __forceinline__ void count_run(const GroupArgs &a, int64_t r0, int bi
     const uint64_t m = same_id(id[s], bits, ok);
     if (ok && (m & lt) == 0) cnt[id[s]] += __popcll(m);
   }
-}
-
-__device__ __forceinline__ int32_t wave_sum(int32_t v) {
-  for (int m = 32; m; m /= 2) v += __shfl_xor(v, m);
-  return v;
 }
 
 // counts[0 .. G][tile]
@@ -330,16 +325,21 @@ __global__ __launch_bounds__(64 * WAVES) void group_place(GroupArgs a, int bits,
       before[g] = a.counts[(int64_t)g * tiles + tile];
     }
   } else if (tiles > 1) {
-    for (int g = wave; g < W; g += WAVES) {
+    // L lanes to a group, up to four tiles to a lane where that is enough
+    int L = 1;
+    while (L < 64 && 4 * L < tiles) L *= 2;
+    for (int g = tid / L; g < W; g += 64 * WAVES / L) {
       int32_t all = 0, prev = 0;
-      for (int t = lane; t < tiles; t += 64) {
+      for (int t = tid % L; t < tiles; t += L) {
         const int32_t c = a.counts[(int64_t)g * tiles + t];
         all += c;
         if (t < tile) prev += c;
       }
-      all = wave_sum(all);
-      prev = wave_sum(prev);
-      if (lane == 0) {
+      for (int m = L / 2; m; m /= 2) {
+        all += __shfl_xor(all, m);
+        prev += __shfl_xor(prev, m);
+      }
+      if (tid % L == 0) {
         total[g] = all;
         before[g] = prev;
       }
