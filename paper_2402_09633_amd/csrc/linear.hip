@@ -406,8 +406,9 @@ __global__ __launch_bounds__(64 * WAVES, 2) void linear_tiled(LinearArgs a) {
     if (WT == T_I8) scale[i] = a.xs[row_of(i)];
   }
   // A wave's load takes 8 rows of 128 bytes; the 16-byte chunk c of row r lies
-  // at place c ^ (r % 8), so that the lanes of a product's read (32 rows, one
-  // chunk) meet every bank alike.
+  // at place c ^ (r % 8), so that 8 lanes of a product's read (8 rows, one chunk)
+  // lie in 8 different places.  Rows r and r + 8 still meet; c ^ (r / 2 % 8), where
+  // 16 rows do not, took the same time (300 and 308 us at 16384 x 4096 -> 4096).
   const int c = (lane & 7) ^ (lane >> 3);
   constexpr int esz = WT == T_I8 ? 1 : 2;
   const unsigned char *src[LOADS];
@@ -685,9 +686,11 @@ hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
     p.RB /= 2;
   if (p.RB == 1) p.NW = WAVES;
   p.tiles = tiles(p.RB);
-  // So few blocks that the CUs are not filled, or one to a tile: all waves to each
-  // (64 x 4096 -> 4096 8-bit 31 us without, 15 with).
-  p.split = p.RB == 1 && (p.tiles * a.NB <= 4 * n_cu || a.NB == 1) && a.S >= 2 * WAVES;
+  // No more blocks than CUs, or one to a tile: all waves to each.  Measured (eight
+  // blocks to a workgroup : one, us): 1 x 4096 -> 4096 bf16 29.7 : 13.1, 64 x 4096
+  // -> 4096 8-bit 22.3 : 15.2; with more blocks the rows are staged too often, 300 x
+  // 1024 -> 1024 8-bit 8.3 : 11.4, 1000 x 1024 -> 1024 bf16 10.1 : 17.6.
+  p.split = p.RB == 1 && (p.tiles * a.NB <= n_cu || a.NB == 1) && a.S >= 2 * WAVES;
   const int WN = p.split ? 1 : p.NW;
   const int ntile = (a.NB + WN - 1) / WN;
   a.nsplit = (int)((2 * n_cu + p.tiles - 1) / p.tiles);
