@@ -10,7 +10,8 @@ namespace {
 // ---- rows to 8 bits ----
 // One pass over the rows: L lanes hold a row (C units of eight elements
 // each), form its largest absolute value and round the values they hold.
-// Bound by memory: x is read and q written once.
+// Bound by memory: x is read and q written once; 1000513 x 128 fp32 110 us, 5.9
+// TB/s.
 constexpr int Q_WAVES = 4;
 
 __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q) {
@@ -227,7 +228,8 @@ hipError_t norm_t(const NormArgs &a, hipStream_t stream) {
 // comes last.  In a tile every wave owns a run of consecutive rows and counters
 // of its own: the lanes of a step that hold the same id are found with one
 // ballot per bit of the id, so there are no atomics and the order is the
-// input's.  Reads the ids twice, writes the order once.
+// input's.  Reads the ids twice, writes the order once; bound by the latency of
+// its launches (2000 rows 6.8 us, 1000513 rows in 16 groups 14.2).
 //
 // How the tiles' counts become places: with few of them (G + 1 times the tiles
 // at most GROUP_DIRECT) every tile sums them itself; else

@@ -121,3 +121,34 @@ def test_plain_quantize_on_ties():
 def test_plain_group():
     off, order = R.group([2, 0, -1, 2, 5, 0], 3)
     assert off.tolist() == [0, 2, 2, 4] and order.tolist() == [1, 5, 0, 3, 2, 4]
+
+
+@pytest.mark.parametrize("bits", [8, 11])
+def test_16_bit_rounding_rule(bits):
+    """The kernels round a 16-bit row to 8 bits by one multiply-add with a factor
+    next to 127 / top, taken on the side that the rounding error of s = fl32(top /
+    127) asks for (and both sides where s has none).  Over all mantissas of the
+    largest value and of the others, and all exponents that do not round to 0, it
+    must give the exact quotient's nearest whole number, ties to even."""
+    lo, hi = 1 << (bits - 1), 1 << bits
+    jx = np.arange(lo, hi, dtype=np.float64)
+    xs = (jx[:, None] / 2.0 ** np.arange(10)).ravel()
+    ties = 0
+    for jm in range(lo, hi):
+        top = np.float32(jm)
+        s = np.float32(top / np.float32(127))
+        d = float(s) * 127 - float(top)  # exact: 24 + 7 bits
+        f = np.float32(np.float32(127) / top)
+        e = float(f) * float(top) - 127.0
+        below = np.nextafter(f, np.float32(0)) if e >= 0 else f
+        above = np.nextafter(f, np.float32(np.inf)) if e <= 0 else f
+        x = xs[xs <= jm]
+        got = np.rint(x * float(below if d >= 0 else above))  # one rounding, as the fma's
+        if d == 0:
+            ties += 1
+            got = np.rint(0.5 * (got + np.rint(x * float(above))))
+        k = np.floor(x / float(s))
+        r = 2 * (x - k * float(s))  # exact
+        want = np.where(r > float(s), k + 1, np.where(r < float(s), k, k + k % 2))
+        assert np.array_equal(got, want), jm
+    assert ties > 0
