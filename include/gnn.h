@@ -356,7 +356,7 @@ int gnn_group_rows(const int32_t *group_ids, int64_t n_rows, int32_t n_groups, i
  *   GNN_INT8:       y[n] = xs ws_g[n] sum_k q(x)[k] q(W_g)[n][k] + b_g[n], rows
  *                   (scale xs) and the weights of each output channel (scale
  *                   ws_g[n]) to 8 bits as by gnn_quantize_rows; the sum in int32
- *                   (exact). */
+ *                   (exact), times ws_g[n], times xs, plus the bias in fp32. */
 typedef struct gnn_linear_dims {
   uint32_t struct_size; /* = sizeof(gnn_linear_dims)                         */
   int32_t in_features;  /* 1..16384                                           */

@@ -14,9 +14,9 @@ namespace gnn {
 namespace {
 
 constexpr int WAVES = 8;
-constexpr int CHUNK = 4096;        // most bytes of a row staged at a time
-constexpr int HALF = 78 * 1024;    // LDS of a tile of more than 32 rows: two fit on a CU
-constexpr int LDS_PAD = 16;  // bytes between staged rows: 16-byte slots of 8 rows differ
+constexpr int CHUNK = 4096;      // most bytes of a row staged at a time
+constexpr int HALF = 78 * 1024;  // LDS of a tile of more than 32 rows: two fit on a CU
+constexpr int LDS_PAD = 16;      // bytes between staged rows: 16-byte slots of 8 rows differ
 
 template <int WT>
 struct Mma {
@@ -225,9 +225,10 @@ __device__ __forceinline__ void finish_block(const LinearArgs &a,
 // One row tile (PM = 32 RB rows of one group) by all waves: the rows are
 // staged once (MULTI: chunk by chunk, where they do not fit), the weights come
 // from the caches in fragment order, RING steps of them in flight.  A wave takes
-// the tile's RB row blocks and one block of 32 channels at a time.  WK waves share the steps of a block (few rows: a call is then bound by how long
-// the weights take, and all waves fetch them); their sums are added in LDS, in
-// the waves' order.
+// the tile's RB row blocks and one block of 32 channels at a time.  WK waves
+// share the steps of a block (few rows: a call is then bound by how long the
+// weights take, and all waves fetch them); their sums are added in LDS, in the
+// waves' order.
 //
 // Bound by HBM: a row is read and an output written once.  1000513 x 384 -> 128
 // 8-bit from fp32 rows 346 us, 5.2 TB/s, the rate of a large copy; 300000 x 512 ->
@@ -304,7 +305,7 @@ __global__ __launch_bounds__(64 * NW, RB > 1 ? 4 : 2) void linear_panel(LinearAr
         const int k0 = ch * (a.chunk / esz);
         __syncthreads();
         stage<WT, XT, false, MAXU, RB, NW>(a, rows, scale, smem, pitch, nrow, k0,
-                                   min(a.K - k0, a.chunk / esz));
+                                           min(a.K - k0, a.chunk / esz));
         __syncthreads();
       }
       if (!live) continue;
@@ -374,7 +375,7 @@ __global__ __launch_bounds__(64 * NW, RB > 1 ? 4 : 2) void linear_panel(LinearAr
 // Where a row does not fit beside its neighbours in LDS, the matrix cores bound
 // the layer, and every byte has to be used often once it is on the CU: tiles of
 // 64 TR rows x 256 channels, eight waves of 32 TR x 64.  The rows (already in
-// the weights' type, whole steps of 32 bytes) go through LDS, 128 bytes of each
+// the weights' type, whole chunks of 16 bytes) go through LDS, 128 bytes of each
 // at a time and two such stages in turn; a wave's weights come from the caches
 // into registers, in fragment order.  While a stage is multiplied, the next one's
 // weights and the rows of the one after it are in flight.  16384 x 4096 -> 4096 in

@@ -307,6 +307,45 @@ def test_rows_in_no_group_keep_their_values(G):
     assert np.array_equal(new[100:400], y[100:400])
 
 
+def test_order_without_groups(G):
+    w, b = _weights(1, 40, 24, 1)
+    for kind in ("bf16", "i8"):
+        x = _x(700, 24, "bf16", 2)
+        order = torch.as_tensor(np.random.default_rng(1).permutation(700).astype(np.int32)).cuda()
+        layer = _layer(G, w, b, kind)
+        assert torch.equal(layer(x, order=order), layer(x))
+        # a row named twice, with the same weights, has its one result; a row
+        # that no position names keeps its value
+        order[5] = order[6]
+        out = torch.full((700, 40), 2.0, device="cuda")
+        y = layer(x, order=order, out=out)
+        named = torch.zeros(700, dtype=torch.bool, device="cuda")
+        named[order.long()] = True
+        assert torch.equal(y[named], layer(x, out_dtype=torch.float32)[named])
+        assert int((~named).sum()) == 1 and (y[~named] == 2).all()
+
+
+def test_one_group_by_its_offsets(G):
+    w, b = _weights(1, 33, 24, 1)
+    layer = _layer(G, w, b, "bf16")
+    x = _x(300, 24, "bf16", 2)
+    off = torch.tensor([37, 205], dtype=torch.int32, device="cuda")
+    y = layer(x, offsets=off, out=torch.full((300, 33), 2.0, device="cuda"))
+    assert (y[:37] == 2).all() and (y[205:] == 2).all()
+    _check(_np(y)[37:205], _np(x)[37:205], w[0], b[0], "bf16", "f32")
+
+
+@pytest.mark.parametrize("kind", ["i8", "bf16"])
+def test_every_row_its_own_group(G, kind):
+    m = 500
+    w, b = _weights(m, 9, 20, 1)
+    x = _x(m, 20, "bf16", 2)
+    off = torch.arange(m + 1, dtype=torch.int32, device="cuda")
+    y = _np(_layer(G, w, b, kind)(x, offsets=off, out_dtype=torch.float32))
+    for i in range(0, m, 7):
+        _check(y[i:i + 1], _np(x)[i:i + 1], w[i], b[i], kind, "f32", f"row {i}")
+
+
 @pytest.mark.parametrize("kind", ["i8", "bf16", "f16"])
 def test_not_finite_rows_stay_alone(G, kind):
     w, b = _weights(1, 70, 50, 1)
@@ -586,6 +625,33 @@ def test_one_layer_mlp_is_a_linear_layer(G):
     mlp, layers = _mlp(G, [50, 30], 1, "i8", 1)
     x = _x(400, 50, "f32", 2)
     assert torch.equal(mlp(x), _layer(G, layers[0][0], layers[0][1], "i8")(x))
+
+
+def test_mlp_refusals(G):
+    mlp, _ = _mlp(G, [6, 16, 4], 3, "bf16", 1)
+    one, _ = _mlp(G, [6, 16, 4], 1, "bf16", 1)
+    x, ids = torch.ones(5, 6, device="cuda"), torch.zeros(5, dtype=torch.int32, device="cuda")
+    with pytest.raises(G.GnnError, match="group_ids"):
+        mlp(x)
+    with pytest.raises(G.GnnError, match="group_ids"):
+        one(x, ids)
+    with pytest.raises(G.GnnError, match="x_type"):
+        one(x.to(torch.int8))
+    with pytest.raises(TypeError):
+        mlp(x, ids[:4])
+    with pytest.raises(TypeError):
+        mlp(x, ids.long())
+    with pytest.raises(ValueError):
+        mlp(torch.ones(5, 7, device="cuda"), ids)
+    assert one(x[:0]).shape == (0, 4) and mlp(x[:0], ids[:0]).shape == (0, 4)
+    need = G.gnn_mlp_workspace(mlp.handle, G.GNN_FP32, 5)
+    ws, y = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.full((5, 4), 9.0, device="cuda")
+    with pytest.raises(G.GnnError, match="workspace"):
+        G.gnn_mlp_apply(mlp.handle, x, G.GNN_FP32, 6, ids, 5, y, G.GNN_FP32, 4, ws, need - 1)
+    torch.cuda.synchronize()
+    assert (y == 9).all()
+    G.gnn_mlp_apply(mlp.handle, x, G.GNN_FP32, 6, ids, 5, y, G.GNN_FP32, 4, ws, need)
+    assert torch.equal(y, mlp(x, ids))
 
 
 def test_wide_embedding_feeds_the_radius_search(G):
