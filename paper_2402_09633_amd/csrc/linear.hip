@@ -222,8 +222,16 @@ __device__ __forceinline__ void finish_block(const LinearArgs &a,
     store(std::integral_constant<int, T_F16>());
 }
 
+// How rows are staged: whole; in chunks, where they do not fit; or whole and
+// narrow, 32 to a tile, in few enough registers for three workgroups to a CU
+// (20011 x 391 -> 259 8-bit 18.7 us without, 15.8 with; rows past narrow_bytes
+// lose by it, 3000 x 1024 -> 1024 13.3 and 18.4; fp32 rows to 8 bits take the
+// registers of two).
+enum { WHOLE, CHUNKS, NARROW };
+constexpr int narrow_bytes(int w_type) { return w_type == T_I8 ? 768 : 1024; }
+
 // One row tile (PM = 32 RB rows of one group) by all waves: the rows are
-// staged once (MULTI: chunk by chunk, where they do not fit), the weights come
+// staged once (CHUNKS: piece by piece), the weights come
 // from the caches in fragment order, RING steps of them in flight.  A wave takes
 // the tile's RB row blocks and one block of 32 channels at a time.  WK waves
 // share the steps of a block (few rows: a call is then bound by how long the
@@ -234,14 +242,21 @@ __device__ __forceinline__ void finish_block(const LinearArgs &a,
 // 8-bit from fp32 rows 346 us, 5.2 TB/s, the rate of a large copy; 300000 x 512 ->
 // 512 8-bit from bf16 165 us, 3.7 TB/s, the products' 33 us of matrix time and the
 // weights' way from L2 (256 KB to a tile) not all covered.
-template <int WT, int XT, int RB, int WK, int NW, bool MULTI>
-__global__ __launch_bounds__(64 * NW, RB > 1 ? 4 : 2) void linear_panel(LinearArgs a) {
-  constexpr int PM = 32 * RB, RING = RB == 1 ? 8 : 4;
+template <int WT, int XT, int RB, int WK, int NW, int MODE>
+__global__ __launch_bounds__(64 * NW, RB > 1           ? 4
+                                     : MODE != NARROW ? 2
+                                     : WT == T_I8 && XT == T_F32 ? 4 : 6) void linear_panel(
+    LinearArgs a) {
+  constexpr bool MULTI = MODE == CHUNKS;
+  constexpr int PM = 32 * RB, RING = RB == 1 && MODE != NARROW ? 8 : 4;
   constexpr int WN = NW / WK;  // channel blocks at a time
   static_assert(WK == 1 || (RB == 1 && WK == NW), "one block to a workgroup");
   typedef typename Mma<WT>::acc acc_t;
   constexpr bool QUANT = WT == T_I8 && XT != T_I8;
-  constexpr int MAXU = (RB > 1 ? HALF / PM - LDS_PAD : CHUNK) / (WT == T_I8 ? 8 : 16);
+  constexpr int MAXU = (RB > 1           ? HALF / PM - LDS_PAD
+                        : MODE == NARROW ? narrow_bytes(WT)
+                                         : CHUNK) /
+                       (WT == T_I8 ? 8 : 16);
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ int32_t rows[PM];
   __shared__ int64_t row_at[PM];  // where a row lies in y
@@ -575,11 +590,11 @@ struct Plan {
   int64_t tiles;
 };
 
-template <int WT, int XT, int RB, int WK, int NW, bool MULTI>
+template <int WT, int XT, int RB, int WK, int NW, int MODE>
 hipError_t panel(const LinearArgs &a, const Plan &p, hipStream_t stream) {
   size_t lds = (size_t)32 * RB * (a.chunk + LDS_PAD);
   if (WK > 1 && lds < 4096 * NW) lds = 4096 * NW;
-  return launch_lds(linear_panel<WT, XT, RB, WK, NW, MULTI>,
+  return launch_lds(linear_panel<WT, XT, RB, WK, NW, MODE>,
                     dim3((uint32_t)(p.tiles * a.nsplit)), dim3(64 * NW), lds, stream, a);
 }
 
@@ -587,21 +602,22 @@ template <int WT, int XT>
 hipError_t panel_rows(const LinearArgs &a, const Plan &p, hipStream_t stream) {
   if (p.multi) {
     if constexpr (WT != T_I8 || XT == T_I8) {
-      if (p.split) return panel<WT, XT, 1, 8, 8, true>(a, p, stream);
-      return panel<WT, XT, 1, 1, 8, true>(a, p, stream);
+      if (p.split) return panel<WT, XT, 1, 8, 8, CHUNKS>(a, p, stream);
+      return panel<WT, XT, 1, 1, 8, CHUNKS>(a, p, stream);
     }
     return hipErrorInvalidValue;  // such rows are rounded beforehand
   }
   if (p.RB == 4) {
-    if (p.NW == 8) return panel<WT, XT, 4, 1, 8, false>(a, p, stream);
-    return panel<WT, XT, 4, 1, 4, false>(a, p, stream);
+    if (p.NW == 8) return panel<WT, XT, 4, 1, 8, WHOLE>(a, p, stream);
+    return panel<WT, XT, 4, 1, 4, WHOLE>(a, p, stream);
   }
   if (p.RB == 2) {
-    if (p.NW == 8) return panel<WT, XT, 2, 1, 8, false>(a, p, stream);
-    return panel<WT, XT, 2, 1, 4, false>(a, p, stream);
+    if (p.NW == 8) return panel<WT, XT, 2, 1, 8, WHOLE>(a, p, stream);
+    return panel<WT, XT, 2, 1, 4, WHOLE>(a, p, stream);
   }
-  if (p.split) return panel<WT, XT, 1, 8, 8, false>(a, p, stream);
-  return panel<WT, XT, 1, 1, 8, false>(a, p, stream);
+  if (p.split) return panel<WT, XT, 1, 8, 8, WHOLE>(a, p, stream);
+  if (a.S * 32 <= narrow_bytes(WT)) return panel<WT, XT, 1, 1, 8, NARROW>(a, p, stream);
+  return panel<WT, XT, 1, 1, 8, WHOLE>(a, p, stream);
 }
 
 template <int WT>
