@@ -703,7 +703,14 @@ hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
   };
   p.NW = a.NB <= 4 ? 4 : WAVES;
   const int room = p.NW == WAVES ? HALF : HALF / 2;
-  p.RB = p.multi ? 1 : 4;
+  // Output rows that do not start on 64 bytes share cache sectors between two
+  // blocks' stores, which have to meet in L2: long ones do better with 64 rows to a
+  // tile, whose output stays there (bf16 184899 x 64 -> 1537 244 : 198 us, fp32 out
+  // -> 769 210 : 166, 100000 x 256 -> 1000 8-bit 84 : 79; short ones and whole
+  // sectors lose by it, -> 513 71 : 73, -> 1536 138 : 144).
+  const int64_t ysz = type_bytes(a.y_type);
+  const bool torn = ((uintptr_t)a.y % 64 || a.y_stride * ysz % 64) && a.N * ysz > 1536;
+  p.RB = p.multi ? 1 : torn ? 2 : 4;
   while (p.RB > 1 && (32 * p.RB * (a.chunk + LDS_PAD) > (p.RB == 4 ? room : HALF) ||
                       a.n / (32 * p.RB) < 2 * n_cu))
     p.RB /= 2;
