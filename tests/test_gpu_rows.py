@@ -90,7 +90,8 @@ def test_quantize_random_bits(G):
 
 @pytest.mark.parametrize("n,g", [(1, 1), (2, 5), (63, 2), (64, 3), (65, 64), (4095, 7), (4096, 4),
                                  (4097, 4), (10_000, 300), (70_001, 1), (50_003, 4096),
-                                 (300_000, 16), (3_000_001, 5)])
+                                 (300_000, 16), (3_000_001, 5), (3000, 2000), (4096, 900),
+                                 (8192, 899), (8193, 899), (2048, 3), (2049, 3), (1_200_000, 60)])
 def test_group(G, n, g):
     print(f"group {n} rows {g} groups", flush=True)
     rng = np.random.default_rng(n + g)
