@@ -1,0 +1,83 @@
+"""Row operators on the GPU at the ends of their ranges: the smallest scales, the
+widest rows and the most rows."""
+import numpy as np
+import pytest
+import torch
+
+from tests import rows_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2402_09633_amd import gnn
+    return gnn
+
+
+def _next_to_halves(scale_bits, seed):
+    """fp32 rows whose scales have the given binade (bits of the scale's exponent
+    field), and whose values are the numbers to both sides of every half step:
+    the quotients are as near to a half as they can be."""
+    rng = np.random.default_rng(seed)
+    m = rng.integers(1 << 23, 1 << 24, size=64, dtype=np.int64)
+    m[:4] = [1 << 23, (1 << 23) + 1, (1 << 24) - 1, (1 << 24) - 2]
+    unit = 2.0 ** (scale_bits - 150)  # an ulp of the scales
+    tops = (127.0 * m * unit).astype(np.float32)
+    s = (tops.astype(np.float64) / 127.0).astype(np.float32).astype(np.float64)
+    h = np.concatenate([np.arange(0.5, 126.5), -np.arange(0.5, 126.5)])
+    at = (h[None, :] * s[:, None]).astype(np.float32)
+    x = np.concatenate([tops[:, None], at, np.nextafter(at, np.float32(np.inf)),
+                        np.nextafter(at, np.float32(-np.inf))], axis=1).astype(np.float32)
+    return x
+
+
+@pytest.mark.parametrize("scale_bits", [1, 2, 3, 24, 25, 126, 127, 128, 200, 246, 247])
+def test_quotients_next_to_a_half(G, scale_bits):
+    # at scale_bits 1 (scales from 2^-126 to 2^-125) half an ulp of the scale is
+    # below the smallest fp32 number
+    x = _next_to_halves(scale_bits, scale_bits)
+    assert np.isfinite(x).all()
+    qr, sr = R.quantize(x)
+    assert (sr > 0).all()
+    q, s = G.quantize_rows(torch.as_tensor(x).cuda())
+    assert np.array_equal(s.cpu().numpy(), sr)
+    wrong = np.argwhere(q.cpu().numpy() != qr)
+    assert len(wrong) == 0, f"{len(wrong)} of {x.size}, the first at {wrong[:1]}"
+
+
+def test_layers_round_the_smallest_rows_and_weights_alike(G):
+    # rows rounded while they are staged, and the weights' own rounding
+    x = _next_to_halves(1, 5)
+    k = x.shape[1]
+    w = _next_to_halves(1, 6)[:40]
+    unit = np.eye(k, dtype=np.float32)[:200]  # rows that pick single columns: q = 127, scale 1 / 127
+    layer = G.Linear(np.concatenate([w.ravel(), np.zeros(len(w), np.float32)]),
+                     G.make_linear_dims(k, len(w), 1, G.GNN_INT8))
+    wq, ws = R.quantize(w)
+    us = np.float32(1.0 / 127.0)
+    want = (wq.T[:200].astype(np.float32) * 127 * ws[None, :]) * us
+    got = layer(torch.as_tensor(unit).cuda()).cpu().numpy()
+    # products of small numbers, the last of which may round to a subnormal one
+    assert (np.abs(got - want) <= 2.0 ** -149 + 2.0 ** -23 * np.abs(want)).all()
+    ones = np.zeros((64, k), np.float32)
+    ones[:, :64] = np.eye(64)
+    pick = G.Linear(np.concatenate([ones.ravel(), np.zeros(64, np.float32)]),
+                    G.make_linear_dims(k, 64, 1, G.GNN_INT8))
+    xq, xs = R.quantize(x)
+    want = (xq[:, :64].astype(np.float32) * 127 * us) * xs[:, None]
+    got = pick(torch.as_tensor(x).cuda()).cpu().numpy()
+    assert (np.abs(got - want) <= 2.0 ** -149 + 2.0 ** -23 * np.abs(want)).all()
+
+
+def test_smallest_scales_of_16_bit_rows(G):
+    # bf16 rows with scales around 2^-126, below which a row counts as zero
+    rng = np.random.default_rng(2)
+    tops = torch.as_tensor(np.ldexp(rng.uniform(0.9, 2.2, 300), -119).astype(np.float32))
+    x = torch.as_tensor(rng.uniform(-1, 1, (300, 200)).astype(np.float32)) * tops[:, None]
+    x[:, 0] = tops
+    x = x.to(torch.bfloat16)
+    qr, sr = R.quantize(x.float().numpy())
+    assert (sr == 0).any() and (sr > 0).any()
+    q, s = G.quantize_rows(x.cuda())
+    assert np.array_equal(s.cpu().numpy(), sr) and np.array_equal(q.cpu().numpy(), qr)
