@@ -15,12 +15,12 @@ namespace {
 constexpr int Q_WAVES = 4;
 
 __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q) {
-  if (k + 8 <= K) {
+  if (k <= K - 8) {
     __builtin_memcpy(row + k, &q, 8);
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      if (k + j < K) row[k + j] = (int8_t)(q[j / 4] >> (8 * (j % 4)));
+      if (j < K - k) row[k + j] = (int8_t)(q[j / 4] >> (8 * (j % 4)));
   }
 }
 
@@ -54,7 +54,8 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L
 }
 
 // Rows too wide for a wave's registers: a workgroup to a row, which is read
-// twice (the second time from the caches).
+// twice (the second time from the caches).  The step past the end of the widest
+// rows (to 2^31 - 1) is no 32-bit number.
 template <int XT>
 __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
   __shared__ float part[Q_WAVES];
@@ -63,8 +64,8 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
   for (int64_t r = blockIdx.x; r < a.n; r += gridDim.x) {
     const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
     uint32_t bits = 0;
-    for (int k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
-      bits = max_bits<XT>(load8_end<XT>(row, k, a.K), bits);
+    for (int64_t k = 8 * tid; k < a.K; k += 8 * 64 * Q_WAVES)
+      bits = max_bits<XT>(load8_end<XT>(row, (int)k, a.K), bits);
     float top = lanes_max(top_of<XT>(bits), 64);
     __syncthreads();  // part has been read for the row before
     if ((tid & 63) == 0) part[tid >> 6] = top;
@@ -74,14 +75,14 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_wide(QuantArgs a) {
     const Quant z = quant_of<XT>(top);
     if (tid == 0) a.scales[r] = z.s;
     int8_t *q = a.q + r * a.q_stride;
-    for (int k = 8 * tid; k < width; k += 8 * 64 * Q_WAVES)
-      store_q8(q, k, width, quantize8<XT>(to_f32<XT>(load8_end<XT>(row, k, a.K)), z));
+    for (int64_t k = 8 * tid; k < width; k += 8 * 64 * Q_WAVES)
+      store_q8(q, (int)k, width, quantize8<XT>(to_f32<XT>(load8_end<XT>(row, (int)k, a.K)), z));
   }
 }
 
 template <int XT>
 hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
-  const int units = (a.K + 7) / 8;
+  const int units = (int)(((int64_t)a.K + 7) / 8);
   const dim3 block(64 * Q_WAVES);
   if (units > 512)
     return launch(quantize_wide<XT>, dim3((uint32_t)(a.n < (1 << 20) ? a.n : 1 << 20)), block, 0,

@@ -81,3 +81,30 @@ def test_smallest_scales_of_16_bit_rows(G):
     assert (sr == 0).any() and (sr > 0).any()
     q, s = G.quantize_rows(x.cuda())
     assert np.array_equal(s.cpu().numpy(), sr) and np.array_equal(q.cpu().numpy(), qr)
+
+
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("width", [(1 << 31) - 1, (1 << 31) - 2044])
+def test_widest_row(G, kind, width):
+    """A row of as many elements as a width can count: the step past its end is
+    beyond 2^31."""
+    print(f"widest row {width} {kind}", flush=True)
+    x = torch.empty(width, dtype=kind, device="cuda")
+    part = 1 << 27
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    top = 0.0
+    for i in range(0, width, part):
+        n = min(part, width - i)
+        x[i:i + n] = torch.randn(n, device="cuda", generator=gen)
+        top = max(top, float(x[i:i + n].float().abs().max()))
+    x[-1] = 3 * top
+    out = torch.full((width + 8,), 99, dtype=torch.int8, device="cuda")
+    s = torch.empty(1, device="cuda")
+    G.quantize_rows(x.view(1, width), out=(out[:width].view(1, width), s))
+    want = np.float32(float(x[-1].float()) / 127.0)
+    assert s.item() == float(want)
+    assert (out[width:] == 99).all() and out[width - 1] == 127
+    for i in range(0, width, part):
+        n = min(part, width - i)
+        q = torch.round(x[i:i + n].double() / float(want)).to(torch.int8)
+        assert torch.equal(out[i:i + n], q), i
