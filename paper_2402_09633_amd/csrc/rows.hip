@@ -13,6 +13,7 @@ namespace {
 // Bound by memory: x is read and q written once; 1000513 x 128 fp32 110 us, 5.9
 // TB/s.
 constexpr int Q_WAVES = 4;
+constexpr int Q_GRID = 1 << 20;  // most workgroups of a launch
 
 __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q) {
   if (k <= K - 8) {
@@ -25,11 +26,7 @@ __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q)
 }
 
 template <int XT, int C, bool FULL>
-__global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = 64 / L, sub = lane / L, u0 = lane % L;
-  const int64_t r = ((int64_t)blockIdx.x * Q_WAVES + wave) * per + sub;
-  if (r >= a.n) return;
+__device__ __forceinline__ void quantize_row(const QuantArgs &a, int64_t r, int u0, int L) {
   const int width = a.pad ? a.pad : a.K;
   const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
   Raw8<XT> raw[C];
@@ -51,6 +48,15 @@ __global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L
       store_q8(q, 8 * (u0 + L * c), width, v);
   }
   for (int u = u0 + L * C; 8 * u < width; u += L) store_q8(q, 8 * u, width, u2{0u, 0u});
+}
+
+template <int XT, int C, bool FULL>
+__global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = 64 / L, sub = lane / L, u0 = lane % L;
+  const int64_t step = (int64_t)gridDim.x * Q_WAVES * per;
+  for (int64_t r = ((int64_t)blockIdx.x * Q_WAVES + wave) * per + sub; r < a.n; r += step)
+    quantize_row<XT, C, FULL>(a, r, u0, L);
 }
 
 // Rows too wide for a wave's registers: a workgroup to a row, which is read
@@ -85,14 +91,16 @@ hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
   const int units = (int)(((int64_t)a.K + 7) / 8);
   const dim3 block(64 * Q_WAVES);
   if (units > 512)
-    return launch(quantize_wide<XT>, dim3((uint32_t)(a.n < (1 << 20) ? a.n : 1 << 20)), block, 0,
+    return launch(quantize_wide<XT>, dim3((uint32_t)(a.n < Q_GRID ? a.n : Q_GRID)), block, 0,
                   stream, a);
   int L = 16;
   while (L / 2 >= units) L /= 2;
   while (8 * L < units) L *= 2;
   const int C = (units + L - 1) / L;
   const int64_t rows = (int64_t)Q_WAVES * (64 / L);
-  const dim3 grid((uint32_t)((a.n + rows - 1) / rows));
+  // a launch takes fewer than 2^32 threads: 2^28 rows of 16 to a workgroup go round
+  const int64_t wgs = (a.n + rows - 1) / rows;
+  const dim3 grid((uint32_t)(wgs < Q_GRID ? wgs : Q_GRID));
   auto go = [&](auto n) {
     constexpr int CC = decltype(n)::value;
     if (a.K == 8 * CC * L) return launch(quantize_rows<XT, CC, true>, grid, block, 0, stream, a, L);

@@ -108,3 +108,30 @@ def test_widest_row(G, kind, width):
         n = min(part, width - i)
         q = torch.round(x[i:i + n].double() / float(want)).to(torch.int8)
         assert torch.equal(out[i:i + n], q), i
+
+
+@pytest.mark.parametrize("width,short", [(65, 0), (70, 15)])
+def test_most_rows(G, width, short):
+    """As many rows as a call takes, of a width at which a workgroup of 256 threads
+    holds 16 rows: a workgroup for every 16 would be 2^32 threads in one launch."""
+    n = (1 << 28) - short
+    print(f"most rows {n} x {width}", flush=True)
+    x = torch.empty(n, width, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    part = 1 << 23
+    base = torch.randn(part, width, device="cuda", generator=gen).to(torch.bfloat16)
+    for i in range(0, n, part):  # the same rows a few places on, and of another size
+        m = min(part, n - i)
+        x[i:i + m] = torch.roll(base, i // part, 0)[:m] * (1.0 + i // part)
+    q, s = G.quantize_rows(x)
+    for i in range(0, n, part):
+        xd = x[i:i + part].double()
+        want = (xd.abs().amax(1) / 127.0).float()
+        assert torch.equal(s[i:i + part], want), i
+        assert torch.equal(q[i:i + part], torch.round(xd / want.double()[:, None]).to(torch.int8)), i
+
+
+def test_more_rows_than_are_taken_are_refused(G):
+    x = torch.zeros((1 << 28) + 1, 1, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(G.GnnError, match="rows"):
+        G.quantize_rows(x)
