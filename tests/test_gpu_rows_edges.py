@@ -135,3 +135,67 @@ def test_more_rows_than_are_taken_are_refused(G):
     x = torch.zeros((1 << 28) + 1, 1, dtype=torch.bfloat16, device="cuda")
     with pytest.raises(G.GnnError, match="rows"):
         G.quantize_rows(x)
+
+
+def test_most_rows_in_group_order(G):
+    n, g = 1 << 28, 5
+    print(f"most rows grouped {n}", flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    ids = torch.randint(-1, g + 1, (n,), device="cuda", generator=gen, dtype=torch.int32)
+    off, order = G.group_rows(ids, g)
+    start = 0
+    for j in [*range(g), None]:
+        mine = (ids == j) if j is not None else (ids < 0) | (ids >= g)
+        rows = torch.nonzero(mine).flatten().to(torch.int32)  # ascending
+        assert off[0 if j == 0 else (g if j is None else j)].item() == start
+        assert torch.equal(order[start:start + rows.numel()], rows), j
+        start += rows.numel()
+    assert start == n
+
+
+@pytest.mark.parametrize("kind", ["GNN_BF16", "GNN_INT8"])
+def test_most_rows_through_a_layer(G, kind):
+    n, k, width = 1 << 28, 9, 7
+    print(f"most rows through a layer {n} {kind}", flush=True)
+    rng = np.random.default_rng(1)
+    w = rng.normal(size=(2, width, k)).astype(np.float32)
+    b = rng.normal(size=(2, width)).astype(np.float32)
+    layer = G.Linear(np.concatenate([w.reshape(2, -1), b], 1).ravel(),
+                     G.make_linear_dims(k, width, 2, getattr(G, kind)))
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(n, k, dtype=torch.bfloat16, device="cuda")
+    part = 1 << 25
+    for i in range(0, n, part):
+        x[i:i + part] = torch.randn(part, k, device="cuda", generator=gen)
+    cut = n - 77
+    off = torch.tensor([3, cut, n - 2], dtype=torch.int32, device="cuda")
+    y = layer(x, offsets=off, out=torch.full((n, width), 5.0, dtype=torch.bfloat16, device="cuda"))
+    assert (y[:3] == 5).all() and (y[n - 2:] == 5).all()
+    # the same rows in small calls: 8-bit sums are exact, and so few 16-bit
+    # products are summed in one step
+    for g, lo, hi in ((0, 3, 5000), (0, (1 << 27) - 3000, (1 << 27) + 3000),
+                      (0, cut - 5000, cut), (1, cut, n - 2)):
+        few = torch.tensor([0, hi - lo, hi - lo] if g == 0 else [0, 0, hi - lo],
+                           dtype=torch.int32, device="cuda")
+        assert torch.equal(y[lo:hi], layer(x[lo:hi], offsets=few)), (g, lo)
+        ref, bound = R.linear(x[lo:hi].float().cpu().numpy(),
+                              w[g] if kind == "GNN_INT8" else
+                              torch.as_tensor(w[g]).to(torch.bfloat16).float().numpy(),
+                              b[g], "i8" if kind == "GNN_INT8" else "bf16")
+        err = np.abs(y[lo:hi].double().cpu().numpy() - ref)
+        assert (err <= R.stored(ref, bound, "bf16")).all()
+
+
+def test_most_rows_through_a_network(G):
+    n, widths = 1 << 28, [4, 8, 3]
+    print(f"most rows through a network {n}", flush=True)
+    rng = np.random.default_rng(1)
+    dims = G.make_mlp_dims(widths, 2, G.GNN_INT8)
+    mlp = G.Mlp(rng.normal(size=G.gnn_mlp_weight_count(dims)).astype(np.float32), dims)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(n, widths[0], device="cuda", generator=gen)
+    ids = torch.randint(-1, 2, (n,), device="cuda", generator=gen, dtype=torch.int32)
+    y = mlp(x, ids)
+    for lo, hi in ((0, 5000), ((1 << 27) - 3000, (1 << 27) + 3000), (n - 5000, n)):
+        assert torch.equal(y[lo:hi], mlp(x[lo:hi], ids[lo:hi])), lo
+        assert (y[lo:hi][ids[lo:hi] < 0] == 0).all() and y[lo:hi].isfinite().all()
