@@ -9,6 +9,7 @@ module raises.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 
 import numpy as np
@@ -80,6 +81,17 @@ def make_filter_dims(in_features=3, hidden=64, ln_eps=1e-5) -> gnn_filter_dims:
     return gnn_filter_dims(ctypes.sizeof(gnn_filter_dims), in_features, hidden, ln_eps)
 
 
+_INT32_MAX = 2 ** 31 - 1
+
+
+def _int32(what: str, v) -> int:
+    """A whole number of 32 bits: ctypes would pass the low bits of a larger one."""
+    v = operator.index(v)
+    if not -_INT32_MAX <= v <= _INT32_MAX:
+        raise ValueError(f"{what}: {v} is not a 32-bit number")
+    return v
+
+
 class gnn_linear_dims(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("in_features", ctypes.c_int32),
                 ("out_features", ctypes.c_int32), ("n_groups", ctypes.c_int32),
@@ -87,7 +99,8 @@ class gnn_linear_dims(ctypes.Structure):
 
 
 def make_linear_dims(in_features, out_features, n_groups=1, dtype=GNN_BF16) -> gnn_linear_dims:
-    return gnn_linear_dims(ctypes.sizeof(gnn_linear_dims), in_features, out_features, n_groups,
+    return gnn_linear_dims(ctypes.sizeof(gnn_linear_dims), _int32("in_features", in_features),
+                           _int32("out_features", out_features), _int32("n_groups", n_groups),
                            dtype)
 
 
@@ -102,8 +115,9 @@ def make_mlp_dims(widths, n_groups=1, dtype=GNN_BF16, ln_eps=1e-5) -> gnn_mlp_di
     """widths: of the input, the hidden layers and the output."""
     if not 2 <= len(widths) <= GNN_MLP_MAX_LAYERS + 1:
         raise ValueError(f"2..{GNN_MLP_MAX_LAYERS + 1} widths, got {len(widths)}")
-    w = (ctypes.c_int32 * (GNN_MLP_MAX_LAYERS + 1))(*widths)
-    return gnn_mlp_dims(ctypes.sizeof(gnn_mlp_dims), len(widths) - 1, w, n_groups, dtype, ln_eps)
+    w = (ctypes.c_int32 * (GNN_MLP_MAX_LAYERS + 1))(*[_int32("width", v) for v in widths])
+    return gnn_mlp_dims(ctypes.sizeof(gnn_mlp_dims), len(widths) - 1, w,
+                        _int32("n_groups", n_groups), dtype, ln_eps)
 
 
 class gnn_profile_stats(ctypes.Structure):
@@ -541,6 +555,8 @@ def _rows(what: str, t: torch.Tensor, width=None, n=None, device=None):
         raise ValueError(f"{what}: rows of {cols}, expected {width}")
     if n is not None and rows != n:
         raise ValueError(f"{what}: {rows} rows, expected {n}")
+    if cols > _INT32_MAX:  # the call's width has 32 bits
+        raise ValueError(f"{what}: rows of {cols}, at most {_INT32_MAX} are supported")
     if step != 1 and cols > 1:
         raise ValueError(f"{what}: the elements of a row must be contiguous")
     if stride < cols:
@@ -574,6 +590,7 @@ def _device(what: str, t) -> torch.device:
 def gnn_quantize_rows(x, x_type: int, x_stride: int, n_rows: int, width: int, q, q_stride: int,
                       scales, stream=None) -> int:
     """As the C call; addresses or contiguous tensors."""
+    _int32("width", width)
     return _check(lib.gnn_quantize_rows(_addr(x), x_type, x_stride, n_rows, width, _addr(q),
                                         q_stride, _addr(scales), _stream(stream)))
 
@@ -604,12 +621,13 @@ def quantize_rows(x: torch.Tensor, out=None, stream=None):
 
 
 def gnn_group_workspace(n_rows: int, n_groups: int) -> int:
-    return int(lib.gnn_group_workspace(n_rows, n_groups))
+    return int(lib.gnn_group_workspace(n_rows, _int32("n_groups", n_groups)))
 
 
 def gnn_group_rows(group_ids, n_rows: int, n_groups: int, offsets, order, workspace=None,
                    workspace_bytes: int = 0, stream=None) -> int:
     """As the C call; addresses or contiguous tensors."""
+    _int32("n_groups", n_groups)
     return _check(lib.gnn_group_rows(_addr(group_ids), n_rows, n_groups, _addr(offsets),
                                      _addr(order), _addr(workspace), workspace_bytes,
                                      _stream(stream)))
