@@ -785,19 +785,21 @@ class Mlp(_RowsHandle):
 
     def __init__(self, weights: np.ndarray, dims: gnn_mlp_dims):
         self.dims = dims
+        # the network's own: the caller may use dims for the next one
+        self.widths = tuple(dims.widths[:dims.n_layers + 1])
         self.handle = gnn_mlp_create(weights, dims)
         self.device = torch.device("cuda", torch.cuda.current_device())
 
     def __call__(self, x: torch.Tensor, group_ids=None, out=None, out_dtype=None,
                  stream=None) -> torch.Tensor:
-        d, dev = self.dims, self.device
+        dev = self.device
         if stream is not None:
             with _on(dev, stream):
                 return self(x, group_ids, out, out_dtype)
-        xa, xt, xs = _rows("x", x, d.widths[0], None, dev)
+        xa, xt, xs = _rows("x", x, self.widths[0], None, dev)
         n = x.shape[0]
         ids = _vector("group_ids", group_ids, torch.int32, n, dev)
-        out, (ya, yt, ys) = self._out(n, d.widths[d.n_layers], x, out, out_dtype, ids is not None)
+        out, (ya, yt, ys) = self._out(n, self.widths[-1], x, out, out_dtype, ids is not None)
         nb = lib.gnn_mlp_workspace(self.handle, xt, n)
         ws = _scratch(nb, dev)
         _check(lib.gnn_mlp_apply(self.handle, xa, xt, xs, ids, n, ya, yt, ys, _addr(ws), nb,
