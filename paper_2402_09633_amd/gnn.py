@@ -537,6 +537,8 @@ def _on(device, stream):
     `device`."""
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(stream), device=device)
+    if stream.device != device:
+        raise ValueError(f"stream: expected one of {device}, got one of {stream.device}")
     return torch.cuda.stream(stream)
 
 

@@ -23,3 +23,42 @@ def test_dims_of_one_network_reused_for_the_next(G):
     second = G.Mlp(rng.normal(size=G.gnn_mlp_weight_count(dims)).astype(np.float32), dims)
     assert torch.equal(first(x), y)
     assert second(x[:, :5]).shape == (50, 2)
+
+
+def _all_calls(G):
+    """Every call with a stream argument, as a function of the stream alone."""
+    rng = np.random.default_rng(1)
+    x = torch.as_tensor(rng.normal(size=(300, 6)).astype(np.float32)).cuda()
+    ids = torch.as_tensor(rng.integers(0, 3, 300).astype(np.int32)).cuda()
+    ld, md = G.make_linear_dims(6, 4, 3), G.make_mlp_dims([6, 16, 4], 3, G.GNN_INT8)
+    layer = G.Linear(rng.normal(size=G.gnn_linear_weight_count(ld)).astype(np.float32), ld)
+    mlp = G.Mlp(rng.normal(size=G.gnn_mlp_weight_count(md)).astype(np.float32), md)
+    off, order = G.group_rows(ids, 3)
+    torch.cuda.synchronize()
+    return [lambda s: G.quantize_rows(x, stream=s), lambda s: G.group_rows(ids, 3, stream=s),
+            lambda s: (layer(x, offsets=off, order=order, stream=s),),
+            lambda s: (mlp(x, ids, stream=s),)]
+
+
+def test_streams_of_other_devices_are_refused(G):
+    here = torch.cuda.Stream()
+
+    class Elsewhere(torch.cuda.Stream):
+        device = torch.device("cuda", 1 + torch.cuda.current_device())
+
+    for call in _all_calls(G):
+        with pytest.raises(ValueError, match="stream"):
+            call(Elsewhere())
+        call(here)
+    torch.cuda.synchronize()
+
+
+def test_streams_by_handle(G):
+    side = torch.cuda.Stream()
+    for call in _all_calls(G):
+        want = call(None)
+        torch.cuda.synchronize()
+        for s in (side, side.cuda_stream, 0):  # 0: the default stream
+            got = call(s)
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(got, want))
