@@ -265,6 +265,9 @@ int gnn_set_workspace_limit(gnn_handle *h, int64_t bytes);
  * the message of the last failed call on this thread ("" if none).  The
  * pointer stays valid until the next failing call on the same thread. */
 const char *gnn_last_error(void);
+/* That call's error code (GNN_OK if none): the calls that return a handle, or 0
+ * for a count, have no other place for it. */
+int gnn_last_error_code(void);
 
 /* ---- graph construction ---------------------------------------------------
  * Paper section 2.1: an embedding network maps every space point into a

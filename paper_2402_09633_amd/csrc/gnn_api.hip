@@ -31,6 +31,7 @@ using namespace gnn;
 namespace {
 
 thread_local std::string g_last_error;
+thread_local int g_last_code = GNN_OK;
 
 int fail(int code, const char *fmt, ...) {
   char buf[512];
@@ -39,6 +40,7 @@ int fail(int code, const char *fmt, ...) {
   vsnprintf(buf, sizeof buf, fmt, ap);
   va_end(ap);
   g_last_error = buf;
+  g_last_code = code;
   return code;
 }
 
@@ -1363,6 +1365,8 @@ size_t gnn_weight_count(const gnn_dims *dims) {
 }
 
 const char *gnn_last_error(void) { return g_last_error.c_str(); }
+
+int gnn_last_error_code(void) { return g_last_code; }
 
 gnn_handle *gnn_create(const float *weights, const gnn_dims *dims) {
   if (check_dims(dims) != GNN_OK) return nullptr;

@@ -48,7 +48,7 @@ EXPORTS = ("gnn_weight_count", "gnn_create", "gnn_infer", "gnn_infer_logits", "g
            "gnn_hbm_probe", "gnn_quantize_rows", "gnn_group_workspace", "gnn_group_rows",
            "gnn_linear_weight_count", "gnn_linear_create", "gnn_linear_workspace",
            "gnn_linear_apply", "gnn_linear_destroy", "gnn_mlp_weight_count", "gnn_mlp_create",
-           "gnn_mlp_workspace", "gnn_mlp_apply", "gnn_mlp_destroy")
+           "gnn_mlp_workspace", "gnn_mlp_apply", "gnn_mlp_destroy", "gnn_last_error_code")
 STAGES = ("csr", "node_enc", "edge_enc", "edge_update", "aggregate", "node_update",
           "classifier", "total")
 
@@ -173,6 +173,8 @@ def _load():
     L.gnn_set_workspace_limit.argtypes = [vp, i64]
     L.gnn_last_error.restype = ctypes.c_char_p
     L.gnn_last_error.argtypes = []
+    L.gnn_last_error_code.restype = ctypes.c_int
+    L.gnn_last_error_code.argtypes = []
     L.gnn_profile_enable.restype = ctypes.c_int
     L.gnn_profile_enable.argtypes = [vp, ctypes.c_int]
     L.gnn_profile_read.restype = ctypes.c_int
@@ -267,6 +269,10 @@ def _check(rc: int) -> int:
 
 def gnn_last_error() -> str:
     return lib.gnn_last_error().decode()
+
+
+def gnn_last_error_code() -> int:
+    return int(lib.gnn_last_error_code())
 
 
 def gnn_weight_count(dims: gnn_dims) -> int:
@@ -664,13 +670,13 @@ def gnn_mlp_weight_count(dims: gnn_mlp_dims) -> int:
 def _create_from_blob(count, create, weights, dims, what: str) -> int:
     n = int(count(ctypes.byref(dims)))
     if n == 0:
-        raise GnnError(GNN_E_INVALID_ARG, gnn_last_error())
+        raise GnnError(gnn_last_error_code(), gnn_last_error())
     w = np.ascontiguousarray(weights, np.float32)
     if w.size != n:
         raise ValueError(f"{what} blob has {w.size} floats, dims need {n}")
     h = create(w.ctypes.data, ctypes.byref(dims))
     if not h:
-        raise GnnError(GNN_E_INVALID_ARG, gnn_last_error())
+        raise GnnError(gnn_last_error_code(), gnn_last_error())
     return h
 
 

@@ -1,4 +1,5 @@
 """The binding of the row operators, as far as it needs no GPU."""
+import numpy as np
 import pytest
 import torch
 
@@ -40,3 +41,28 @@ def test_rows_wider_than_32_bits_are_refused(G):
             G._rows("x", x, None, None, meta)
     x = torch.empty(2, (1 << 31) - 1, dtype=torch.bfloat16, device=meta)
     assert G._rows("x", x, None, None, meta)[1:] == (G.GNN_BF16, (1 << 31) - 1)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(in_features=0), "GNN_E_INVALID_ARG"), (dict(dtype=9), "GNN_E_INVALID_ARG"),
+    (dict(in_features=16385), "GNN_E_UNSUPPORTED"), (dict(n_groups=4097), "GNN_E_UNSUPPORTED"),
+    (dict(dtype=0), "GNN_E_UNSUPPORTED")])
+def test_refused_layers_say_why(G, kw, code):
+    d = G.make_linear_dims(**{**dict(in_features=8, out_features=8), **kw})
+    with pytest.raises(G.GnnError) as e:
+        G.gnn_linear_create(np.zeros(72, np.float32), d)
+    assert e.value.code == getattr(G, code) == G.gnn_last_error_code()
+    with pytest.raises(G.GnnError) as e:
+        G.gnn_mlp_create(np.zeros(72, np.float32),
+                         G.make_mlp_dims([d.in_features, 8], d.n_groups, d.dtype))
+    assert e.value.code == getattr(G, code)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="a GPU is visible")
+def test_creating_without_a_device_says_so(G):
+    with pytest.raises(G.GnnError) as e:
+        G.gnn_linear_create(np.zeros(72, np.float32), G.make_linear_dims(8, 8))
+    assert e.value.code == G.GNN_E_NO_DEVICE
+    with pytest.raises(G.GnnError) as e:
+        G.gnn_mlp_create(np.zeros(72, np.float32), G.make_mlp_dims([8, 8]))
+    assert e.value.code == G.GNN_E_NO_DEVICE
