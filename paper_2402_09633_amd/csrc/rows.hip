@@ -13,7 +13,7 @@ namespace {
 // Bound by memory: x is read and q written once; 1000513 x 128 fp32 110 us, 5.9
 // TB/s.
 constexpr int Q_WAVES = 4;
-constexpr int Q_GRID = 1 << 20;  // most workgroups of a launch
+constexpr int Q_GRID = 1 << 20;  // most workgroups in a dimension of a launch
 
 __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q) {
   if (k <= K - 8) {
@@ -26,7 +26,12 @@ __device__ __forceinline__ void store_q8(int8_t *row, int k, int K, const u2 &q)
 }
 
 template <int XT, int C, bool FULL>
-__device__ __forceinline__ void quantize_row(const QuantArgs &a, int64_t r, int u0, int L) {
+__global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = 64 / L, sub = lane / L, u0 = lane % L;
+  const int64_t wg = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  const int64_t r = (wg * Q_WAVES + wave) * per + sub;
+  if (r >= a.n) return;
   const int width = a.pad ? a.pad : a.K;
   const elem_t<XT> *row = (const elem_t<XT> *)a.x + r * a.x_stride;
   Raw8<XT> raw[C];
@@ -48,15 +53,6 @@ __device__ __forceinline__ void quantize_row(const QuantArgs &a, int64_t r, int 
       store_q8(q, 8 * (u0 + L * c), width, v);
   }
   for (int u = u0 + L * C; 8 * u < width; u += L) store_q8(q, 8 * u, width, u2{0u, 0u});
-}
-
-template <int XT, int C, bool FULL>
-__global__ __launch_bounds__(64 * Q_WAVES) void quantize_rows(QuantArgs a, int L) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = 64 / L, sub = lane / L, u0 = lane % L;
-  const int64_t step = (int64_t)gridDim.x * Q_WAVES * per;
-  for (int64_t r = ((int64_t)blockIdx.x * Q_WAVES + wave) * per + sub; r < a.n; r += step)
-    quantize_row<XT, C, FULL>(a, r, u0, L);
 }
 
 // Rows too wide for a wave's registers: a workgroup to a row, which is read
@@ -98,9 +94,12 @@ hipError_t quantize_t(const QuantArgs &a, hipStream_t stream) {
   while (8 * L < units) L *= 2;
   const int C = (units + L - 1) / L;
   const int64_t rows = (int64_t)Q_WAVES * (64 / L);
-  // a launch takes fewer than 2^32 threads: 2^28 rows of 16 to a workgroup go round
+  // A dimension of a launch has fewer than 2^32 threads, which 2^28 rows of 16 to a
+  // workgroup reach: a second one behind the first Q_GRID workgroups.  (A loop over
+  // the rows kept a partial row's comparisons in scalar registers, 82 vector
+  // registers in place of 51: 100000 x 1152 bf16 77 us -> 90.)
   const int64_t wgs = (a.n + rows - 1) / rows;
-  const dim3 grid((uint32_t)(wgs < Q_GRID ? wgs : Q_GRID));
+  const dim3 grid((uint32_t)(wgs < Q_GRID ? wgs : Q_GRID), (uint32_t)((wgs + Q_GRID - 1) / Q_GRID));
   auto go = [&](auto n) {
     constexpr int CC = decltype(n)::value;
     if (a.K == 8 * CC * L) return launch(quantize_rows<XT, CC, true>, grid, block, 0, stream, a, L);
