@@ -580,6 +580,17 @@ int gnn_debug_frnn(const float *z, int64_t n_nodes, int32_t dim, float r2, int32
  * slots up to 2^24 points where they can be allocated, else 4. */
 size_t gnn_debug_frnn_bytes(int64_t n_nodes, int32_t dim, int32_t n_slots);
 
+/* Which kernel a gnn_linear_apply call of these widths and rows takes on a device
+ * of n_cu compute units (needs no device; y at an address that is a multiple of
+ * 64; grouped: with offsets): kernel[0] 1 if the rows are converted in a pass of
+ * their own first; kernel[1] row blocks to a wave of the tiles for wide layers (4
+ * or 2), or 0 if row panels take the call, and then kernel[2] blocks of 32 rows
+ * to a panel (4, 2 or 1), kernel[3] its waves, kernel[4] how its rows are staged
+ * (0 whole, 1 in chunks, 2 whole and narrow), kernel[5] 1 if its waves share a
+ * block of channels. */
+int gnn_debug_linear(const gnn_linear_dims *dims, int32_t n_cu, int32_t x_type, int64_t n_rows,
+                     int32_t grouped, int32_t y_type, int64_t y_stride, int32_t kernel[6]);
+
 #ifdef __cplusplus
 }
 #endif

@@ -405,19 +405,31 @@ struct LinearArgs {
   void *y = nullptr;
   int32_t y_type = 0;
   int64_t y_stride = 0;
-  int32_t chunk = 0;              // bytes of a row staged at a time
+  int32_t chunk = 0;              // bytes of a row staged at a time (from the plan)
   int32_t nsplit = 1;             // workgroups that share the output blocks of a row tile
 };
+// How a call runs: which kernel, and what its rows have to be first.
+struct LinearPlan {
+  // rows are given to the launch in the weights' type (8 bits: rounded, with
+  // scales) in rows of 32 S bytes, zeros behind the last element
+  bool convert = false;
+  int tile = 0;                   // tiles for wide layers: row blocks to a wave (0: row panels)
+  // row panels: RB blocks of 32 rows to a tile, NW waves, rows staged in chunks
+  // (multi) or whole, in the registers of three workgroups to a CU (narrow)
+  int RB = 0, NW = 0;
+  bool multi = false, narrow = false;
+  bool split = false;             // the waves share a channel block's steps
+  int64_t tiles = 0;
+  int32_t chunk = 0, nsplit = 1;  // as in LinearArgs
+};
+// From a's widths, types, n, off, y and y_stride.
+LinearPlan linear_plan(const LinearArgs &a, int n_cu);
 // Bytes of a layer's fragments, and the steps of 32 bytes of a row.
 int32_t linear_steps(int32_t K, int w_type);
 size_t linear_frag_bytes(int32_t K, int32_t N, int32_t G, int w_type);
 // Lays out `blob` (device fp32, per group W [N][K] and b [N]).
 hipError_t launch_linear_layout(const float *blob, const LinearArgs &a, void *w, float *ws,
                                 float *bias, hipStream_t stream);
-// Whether a call of n rows takes rows of x_type as they are.  If not, they are
-// given to it in the weights' type (8 bits: rounded, with scales) in rows of
-// 32 S bytes, zeros behind the last element.
-bool linear_takes(const LinearArgs &a, int x_type, int64_t n, int n_cu);
 // Such rows of 16 bits, or of 8 bits that are there already.
 struct ConvertArgs {
   const void *x = nullptr;
@@ -428,7 +440,7 @@ struct ConvertArgs {
   void *y = nullptr;
 };
 hipError_t launch_convert(const ConvertArgs &a, hipStream_t stream);
-hipError_t launch_linear(const LinearArgs &a, int n_cu, hipStream_t stream);
+hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, hipStream_t stream);
 
 // flag <- 1 if any of the 2*n_edges indices lies outside [0, n_nodes).
 hipError_t launch_validate(const int32_t *edge_index, int64_t n_edges, int32_t n_nodes,

@@ -582,16 +582,8 @@ __global__ __launch_bounds__(256) void linear_layout(const float *__restrict__ b
   }
 }
 
-// What a launch of the row panels needs: RB row blocks to a tile, NW waves, rows
-// staged whole or in chunks (multi).
-struct Plan {
-  int RB, NW;
-  bool multi, split;  // split: the waves share a block's steps
-  int64_t tiles;
-};
-
 template <int WT, int XT, int RB, int WK, int NW, int MODE>
-hipError_t panel(const LinearArgs &a, const Plan &p, hipStream_t stream) {
+hipError_t panel(const LinearArgs &a, const LinearPlan &p, hipStream_t stream) {
   size_t lds = (size_t)32 * RB * (a.chunk + LDS_PAD);
   if (WK > 1 && lds < 4096 * NW) lds = 4096 * NW;
   return launch_lds(linear_panel<WT, XT, RB, WK, NW, MODE>,
@@ -599,7 +591,7 @@ hipError_t panel(const LinearArgs &a, const Plan &p, hipStream_t stream) {
 }
 
 template <int WT, int XT>
-hipError_t panel_rows(const LinearArgs &a, const Plan &p, hipStream_t stream) {
+hipError_t panel_rows(const LinearArgs &a, const LinearPlan &p, hipStream_t stream) {
   if (p.multi) {
     if constexpr (WT != T_I8 || XT == T_I8) {
       if (p.split) return panel<WT, XT, 1, 8, 8, CHUNKS>(a, p, stream);
@@ -616,7 +608,7 @@ hipError_t panel_rows(const LinearArgs &a, const Plan &p, hipStream_t stream) {
     return panel<WT, XT, 2, 1, 4, WHOLE>(a, p, stream);
   }
   if (p.split) return panel<WT, XT, 1, 8, 8, WHOLE>(a, p, stream);
-  if (a.S * 32 <= narrow_bytes(WT)) return panel<WT, XT, 1, 1, 8, NARROW>(a, p, stream);
+  if (p.narrow) return panel<WT, XT, 1, 1, 8, NARROW>(a, p, stream);
   return panel<WT, XT, 1, 1, 8, WHOLE>(a, p, stream);
 }
 
@@ -653,54 +645,54 @@ hipError_t launch_linear_layout(const float *blob, const LinearArgs &a, void *w,
 }
 
 // Whether the tiles for wide layers take a call of n rows, and with how many
-// row blocks to a wave (0: the row panels do).  Measured (panels : tiles, us):
-//  - rows up to 1 KB: 100000 x 512 -> 512 bf16 87 : 88, 300000 x 128 -> 128 bf16
-//    42 : 54; past it 100000 x 640 -> 640 159 : 129, 1024 -> 256 107 : 74,
-//    2048 -> 512 367 : 247
-//  - 8-bit layers whose rows come as floats pay for a pass over the rows first:
-//    100000 x 1024 -> 1024 195 : 241, 2048 -> 512 242 : 269, but 30000 x 1024 ->
-//    2048 128 : 110
-//  - few tiles leave CUs idle: 1000 x 4096 -> 512 bf16 30 : 62, 300 x 4096 -> 4096
-//    43 : 63, 4000 x 2048 -> 2048 69 : 42; 32 groups of 312 rows x 1024 -> 1024
-//    43 : 47, of 937 118 : 99
+// row blocks to a wave (0: the row panels do).  extra: its rows would be rounded
+// to 8 bits for the tiles alone, the panels take them as they are.  Measured
+// (panels : tiles, us, bf16 rows and outputs where no type is given):
+//  - rows up to 1 KB: 100000 x 512 -> 512 bf16 88 : 90, 300000 x 128 -> 128 bf16
+//    42 : 54; past it 100000 x 640 -> 640 163 : 134, 1024 -> 256 113 : 80,
+//    2048 -> 512 399 : 258
+//  - 8-bit layers whose rows come as floats pay for a pass over the rows first
+//    (in the tiles' times): 100000 x 1024 -> 1024 197 : 243, 2048 -> 512 237 : 272,
+//    but 30000 x 1024 -> 2048 144 : 117, 8000 x 1024 -> 4096 81 : 62; where 64 of
+//    their rows fit a panel the pass does not pay, 100000 x 1024 -> 1056 200 : 253,
+//    1152 -> 1056 225 : 275, fp32 34000 x 1024 -> 1300 140 : 145 (34000 x 1024 ->
+//    4096 loses by it, 263 : 240)
+//  - few tiles leave CUs idle: 1000 x 4096 -> 512 bf16 33 : 47, 300 x 4096 -> 4096
+//    44 : 49, 4000 x 2048 -> 2048 79 : 41; 32 groups of 312 rows x 1024 -> 1024
+//    43 : 47 with the rows in the last-level cache and 47 : 42 without, of 937
+//    126 : 104
 //  - 256 rows to a tile where that gives every CU one: 16384 x 4096 -> 4096 8-bit
-//    288, with 128 rows 321; 2048 x 4096 -> 4096 55 and 39
-int tiled_rows(const LinearArgs &a, int x_type, int64_t n, int n_cu) {
+//    rows 277, with 128 rows 305; 2048 x 4096 -> 4096 56 and 44
+static int tiled_rows(const LinearArgs &a, bool extra, int64_t n, int n_cu) {
   const int ntile = (a.NB + T_CH - 1) / T_CH;
-  const bool rounds = a.w_type == T_I8 && x_type != T_I8;
-  if (a.S * 32 < (rounds ? 1024 : 1025) || a.NB <= (rounds ? 32 : 4)) return 0;
+  if (a.S * 32 < (extra ? 1024 : 1025) || a.NB <= (extra ? 32 : 4)) return 0;
+  if (extra && n / 64 >= 2 * n_cu && 64 * (a.S * 32 + LDS_PAD) <= HALF) return 0;
   if (n / a.G < 512 || n / 128 * ntile < n_cu / 2) return 0;
   return n / 256 * ntile >= n_cu ? 4 : 2;
 }
 
-bool linear_takes(const LinearArgs &a, int x_type, int64_t n, int n_cu) {
-  if (tiled_rows(a, x_type, n, n_cu))
-    return x_type == a.w_type && a.K * type_bytes(a.w_type) % 16 == 0;
-  if (a.w_type == T_I8) return x_type == T_I8 || a.S * 32 <= CHUNK;
-  return x_type == T_F32 || x_type == a.w_type;
-}
-
-hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
-  LinearArgs a = args;
-  if (const int TR = tiled_rows(a, a.x_type, a.n, n_cu)) {
-    if (a.w_type == T_I8) return tiled<T_I8>(a, TR, stream);
-    if (a.w_type == T_BF16) return tiled<T_BF16>(a, TR, stream);
-    return tiled<T_F16>(a, TR, stream);
+LinearPlan linear_plan(const LinearArgs &a, int n_cu) {
+  // The decision is made once, for the rows as the caller has them, and holds for
+  // the launch after they were converted.
+  const bool rounds = a.w_type == T_I8 && a.x_type != T_I8;
+  const bool panels = a.w_type == T_I8 ? !rounds || a.S * 32 <= CHUNK
+                                       : a.x_type == T_F32 || a.x_type == a.w_type;
+  LinearPlan p;
+  p.tile = tiled_rows(a, rounds && panels, a.n, n_cu);
+  if (p.tile) {
+    p.convert = a.x_type != a.w_type || a.K * type_bytes(a.w_type) % 16 != 0;
+    return p;
   }
+  p.convert = !panels;
   // The rows of a tile stay in LDS: 128 of them where two workgroups' fit on a
   // CU, fewer of wide ones and where there are too few tiles to fill the CUs.
   // Layers of up to four channel blocks keep four waves busy: smaller workgroups,
   // and more of them to a CU (300000 x 128 -> 128 bf16 37 us with four waves, 44
   // with eight; 1000513 x 384 -> 128 f16 272 and 298).  Wider ones take eight
   // (300000 x 512 -> 512 8-bit 187 us, 201 with four waves and 64 rows).
-  Plan p;
   const int row_bytes = a.S * 32;
   p.multi = row_bytes > CHUNK;
-  a.chunk = p.multi ? CHUNK / 2 : row_bytes;
-  auto tiles = [&](int RB) {
-    const int64_t PM = 32 * RB;
-    return a.off ? a.n / PM + a.G : (a.n + PM - 1) / PM;
-  };
+  p.chunk = p.multi ? CHUNK / 2 : row_bytes;
   p.NW = a.NB <= 4 ? 4 : WAVES;
   const int room = p.NW == WAVES ? HALF : HALF / 2;
   // Output rows that do not start on 64 bytes share cache sectors between two
@@ -711,20 +703,34 @@ hipError_t launch_linear(const LinearArgs &args, int n_cu, hipStream_t stream) {
   const int64_t ysz = type_bytes(a.y_type);
   const bool torn = ((uintptr_t)a.y % 64 || a.y_stride * ysz % 64) && a.N * ysz > 1536;
   p.RB = p.multi ? 1 : torn ? 2 : 4;
-  while (p.RB > 1 && (32 * p.RB * (a.chunk + LDS_PAD) > (p.RB == 4 ? room : HALF) ||
+  while (p.RB > 1 && (32 * p.RB * (p.chunk + LDS_PAD) > (p.RB == 4 ? room : HALF) ||
                       a.n / (32 * p.RB) < 2 * n_cu))
     p.RB /= 2;
   if (p.RB == 1) p.NW = WAVES;
-  p.tiles = tiles(p.RB);
+  const int64_t PM = 32 * p.RB;
+  p.tiles = a.off ? a.n / PM + a.G : (a.n + PM - 1) / PM;
   // No more blocks than CUs, or one to a tile: all waves to each.  Measured (eight
   // blocks to a workgroup : one, us): 1 x 4096 -> 4096 bf16 29.7 : 13.1, 64 x 4096
   // -> 4096 8-bit 22.3 : 15.2; with more blocks the rows are staged too often, 300 x
   // 1024 -> 1024 8-bit 8.3 : 11.4, 1000 x 1024 -> 1024 bf16 10.1 : 17.6.
   p.split = p.RB == 1 && (p.tiles * a.NB <= n_cu || a.NB == 1) && a.S >= 2 * WAVES;
+  p.narrow = p.RB == 1 && !p.multi && !p.split && row_bytes <= narrow_bytes(a.w_type);
   const int WN = p.split ? 1 : p.NW;
   const int ntile = (a.NB + WN - 1) / WN;
-  a.nsplit = (int)((2 * n_cu + p.tiles - 1) / p.tiles);
-  if (a.nsplit > ntile || p.split) a.nsplit = ntile;
+  p.nsplit = (int)((2 * n_cu + p.tiles - 1) / p.tiles);
+  if (p.nsplit > ntile || p.split) p.nsplit = ntile;
+  return p;
+}
+
+hipError_t launch_linear(const LinearArgs &args, const LinearPlan &p, hipStream_t stream) {
+  LinearArgs a = args;
+  if (p.tile) {
+    if (a.w_type == T_I8) return tiled<T_I8>(a, p.tile, stream);
+    if (a.w_type == T_BF16) return tiled<T_BF16>(a, p.tile, stream);
+    return tiled<T_F16>(a, p.tile, stream);
+  }
+  a.chunk = p.chunk;
+  a.nsplit = p.nsplit;
   if (a.w_type == T_I8) {
     if (a.x_type == T_I8) return panel_rows<T_I8, T_I8>(a, p, stream);
     if (a.x_type == T_F32) return panel_rows<T_I8, T_F32>(a, p, stream);

@@ -108,17 +108,33 @@ int check_linear_dims(const gnn_linear_dims *d) {
   return GNN_OK;
 }
 
+LinearArgs linear_widths(const gnn_linear_dims &d) {
+  LinearArgs a;
+  a.K = d.in_features;
+  a.N = d.out_features;
+  a.G = d.n_groups;
+  a.w_type = d.dtype;
+  a.NB = (a.N + 31) / 32;
+  a.S = linear_steps(a.K, a.w_type);
+  return a;
+}
+
 // Scratch of a call: its rows in the form that the kernels take, and 8-bit
 // rows' scales, where they do not take the caller's.
 size_t linear_scratch(const gnn_linear *l, int x_type, int64_t n_rows) {
-  if (linear_takes(l->tmpl, x_type, n_rows, l->n_cu)) return 0;
+  if (n_rows == 0) return 0;
+  LinearArgs a = l->tmpl;
+  a.x_type = x_type;
+  a.n = (int32_t)n_rows;
+  if (!linear_plan(a, l->n_cu).convert) return 0;
   const bool round8 = l->dims.dtype == GNN_INT8 && x_type != GNN_INT8;
   return up256((size_t)n_rows * l->tmpl.S * 32) + (round8 ? up256((size_t)n_rows * 4) : 0);
 }
 
 // The launches of a layer; everything has been checked.
 int run_linear(const gnn_linear *l, LinearArgs a, unsigned char *ws, hipStream_t stream) {
-  if (!linear_takes(a, a.x_type, a.n, l->n_cu)) {
+  const LinearPlan plan = linear_plan(a, l->n_cu);
+  if (plan.convert) {
     hipError_t e;
     const int pad = a.S * 32 / type_bytes(a.w_type);
     if (a.w_type == GNN_INT8 && a.x_type != GNN_INT8) {
@@ -151,7 +167,7 @@ int run_linear(const gnn_linear *l, LinearArgs a, unsigned char *ws, hipStream_t
     a.x_type = a.w_type;
     a.x_stride = pad;
   }
-  return launched(launch_linear(a, l->n_cu, stream), "linear layer");
+  return launched(launch_linear(a, plan, stream), "linear layer");
 }
 
 }  // namespace
@@ -232,12 +248,7 @@ gnn_linear *gnn_linear_create(const float *weights, const gnn_linear_dims *dims)
   l->device = dev;
   l->n_cu = cu_count(dev);
   LinearArgs &a = l->tmpl;
-  a.K = dims->in_features;
-  a.N = dims->out_features;
-  a.G = dims->n_groups;
-  a.w_type = dims->dtype;
-  a.NB = (a.N + 31) / 32;
-  a.S = linear_steps(a.K, a.w_type);
+  a = linear_widths(*dims);
   const size_t fb = linear_frag_bytes(a.K, a.N, a.G, a.w_type);
   const size_t cb = up256((size_t)a.G * a.NB * 32 * 4);
   const size_t blob = gnn_linear_weight_count(dims) * 4;
@@ -320,6 +331,30 @@ int gnn_linear_apply(gnn_linear *l, const void *x, int32_t x_type, int64_t x_str
   a.y_type = y_type;
   a.y_stride = y_stride;
   return run_linear(l, a, (unsigned char *)workspace, stream);
+}
+
+int gnn_debug_linear(const gnn_linear_dims *dims, int32_t n_cu, int32_t x_type, int64_t n_rows,
+                     int32_t grouped, int32_t y_type, int64_t y_stride, int32_t kernel[6]) {
+  int rc = check_linear_dims(dims);
+  if (rc || (rc = check_rows(n_rows))) return rc;
+  if (n_rows == 0 || n_cu < 1 || !kernel || !float_type(y_type) ||
+      (!float_type(x_type) && (x_type != GNN_INT8 || dims->dtype != GNN_INT8)))
+    return bad(GNN_E_INVALID_ARG, "bad arguments");
+  static const int32_t some = 0;
+  LinearArgs a = linear_widths(*dims);
+  a.x_type = x_type;
+  a.n = (int32_t)n_rows;
+  a.off = grouped ? &some : nullptr;  // whether there are offsets
+  a.y_type = y_type;
+  a.y_stride = y_stride;
+  const LinearPlan p = linear_plan(a, n_cu);
+  kernel[0] = p.convert;
+  kernel[1] = p.tile;
+  kernel[2] = p.RB;
+  kernel[3] = p.NW;
+  kernel[4] = p.multi ? 1 : p.narrow ? 2 : 0;
+  kernel[5] = p.split;
+  return GNN_OK;
 }
 
 }  // extern "C"

@@ -48,7 +48,8 @@ EXPORTS = ("gnn_weight_count", "gnn_create", "gnn_infer", "gnn_infer_logits", "g
            "gnn_hbm_probe", "gnn_quantize_rows", "gnn_group_workspace", "gnn_group_rows",
            "gnn_linear_weight_count", "gnn_linear_create", "gnn_linear_workspace",
            "gnn_linear_apply", "gnn_linear_destroy", "gnn_mlp_weight_count", "gnn_mlp_create",
-           "gnn_mlp_workspace", "gnn_mlp_apply", "gnn_mlp_destroy", "gnn_last_error_code")
+           "gnn_mlp_workspace", "gnn_mlp_apply", "gnn_mlp_destroy", "gnn_last_error_code",
+           "gnn_debug_linear")
 STAGES = ("csr", "node_enc", "edge_enc", "edge_update", "aggregate", "node_update",
           "classifier", "total")
 
@@ -222,6 +223,9 @@ def _load():
         f.restype, f.argtypes = None, [vp]
     L.gnn_linear_apply.restype = ctypes.c_int
     L.gnn_linear_apply.argtypes = [vp, vp, i32, i64, vp, i64, vp, vp, vp, i32, i64, vp, i64, vp]
+    L.gnn_debug_linear.restype = ctypes.c_int
+    L.gnn_debug_linear.argtypes = [ctypes.POINTER(gnn_linear_dims), i32, i32, i64, i32, i32, i64,
+                                   ctypes.POINTER(ctypes.c_int32)]
     L.gnn_mlp_apply.restype = ctypes.c_int
     L.gnn_mlp_apply.argtypes = [vp, vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, vp]
     L.gnn_server_create.restype = vp
@@ -700,6 +704,15 @@ def gnn_linear_apply(layer, x, x_type: int, x_stride: int, x_scales, n_rows: int
     return _check(lib.gnn_linear_apply(layer, _addr(x), x_type, x_stride, _addr(x_scales), n_rows,
                                        _addr(offsets), _addr(order), _addr(y), y_type, y_stride,
                                        _addr(workspace), workspace_bytes, _stream(stream)))
+
+
+def gnn_debug_linear(dims: gnn_linear_dims, n_cu: int, x_type: int, n_rows: int, grouped=False,
+                     y_type: int = GNN_FP32, y_stride: int = 0) -> tuple:
+    """The C call's kernel[0 .. 5]; y_stride 0: the output's width."""
+    k = (ctypes.c_int32 * 6)()
+    _check(lib.gnn_debug_linear(ctypes.byref(dims), n_cu, x_type, n_rows, int(grouped), y_type,
+                                y_stride or dims.out_features, k))
+    return tuple(k)
 
 
 def gnn_mlp_create(weights: np.ndarray, dims: gnn_mlp_dims) -> int:
