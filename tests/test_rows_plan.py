@@ -2,6 +2,8 @@
 that the GPU tests of the layers reach (256 compute units)."""
 import pytest
 
+from tests.test_gpu_rows_panels import CASES, ROWS
+
 CU = 256
 
 
@@ -66,3 +68,35 @@ def test_debug_linear_refuses(G):
     ("bf16", "bf16", 9000, 1001, 1064, 5, 2), ("f16", "f16", 17_000, 904, 1100, 7, 4)])
 def test_tiles_take(G, kind, xt, m, k, n, g, tile):
     assert plan(G, kind, xt, m, k, n, g)[1] == tile
+
+
+# The calls of test_gpu_rows_panels.py, and the ones that it compares them with.
+@pytest.mark.parametrize("case", CASES, ids=lambda c: f"{c[0]}x{c[1]}-{c[2]}")
+@pytest.mark.parametrize("kind", ["i8", "bf16", "f16"])
+def test_large_calls_take(G, kind, case):
+    m, k, n, out, gap, g, want8, want16 = case
+    want = want8 if kind == "i8" else want16
+    for xt in ROWS[kind]:
+        convert, tile, rb, waves, staging, split = plan(G, kind, xt, m, k, n, g, out, n + gap)
+        if want is not None and len(want) == 2:
+            assert (tile, rb, waves) == (0, *want), xt
+        elif want is not None:
+            assert (tile,) == want, xt
+        if g == 1:  # calls of few rows run something else
+            assert plan(G, kind, xt, 3000, k, n, g, out, n) != (convert, tile, rb, waves, staging, split)
+
+
+def test_the_large_calls_reach_every_large_kernel(G):
+    """Every panel of more than 32 rows, and both tiles, in every pair of weight
+    and row types that they come in."""
+    seen = set()
+    for m, k, n, out, gap, g, _, _ in CASES:
+        for kind, rows in ROWS.items():
+            for xt in rows:
+                convert, tile, rb, waves, staging, split = plan(G, kind, xt, m, k, n, g, out, n + gap)
+                seen.add((kind, kind if convert else xt, tile, rb, waves))
+    for kind, rows in ROWS.items():
+        for xt in rows:
+            for rb, waves in ((4, 8), (2, 8), (4, 4), (2, 4)):
+                assert (kind, xt, 0, rb, waves) in seen, (kind, xt, rb, waves)
+        assert (kind, kind, 4, 0, 0) in seen, kind
