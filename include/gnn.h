@@ -327,7 +327,8 @@ int gnn_frnn(const float *z, int64_t n_nodes, int32_t dim, float r2, int32_t *ed
  * nothing; scratch is the caller's (device memory aligned to 256 bytes, which
  * the call may overwrite until the stream has passed it; each call in flight
  * needs its own), so calls may overlap and may be captured into graphs.
- * Outputs must not overlap inputs.  Results are bitwise deterministic. */
+ * Outputs must not overlap inputs.  Results are bitwise deterministic, but for
+ * rows that several positions of an order name (gnn_linear_apply). */
 #define GNN_F16 2  /* element and weight type: IEEE half precision               */
 #define GNN_INT8 3 /* whole numbers -127..127, with fp32 scales beside them      */
 
@@ -385,8 +386,10 @@ size_t gnn_linear_workspace(const gnn_linear *l, int32_t x_type, int64_t n_rows)
  *            g's rows are at positions offsets[g] .. offsets[g + 1] - 1
  *   order    [n_rows], or NULL: position p is row order[p], of x and of y alike
  * Rows of no group are left as they were in y.  Offsets and order entries out
- * of range are clamped (no fault, meaningless rows); a row that several
- * positions name gets the result of one of them.
+ * of range are clamped (no fault, meaningless rows; an entry below 0 names row 0,
+ * one past the end the last row).  A row that several positions name gets, element
+ * by element, the result of one of them: positions of different groups may mix
+ * in it, and not always alike.
  * y_type GNN_FP32, GNN_BF16 or GNN_F16, rounded once from fp32. */
 int gnn_linear_apply(gnn_linear *l, const void *x, int32_t x_type, int64_t x_stride,
                      const float *x_scales, int64_t n_rows, const int32_t *offsets,

@@ -62,3 +62,32 @@ def test_streams_by_handle(G):
             got = call(s)
             torch.cuda.synchronize()
             assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+@pytest.mark.parametrize("kind", ["GNN_BF16", "GNN_INT8"])
+@pytest.mark.parametrize("m,n", [(64, 300), (4000, 1100), (70_000, 40)])
+def test_row_named_by_positions_of_two_groups(G, kind, m, n):
+    """Every element of such a row is the one or the other group's."""
+    rng = np.random.default_rng(1)
+    k = 24
+    d = G.make_linear_dims(k, n, 2, getattr(G, kind))
+    layer = G.Linear(rng.normal(size=G.gnn_linear_weight_count(d)).astype(np.float32), d)
+    x = torch.as_tensor(rng.normal(size=(m, k)).astype(np.float32)).cuda()
+    half = m // 2
+    off = torch.tensor([0, half, m], dtype=torch.int32, device="cuda")
+    order = torch.arange(m, dtype=torch.int32, device="cuda")
+    order[1:half:3] += half  # named by a position of group 0 and by their own of group 1
+    y = layer(x, offsets=off, order=order, out=torch.full((m, n), 9.0, device="cuda"))
+    first = layer(x, offsets=torch.tensor([0, m, m], dtype=torch.int32, device="cuda"))
+    second = layer(x, offsets=torch.tensor([0, 0, m], dtype=torch.int32, device="cuda"))
+    unnamed = torch.zeros(m, dtype=torch.bool, device="cuda")
+    unnamed[1:half:3] = True
+    twice = torch.roll(unnamed, half)
+    assert (y[unnamed] == 9).all()
+    assert ((y[twice] == first[twice]) | (y[twice] == second[twice])).all()
+    once = ~(unnamed | twice)
+    once[half:] = False
+    assert torch.equal(y[once], first[once])
+    once = ~(unnamed | twice)
+    once[:half] = False
+    assert torch.equal(y[once], second[once])
