@@ -180,10 +180,10 @@ __device__ __forceinline__ float quant_scale(float top) {
 // the even one (without a tie they are the same).
 //
 // fp32.  Factors one step below and above 1 / s round alike unless x / s is next
-// to a half.  Then half the sum h of what they lead to is that half, and x - h s
-// says on which side x / s lies: a multiple of the smaller of ulp(x) and ulp(s) /
-// 2, below s.  Times 2^24 where s < 1 it is exact in fp32 for the smallest scales
-// too, half of whose last place is no fp32 number.
+// to a half.  Then half the sum h of what they lead to, a and b, is that half, and
+// x - h s says on which side x / s lies.  It is formed as 2 (x - a s) + (a - b) s:
+// both steps are exact in fp32 (multiples of the smaller of ulp(x) and ulp(s), at
+// most s), also for the smallest scales, half of whose last place is no fp32 number.
 struct Quant {
   float s, lo, hi;
   bool zero, tie;
@@ -243,11 +243,11 @@ __device__ __forceinline__ u2 quantize8(const f8 &x, const Quant &z) {
     const u2 p = pack_bytes(u);
     if (((p[0] ^ q[0]) | (p[1] ^ q[1])) != 0 || z.zero) {
       asm volatile("");  // a branch, not selected values: it is hardly ever taken
-      const float up = z.s < 1.f ? 0x1p24f : 1.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float h = 0.5f * ((t[j] - ROUND_MAGIC) + (u[j] - ROUND_MAGIC));
-        const float r = __builtin_fmaf(-h, z.s * up, x[j] * up);
+        const float a = t[j] - ROUND_MAGIC, b = u[j] - ROUND_MAGIC;
+        const float h = 0.5f * (a + b);
+        const float r = __builtin_fmaf(2.f, __builtin_fmaf(-a, z.s, x[j]), (a - b) * z.s);
         t[j] = (h + (r == 0.f ? 0.f : __builtin_copysignf(0.25f, r))) + ROUND_MAGIC;
       }
       q = pack_bytes(t);
