@@ -9,7 +9,6 @@ module raises.
 from __future__ import annotations
 
 import ctypes
-import operator
 import os
 
 import numpy as np
@@ -87,10 +86,9 @@ _INT32_MAX = 2 ** 31 - 1
 
 def _int32(what: str, v) -> int:
     """A whole number of 32 bits: ctypes would pass the low bits of a larger one."""
-    v = operator.index(v)
-    if not -_INT32_MAX <= v <= _INT32_MAX:
-        raise ValueError(f"{what}: {v} is not a 32-bit number")
-    return v
+    if -_INT32_MAX <= v <= _INT32_MAX:
+        return v
+    raise ValueError(f"{what}: {v} is not a 32-bit number")
 
 
 class gnn_linear_dims(ctypes.Structure):
