@@ -199,3 +199,26 @@ def test_most_rows_through_a_network(G):
     for lo, hi in ((0, 5000), ((1 << 27) - 3000, (1 << 27) + 3000), (n - 5000, n)):
         assert torch.equal(y[lo:hi], mlp(x[lo:hi], ids[lo:hi])), lo
         assert (y[lo:hi][ids[lo:hi] < 0] == 0).all() and y[lo:hi].isfinite().all()
+
+
+@pytest.mark.parametrize("kind,unit", [("f16", 2.0 ** -24), ("bf16", 2.0 ** -133)])
+@pytest.mark.parametrize("m,k,n", [(5, 64, 40), (4100, 640, 1100), (40_000, 64, 40)])
+def test_subnormal_rows_and_weights_count(G, kind, unit, m, k, n):
+    """Whole multiples of the smallest number of a 16-bit type, on either side: the
+    sums are exact."""
+    t = {"f16": torch.float16, "bf16": torch.bfloat16}[kind]
+    rng = np.random.default_rng(1)
+    small = (rng.integers(-60, 61, (n, k)) * unit).astype(np.float32)
+    big = rng.integers(-8, 9, (m, k)).astype(np.float32)
+    dims = G.make_linear_dims(k, n, 1, G.GNN_F16 if kind == "f16" else G.GNN_BF16)
+    b = np.zeros(n, np.float32)
+    layer = G.Linear(np.concatenate([small.ravel(), b]), dims)
+    y = layer(torch.as_tensor(big).to(t).cuda(), out_dtype=torch.float32)
+    assert np.array_equal(y.double().cpu().numpy(), big.astype(np.float64) @ small.astype(np.float64).T)
+    few = rng.integers(-8, 9, (n, k)).astype(np.float32)
+    layer = G.Linear(np.concatenate([few.ravel(), b]), dims)
+    x = (rng.integers(-60, 61, (m, k)) * unit).astype(np.float32)
+    y = layer(torch.as_tensor(x).to(t).cuda(), out_dtype=torch.float32)
+    assert np.array_equal(y.double().cpu().numpy(), x.astype(np.float64) @ few.astype(np.float64).T)
+    y = layer(torch.as_tensor(x).cuda(), out_dtype=torch.float32)  # rounded on the way
+    assert np.array_equal(y.double().cpu().numpy(), x.astype(np.float64) @ few.astype(np.float64).T)
