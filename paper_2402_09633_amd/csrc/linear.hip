@@ -394,7 +394,7 @@ __global__ __launch_bounds__(64 * NW, RB > 1           ? 4
 // at a time and two such stages in turn; a wave's weights come from the caches
 // into registers, in fragment order.  While a stage is multiplied, the next one's
 // weights and the rows of the one after it are in flight.  16384 x 4096 -> 4096 in
-// 8 bits: 270 us, 2.0 POP/s; 8192 cubed in bf16 897 us, 1.2 PFLOP/s.
+// 8 bits: 270 us, 2.0 POP/s; 8192 cubed in bf16 910 us, 1.2 PFLOP/s.
 constexpr int T_STEPS = 4;                // steps of 32 bytes in a stage
 constexpr int T_BYTES = 32 * T_STEPS;     // of a row
 constexpr int T_CH = 8;                   // channel blocks of a tile
