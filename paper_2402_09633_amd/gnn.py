@@ -86,7 +86,7 @@ _INT32_MAX = 2 ** 31 - 1
 
 def _int32(what: str, v) -> int:
     """A whole number of 32 bits: ctypes would pass the low bits of a larger one."""
-    if -_INT32_MAX <= v <= _INT32_MAX:
+    if -_INT32_MAX - 1 <= v <= _INT32_MAX:
         return v
     raise ValueError(f"{what}: {v} is not a 32-bit number")
 
