@@ -429,6 +429,91 @@ int gnn_mlp_apply(gnn_mlp *m, const void *x, int32_t x_type, int64_t x_stride,
                   hipStream_t stream);
 void gnn_mlp_destroy(gnn_mlp *m); /* waits for the device; NULL-safe */
 
+/* ---- training operators ---------------------------------------------------
+ * What networks of the layers above are trained with: layer norm and its
+ * gradients, the gated feed-forward block and its gradients, and the global norm
+ * of the gradients with clipping.
+ *
+ * The rules of the row operators hold: tables are a pointer and a stride in
+ * elements, of any alignment that their elements have; up to 2^28 rows, widths
+ * 1..16384; calls run on the current device, are asynchronous on `stream`,
+ * allocate nothing and may be captured; scratch is the caller's, aligned to 256
+ * bytes, and each call in flight needs its own; outputs must not overlap inputs
+ * unless said so; results are bitwise deterministic.  GNN_E_INVALID_ARG for bad
+ * counts, types, strides, pointers or scratch; GNN_E_UNSUPPORTED for sizes beyond
+ * these; nothing is enqueued then. */
+
+/* y = gamma (x - mean) rstd + beta over each row's `width` elements, rstd = 1 /
+ * sqrt(variance + eps).  x and y of one float type; gamma, beta [width] fp32.
+ * mean and rstd [n_rows] fp32 keep what the backward pass needs (both or
+ * neither NULL).  All sums in fp32, the variance around the mean.  y may be x
+ * (with its stride). */
+int gnn_layer_norm(const void *x, int32_t type, int64_t x_stride, int64_t n_rows, int32_t width,
+                   const float *gamma, const float *beta, float eps, void *y, int64_t y_stride,
+                   float *mean, float *rstd, hipStream_t stream);
+/* The gradients from dy, of x's type: dx of that type, dgamma and dbeta [width]
+ * fp32 (zeros without rows).  dx may be dy (with its stride). */
+size_t gnn_layer_norm_workspace(int64_t n_rows, int32_t width);
+int gnn_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                            int32_t type, int64_t n_rows, int32_t width, const float *gamma,
+                            const float *mean, const float *rstd, void *dx, int64_t dx_stride,
+                            float *dgamma, float *dbeta, void *workspace, int64_t workspace_bytes,
+                            hipStream_t stream);
+
+/* A gated feed-forward block: g = W_gate x + b_gate, u = W_up x + b_up,
+ * h = act(g) u, y = W_down h + b_down.  Rows, weights and biases of one 16-bit
+ * type; products and sums in fp32; h is rounded to that type (a GNN_F16 h beyond
+ * 65504 is an infinity), and so are the gradients of h, g and u. */
+#define GNN_SILU 0
+#define GNN_GELU 1 /* g Phi(g), Phi the normal distribution (not its tanh form) */
+#define GNN_SIGMOID 2
+#define GNN_RELU 3 /* its derivative at 0 is 0                                  */
+typedef struct gnn_gated_dims {
+  uint32_t struct_size; /* = sizeof(gnn_gated_dims)                            */
+  int32_t in_features, hidden, out_features; /* 1..16384                         */
+  int32_t dtype;        /* GNN_BF16 or GNN_F16                                  */
+  int32_t activation;
+} gnn_gated_dims;
+/* Device pointers; biases may be NULL. */
+typedef struct gnn_gated_weights {
+  uint32_t struct_size;                        /* = sizeof(gnn_gated_weights)  */
+  const void *gate, *up;                       /* [hidden][in_features]        */
+  const void *down;                            /* [out_features][hidden]       */
+  const void *gate_bias, *up_bias, *down_bias; /* [hidden] twice, [out_features] */
+} gnn_gated_weights;
+/* Scratch bytes.  aligned: every table's and weight's address is a multiple of
+ * 16 bytes and every stride one of 8 elements, up to 2^21; calls on others copy
+ * them first and need what 0 gives. 0 for bad arguments. */
+size_t gnn_gated_workspace(const gnn_gated_dims *dims, int64_t n_rows, int32_t backward,
+                           int32_t aligned);
+int gnn_gated(const gnn_gated_dims *dims, const gnn_gated_weights *weights, const void *x,
+              int64_t x_stride, int64_t n_rows, void *y, int64_t y_stride, void *workspace,
+              int64_t workspace_bytes, hipStream_t stream);
+/* All gradients from dy: dx, and those of the weights, which are written (not
+ * added to) where `grads` points, laid out as the weights (zeros without rows);
+ * biases' that are NULL are left out.  g, u and h are formed again from x. */
+int gnn_gated_backward(const gnn_gated_dims *dims, const gnn_gated_weights *weights,
+                       const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
+                       int64_t n_rows, void *dx, int64_t dx_stride,
+                       const gnn_gated_weights *grads, void *workspace, int64_t workspace_bytes,
+                       hipStream_t stream);
+
+/* Gradient clipping: *norm (device, fp32) = the square root of the sum of all
+ * elements' squares, over all tensors, in fp64; out = grad min(1, max_norm /
+ * (norm + 1e-6)), which is NaN everywhere if the norm is.  out may be grad;
+ * otherwise no output may overlap another tensor (checked).  Tensors are
+ * contiguous; some may be empty.  Up to 2^37 elements in all. */
+typedef struct gnn_grad {
+  const void *grad;
+  void *out;
+  int64_t count;
+  int32_t type;     /* GNN_FP32, GNN_BF16 or GNN_F16, of grad and out          */
+  int32_t reserved;
+} gnn_grad;
+size_t gnn_clip_workspace(const gnn_grad *grads, int32_t n_grads); /* host list */
+int gnn_clip_grads(const gnn_grad *grads, int32_t n_grads, float max_norm, float *norm,
+                   void *workspace, int64_t workspace_bytes, hipStream_t stream);
+
 /* ---- serving: a request queue in front of several model instances --------
  * Paper sections 2.3 and 3.2: the GNN runs as a service, one GPU holding
  * several instances of the model (Fig. 4b) behind a queue of requests from

@@ -442,6 +442,113 @@ struct ConvertArgs {
 hipError_t launch_convert(const ConvertArgs &a, hipStream_t stream);
 hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, hipStream_t stream);
 
+// ---- training operators (gated.hip, norm.hip, clip.hip) ----
+// Products C[m][n] = sum_k A(m, k) B(n, k) of 16-bit numbers (gated.hip).
+constexpr int ACT_SILU = 0, ACT_GELU = 1, ACT_SIGMOID = 2, ACT_RELU = 3;
+// What is done with a tile: stored as rows (with a bias), or in fp32 as one of
+// several parts; h = act(g) u; h and the gradients of g and u from that of h.
+constexpr int EPI_ROWS = 0, EPI_PART = 1, EPI_GATE = 2, EPI_GRAD = 3;
+// Which product: A and B with k contiguous (GATE, GRAD, DOWN), B with k
+// outermost (ROWS), both (WEIGHTS).
+constexpr int PRODUCT_GATE = 0, PRODUCT_GRAD = 1, PRODUCT_DOWN = 2, PRODUCT_ROWS = 3,
+              PRODUCT_WEIGHTS = 4;
+constexpr int TILE_128 = 0, TILE_256x128 = 1, TILE_256 = 2;
+struct ProductArgs {
+  // Operands of one or two segments of k (GATE, GRAD: b[1] is the up projection).
+  // Addresses are multiples of 16 bytes, strides (in elements, below 2^21) and
+  // contiguous extents of 8 elements, or zeros fill up to that.
+  const void *a[2] = {nullptr, nullptr}, *b[2] = {nullptr, nullptr};
+  int64_t lda = 0, ldb = 0;
+  int64_t M = 0;
+  int32_t N = 0, K = 0, segs = 1;
+  int32_t mt = 0, nt = 0;        // tiles (set by the launch)
+  int32_t splits = 1, split_steps = INT32_MAX;
+  const void *bias[2] = {nullptr, nullptr};
+  // Rows: m < c_rows to c, the others to c2 (from row 0), each up to c_valid.
+  // GATE, GRAD: h (GRAD: it holds the gradient of h before), ldc its padded
+  // width; c2: [dg | du], 2 ldc wide.  Parts: fp32 [splits][M][ldc].
+  void *c = nullptr, *c2 = nullptr;
+  int64_t ldc = 0;
+  int64_t c_rows = INT64_MAX, c_valid = INT64_MAX;
+  float *sums = nullptr;         // GRAD: column sums [row tiles * waves of m][2 ldc]
+  int32_t act = 0;
+};
+struct ProductPlan {
+  int tile = 0;
+  int32_t splits = 1, split_steps = INT32_MAX;
+};
+ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu);
+// Rows of `sums` that a GRAD product writes.
+inline int64_t product_sum_rows(int tile, int64_t M) {
+  const int64_t tm = tile == TILE_128 ? 128 : 256;
+  return (M + tm - 1) / tm * (tile == TILE_256x128 ? 4 : 2);
+}
+hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hipStream_t stream);
+// Up to FEW_ROWS rows; operands of any alignment (GATE or DOWN).
+constexpr int FEW_ROWS = 64;
+hipError_t launch_few(const ProductArgs &a, bool gate, int type, hipStream_t stream);
+struct JoinArgs {
+  const float *part = nullptr;   // [splits][M][ldp]
+  int32_t splits = 1;
+  int64_t M = 0, ldp = 0;
+  int32_t N = 0;
+  void *c = nullptr, *c2 = nullptr;  // as in ProductArgs
+  int64_t ldc = 0, c_rows = INT64_MAX, c_valid = INT64_MAX;
+};
+hipError_t launch_join(const JoinArgs &a, int type, hipStream_t stream);
+
+// Column sums of a table (norm.hip): sums [width] of rows of any float type, to
+// up to three outputs of one type: columns [0, split) to y[0], [skip, skip +
+// split) to y[1].
+struct SumArgs {
+  const void *x = nullptr;
+  int32_t x_type = 0;
+  int64_t x_stride = 0;  // elements
+  int64_t n = 0;
+  int32_t width = 0;
+  float *part = nullptr;   // scratch, colsum_scratch bytes
+  void *y[2] = {nullptr, nullptr};
+  int32_t y_type = 0, split = 0, skip = 0;
+};
+size_t colsum_scratch(int64_t n, int32_t width);
+hipError_t launch_colsum(const SumArgs &a, hipStream_t stream);
+
+// Layer norm of rows and its gradients (norm.hip).
+struct LayerNormArgs {
+  const void *x = nullptr;
+  int32_t type = 0;       // of x, y, dy and dx
+  int64_t x_stride = 0, y_stride = 0, dy_stride = 0, dx_stride = 0;  // elements
+  int64_t n = 0;
+  int32_t width = 0;
+  float eps = 1e-5f;
+  const float *gamma = nullptr, *beta = nullptr;
+  void *y = nullptr;
+  float *mean = nullptr, *rstd = nullptr;  // written forward (may be null), read backward
+  const void *dy = nullptr;
+  void *dx = nullptr;
+  float *part = nullptr;  // [layer_norm_parts][2][width]: dgamma, dbeta
+};
+int64_t layer_norm_parts(int64_t n, int32_t width);
+hipError_t launch_layer_norm(const LayerNormArgs &a, hipStream_t stream);
+hipError_t launch_layer_norm_backward(const LayerNormArgs &a, hipStream_t stream);
+
+// Sum of squares over many tensors, and scaling (clip.hip).
+constexpr int CLIP_LIST = 96;          // tensors of a launch (its arguments stay below 4 KB)
+constexpr int64_t CLIP_TILE = 16384;   // elements of a workgroup
+struct ClipList {
+  const void *x[CLIP_LIST];
+  void *y[CLIP_LIST];
+  int64_t n[CLIP_LIST];
+  int32_t tile[CLIP_LIST + 1];  // first workgroup of each tensor; the last: their number
+  uint8_t type[CLIP_LIST];
+  int32_t count;
+};
+hipError_t launch_squares(const ClipList &l, double *part, hipStream_t stream);
+// norm <- sqrt(sum of part), scale <- min(1, max_norm / (norm + 1e-6))
+hipError_t launch_norm_scale(const double *part, int64_t n, float max_norm, float *norm,
+                             float *scale, hipStream_t stream);
+hipError_t launch_scale(const ClipList &l, const float *scale, hipStream_t stream);
+
 // flag <- 1 if any of the 2*n_edges indices lies outside [0, n_nodes).
 hipError_t launch_validate(const int32_t *edge_index, int64_t n_edges, int32_t n_nodes,
                            int32_t *flag, hipStream_t stream);

@@ -34,6 +34,10 @@ GNN_LITERAL_GATHER = 2
 GNN_FP32_MFMA = 4
 GNN_F16_WEIGHTS = 8
 GNN_PROFILE_SAMPLE = 2
+GNN_SILU = 0
+GNN_GELU = 1
+GNN_SIGMOID = 2
+GNN_RELU = 3
 
 EXPORTS = ("gnn_weight_count", "gnn_create", "gnn_infer", "gnn_infer_logits", "gnn_infer_noalloc",
            "gnn_filter_weight_count", "gnn_filter_create", "gnn_filter_apply",
@@ -48,7 +52,9 @@ EXPORTS = ("gnn_weight_count", "gnn_create", "gnn_infer", "gnn_infer_logits", "g
            "gnn_linear_weight_count", "gnn_linear_create", "gnn_linear_workspace",
            "gnn_linear_apply", "gnn_linear_destroy", "gnn_mlp_weight_count", "gnn_mlp_create",
            "gnn_mlp_workspace", "gnn_mlp_apply", "gnn_mlp_destroy", "gnn_last_error_code",
-           "gnn_debug_linear")
+           "gnn_debug_linear", "gnn_layer_norm", "gnn_layer_norm_workspace",
+           "gnn_layer_norm_backward", "gnn_gated_workspace", "gnn_gated", "gnn_gated_backward",
+           "gnn_clip_workspace", "gnn_clip_grads")
 STAGES = ("csr", "node_enc", "edge_enc", "edge_update", "aggregate", "node_update",
           "classifier", "total")
 
@@ -117,6 +123,30 @@ def make_mlp_dims(widths, n_groups=1, dtype=GNN_BF16, ln_eps=1e-5) -> gnn_mlp_di
     w = (ctypes.c_int32 * (GNN_MLP_MAX_LAYERS + 1))(*[_int32("width", v) for v in widths])
     return gnn_mlp_dims(ctypes.sizeof(gnn_mlp_dims), len(widths) - 1, w,
                         _int32("n_groups", n_groups), dtype, ln_eps)
+
+
+class gnn_gated_dims(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("in_features", ctypes.c_int32),
+                ("hidden", ctypes.c_int32), ("out_features", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
+
+
+def make_gated_dims(in_features, hidden, out_features, dtype=GNN_BF16,
+                    activation=GNN_SILU) -> gnn_gated_dims:
+    return gnn_gated_dims(ctypes.sizeof(gnn_gated_dims), _int32("in_features", in_features),
+                          _int32("hidden", hidden), _int32("out_features", out_features),
+                          dtype, activation)
+
+
+class gnn_gated_weights(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32)] + [
+        (name, ctypes.c_void_p) for name in ("gate", "up", "down", "gate_bias", "up_bias",
+                                             "down_bias")]
+
+
+class gnn_grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64),
+                ("type", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class gnn_profile_stats(ctypes.Structure):
@@ -226,6 +256,25 @@ def _load():
                                    ctypes.POINTER(ctypes.c_int32)]
     L.gnn_mlp_apply.restype = ctypes.c_int
     L.gnn_mlp_apply.argtypes = [vp, vp, i32, i64, vp, i64, vp, i32, i64, vp, i64, vp]
+    L.gnn_layer_norm.restype = ctypes.c_int
+    L.gnn_layer_norm.argtypes = [vp, i32, i64, i64, i32, vp, vp, ctypes.c_float, vp, i64, vp, vp,
+                                 vp]
+    L.gnn_layer_norm_workspace.restype = ctypes.c_size_t
+    L.gnn_layer_norm_workspace.argtypes = [i64, i32]
+    L.gnn_layer_norm_backward.restype = ctypes.c_int
+    L.gnn_layer_norm_backward.argtypes = [vp, i64, vp, i64, i32, i64, i32, vp, vp, vp, vp, i64, vp,
+                                          vp, vp, i64, vp]
+    gdp, gwp = ctypes.POINTER(gnn_gated_dims), ctypes.POINTER(gnn_gated_weights)
+    L.gnn_gated_workspace.restype = ctypes.c_size_t
+    L.gnn_gated_workspace.argtypes = [gdp, i64, i32, i32]
+    L.gnn_gated.restype = ctypes.c_int
+    L.gnn_gated.argtypes = [gdp, gwp, vp, i64, i64, vp, i64, vp, i64, vp]
+    L.gnn_gated_backward.restype = ctypes.c_int
+    L.gnn_gated_backward.argtypes = [gdp, gwp, vp, i64, vp, i64, i64, vp, i64, gwp, vp, i64, vp]
+    L.gnn_clip_workspace.restype = ctypes.c_size_t
+    L.gnn_clip_workspace.argtypes = [vp, i32]
+    L.gnn_clip_grads.restype = ctypes.c_int
+    L.gnn_clip_grads.argtypes = [vp, i32, ctypes.c_float, vp, vp, i64, vp]
     L.gnn_server_create.restype = vp
     L.gnn_server_create.argtypes = [vp, ctypes.c_int]
     L.gnn_server_submit.restype = i64
@@ -824,6 +873,208 @@ class Mlp(_RowsHandle):
         _check(lib.gnn_mlp_apply(self.handle, xa, xt, xs, ids, n, ya, yt, ys, _addr(ws), nb,
                                  _raw_stream(dev.index)))
         return out
+
+
+# ---- training operators ----
+
+_ACTIVATIONS = {"silu": GNN_SILU, "gelu": GNN_GELU, "sigmoid": GNN_SIGMOID, "relu": GNN_RELU}
+
+
+def _elsewhere(what: str, t, stream):
+    """(device of t, context to run the call in): None where the call may run as
+    it is, on the current stream of the current device."""
+    dev = _device(what, t)
+    if stream is None and dev.index == torch.cuda.current_device():
+        return dev, None
+    return dev, _on(dev, torch.cuda.current_stream(dev) if stream is None else stream)
+
+
+def _like(what: str, x: torch.Tensor, width: int, out, device):
+    """A table of x's type and number of rows, new if none is given; (table, address,
+    stride)."""
+    if out is None:
+        out = torch.empty(x.shape[0], width, dtype=x.dtype, device=device)
+        return out, out.data_ptr(), width
+    a, t, s = _rows(what, out, width, x.shape[0], device)
+    if out.dtype != x.dtype:
+        raise TypeError(f"{what}: expected {x.dtype}, got {out.dtype}")
+    return out, a, s
+
+
+def _float_rows(what: str, t, width=None, n=None, device=None):
+    a, kind, s = _rows(what, t, width, n, device)
+    if kind == GNN_INT8:
+        raise TypeError(f"{what}: expected rows of a float type")
+    return a, kind, s
+
+
+def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float = 1e-5,
+               out=None, save: bool = False, stream=None):
+    """The layer norm of x's rows, of x's type; with ``save`` (y, mean, rstd), which
+    ``layer_norm_backward`` takes.  gamma, beta: fp32.  ``out`` may be x."""
+    dev, where = _elsewhere("x", x, stream)
+    if where is not None:
+        with where:
+            return layer_norm(x, gamma, beta, eps, out, save)
+    xa, xt, xs = _float_rows("x", x, None, None, dev)
+    n, k = x.shape
+    ga = _vector("gamma", gamma, torch.float32, k, dev)
+    ba = _vector("beta", beta, torch.float32, k, dev)
+    out, ya, ys = _like("out", x, k, out, dev)
+    mean = rstd = None
+    if save:
+        mean, rstd = torch.empty(2, n, dtype=torch.float32, device=dev).unbind(0)
+    _check(lib.gnn_layer_norm(xa, xt, xs, n, k, ga, ba, eps, ya, ys, _addr(mean), _addr(rstd),
+                              _raw_stream(dev.index)))
+    return (out, mean, rstd) if save else out
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor,
+                        mean: torch.Tensor, rstd: torch.Tensor, out=None, stream=None):
+    """(dx, dgamma, dbeta) from dy and what ``layer_norm`` saved; ``out``: the dx to
+    fill, which may be dy."""
+    dev, where = _elsewhere("x", x, stream)
+    if where is not None:
+        with where:
+            return layer_norm_backward(dy, x, gamma, mean, rstd, out)
+    xa, xt, xs = _float_rows("x", x, None, None, dev)
+    n, k = x.shape
+    da, dt, ds = _float_rows("dy", dy, k, n, dev)
+    if dt != xt:
+        raise TypeError(f"dy: expected {x.dtype}, got {dy.dtype}")
+    ga = _vector("gamma", gamma, torch.float32, k, dev)
+    ma = _vector("mean", mean, torch.float32, n, dev)
+    ra = _vector("rstd", rstd, torch.float32, n, dev)
+    out, oa, os_ = _like("out", x, k, out, dev)
+    dgamma, dbeta = torch.empty(2, k, dtype=torch.float32, device=dev).unbind(0)
+    nb = lib.gnn_layer_norm_workspace(n, k)
+    ws = _scratch(nb, dev)
+    _check(lib.gnn_layer_norm_backward(da, ds, xa, xs, xt, n, k, ga, ma, ra, oa, os_,
+                                       dgamma.data_ptr(), dbeta.data_ptr(), _addr(ws), nb,
+                                       _raw_stream(dev.index)))
+    return out, dgamma, dbeta
+
+
+def _gated_args(x, w_gate, w_up, w_down, biases, activation, dev):
+    """(dims, weights, address and stride of x, whether everything is aligned)."""
+    xa, xt, xs = _rows("x", x, None, None, dev)
+    if xt not in (GNN_BF16, GNN_F16):
+        raise TypeError(f"x: rows of {x.dtype} are not supported, bfloat16 and float16 are")
+    act = _ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"activation: {activation!r} is none of {', '.join(_ACTIVATIONS)}")
+    k = x.shape[1]
+    for what, w in (("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down)):
+        if not isinstance(w, torch.Tensor) or w.dim() != 2 or w.dtype != x.dtype:
+            raise TypeError(f"{what}: expected a 2-D tensor of {x.dtype}")
+        if not w.is_contiguous() or w.device != dev:
+            raise ValueError(f"{what}: expected a contiguous tensor on {dev}")
+    hidden, n_out = w_gate.shape[0], w_down.shape[0]
+    for what, w, shape in (("w_gate", w_gate, (hidden, k)), ("w_up", w_up, (hidden, k)),
+                           ("w_down", w_down, (n_out, hidden))):
+        if tuple(w.shape) != shape:
+            raise ValueError(f"{what}: expected shape {shape}, got {tuple(w.shape)}")
+    b = (None, None, None) if biases is None else tuple(biases)
+    if len(b) != 3:
+        raise ValueError("biases: expected three, of gate, up and down (some may be None)")
+    ba = [_vector(what, v, x.dtype, n, dev) for what, v, n in
+          zip(("gate bias", "up bias", "down bias"), b, (hidden, hidden, n_out))]
+    dims = make_gated_dims(k, hidden, n_out, xt, act)
+    ptrs = (w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
+    weights = gnn_gated_weights(ctypes.sizeof(gnn_gated_weights), *ptrs, *ba)
+    return dims, weights, xa, xs, _lies_aligned(xa, xs) and all(p % 16 == 0 for p in ptrs)
+
+
+def _lies_aligned(address: int, stride: int) -> bool:
+    return address % 16 == 0 and stride % 8 == 0 and stride <= 1 << 21
+
+
+def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+          biases=None, activation: str = "silu", out=None, stream=None) -> torch.Tensor:
+    """A gated feed-forward block: act(x w_gate^T + b) * (x w_up^T + b) through w_down.
+    Rows, weights and biases (of gate, up and down) bfloat16 or float16; activation
+    "silu", "gelu", "sigmoid" or "relu"."""
+    dev, where = _elsewhere("x", x, stream)
+    if where is not None:
+        with where:
+            return gated(x, w_gate, w_up, w_down, biases, activation, out)
+    dims, weights, xa, xs, aligned = _gated_args(x, w_gate, w_up, w_down, biases, activation, dev)
+    n = x.shape[0]
+    out, ya, ys = _like("out", x, dims.out_features, out, dev)
+    nb = lib.gnn_gated_workspace(dims, n, 0, aligned)
+    ws = _scratch(nb, dev)
+    _check(lib.gnn_gated(dims, weights, xa, xs, n, ya, ys, _addr(ws), nb, _raw_stream(dev.index)))
+    return out
+
+
+def gated_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+                   w_down: torch.Tensor, biases=None, activation: str = "silu", out=None,
+                   stream=None):
+    """(dx, dw_gate, dw_up, dw_down, db_gate, db_up, db_down) of ``gated`` from dy;
+    None for biases that are None.  ``out``: the dx to fill."""
+    dev, where = _elsewhere("x", x, stream)
+    if where is not None:
+        with where:
+            return gated_backward(dy, x, w_gate, w_up, w_down, biases, activation, out)
+    dims, weights, xa, xs, aligned = _gated_args(x, w_gate, w_up, w_down, biases, activation, dev)
+    n = x.shape[0]
+    da, dt, ds = _rows("dy", dy, dims.out_features, n, dev)
+    if dt != dims.dtype:
+        raise TypeError(f"dy: expected {x.dtype}, got {dy.dtype}")
+    out, oa, os_ = _like("out", x, dims.in_features, out, dev)
+    grads = [torch.empty_like(w) for w in (w_gate, w_up, w_down)]
+    grads += [None if b is None else torch.empty_like(b)
+              for b in (biases if biases is not None else (None, None, None))]
+    into = gnn_gated_weights(ctypes.sizeof(gnn_gated_weights), *map(_addr, grads))
+    nb = lib.gnn_gated_workspace(dims, n, 1, aligned and _lies_aligned(da, ds))
+    ws = _scratch(nb, dev)
+    _check(lib.gnn_gated_backward(dims, weights, da, ds, xa, xs, n, oa, os_, into, _addr(ws), nb,
+                                  _raw_stream(dev.index)))
+    return (out, *grads)
+
+
+_GRAD = np.dtype([("grad", np.uint64), ("out", np.uint64), ("count", np.int64),
+                  ("type", np.int32), ("reserved", np.int32)])
+
+
+def clip_grads(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
+    """The global norm of the gradients (a 0-dim fp32 tensor on their device), which
+    are scaled by min(1, max_norm / (norm + 1e-6)): in place, or into ``out``, a
+    tensor of the same size and type for each.  Contiguous fp32, bfloat16 and
+    float16 tensors, side by side in any mixture."""
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if not grads:
+        raise ValueError("grads: expected one tensor at least")
+    dev, where = _elsewhere("grads", grads[0], stream)
+    if where is not None:
+        with where:
+            return clip_grads(grads, max_norm, out)
+    if len(out) != len(grads):
+        raise ValueError(f"out: {len(out)} tensors, expected {len(grads)}")
+    for what, ts in (("grads", grads), ("out", out)) if out is not grads else (("grads", grads),):
+        for t in ts:
+            if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES or t.dtype == torch.int8:
+                raise TypeError(f"{what}: expected float32, bfloat16 and float16 tensors")
+            if not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"{what}: expected contiguous tensors on {dev}")
+    table = np.zeros(len(grads), _GRAD)
+    table["grad"] = [t.data_ptr() for t in grads]
+    table["count"] = counts = [t.numel() for t in grads]
+    kinds = [t.dtype for t in grads]
+    table["type"] = [_TYPES[k] for k in kinds]
+    if out is grads:
+        table["out"] = table["grad"]
+    else:
+        if [t.numel() for t in out] != counts or [t.dtype for t in out] != kinds:
+            raise ValueError("out: expected tensors of the gradients' sizes and types")
+        table["out"] = [t.data_ptr() for t in out]
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    nb = lib.gnn_clip_workspace(table.ctypes.data, len(grads))
+    ws = _scratch(nb, dev)
+    _check(lib.gnn_clip_grads(table.ctypes.data, len(grads), max_norm, norm.data_ptr(), _addr(ws),
+                              nb, _raw_stream(dev.index)))
+    return norm
 
 
 def gnn_server_create(handle, n_instances: int):

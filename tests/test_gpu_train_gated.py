@@ -1,0 +1,188 @@
+"""The gated block and its gradients on the GPU against their 64-bit forms."""
+import pytest
+import torch
+
+from tests import train_ref as R
+
+pytestmark = pytest.mark.gpu
+KINDS = {"bf16": torch.bfloat16, "f16": torch.float16}
+ACTS = ["silu", "gelu", "sigmoid", "relu"]
+
+
+@pytest.fixture(scope="module")
+def G():
+    from paper_2402_09633_amd import gnn
+    return gnn
+
+
+def make(m, k, h, n, kind, seed, bias=True, scale=1.0):
+    """(x, weights, biases, dy)"""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def rand(*shape, by=1.0):
+        return (torch.randn(*shape, device="cuda", generator=g) * by).to(kind)
+
+    w = [rand(h, k, by=k ** -0.5), rand(h, k, by=k ** -0.5), rand(n, h, by=h ** -0.5)]
+    b = [rand(h, by=0.3), rand(h, by=0.3), rand(n, by=0.3)] if bias else [None] * 3
+    return rand(m, k, by=scale), w, b, rand(m, n)
+
+
+def wider(t, pitch, first=0):
+    big = torch.full((t.shape[0], pitch), 7.0, dtype=t.dtype, device=t.device)
+    big[:, first:first + t.shape[1]] = t
+    return big[:, first:first + t.shape[1]]
+
+
+def check(G, x, w, b, dy, act, backward=True):
+    biases = None if b[0] is None and b[2] is None else b
+    y = G.gated(x, *w, biases=biases, activation=act)
+    R.within(y, *R.gated(x, w, b, act))
+    if not backward:
+        return y, None
+    got = G.gated_backward(dy, x, *w, biases=biases, activation=act)
+    for i, (have, (v, e)) in enumerate(zip(got, R.gated_backward(dy, x, w, b, act))):
+        if have is not None:
+            R.within(have, v, e)
+    return y, got
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("m", [1, 2, 15, 16, 17, 33, 48, 63, 64, 65, 127, 128, 129, 300])
+def test_rows(G, m, kind):
+    check(G, *make(m, 72, 104, 40, KINDS[kind], m), "silu")
+    check(G, *make(m, 37, 75, 29, KINDS[kind], m), "gelu")
+
+
+@pytest.mark.parametrize("m", [5, 70])
+@pytest.mark.parametrize("k,h,n", [
+    (1, 1, 1), (8, 8, 8), (3, 200, 5), (7, 9, 300), (64, 64, 64), (65, 63, 66), (128, 256, 128),
+    (129, 257, 127), (200, 24, 136), (391, 131, 259), (512, 72, 8), (8, 520, 264)])
+def test_widths(G, m, k, h, n):
+    for kind in KINDS.values():
+        check(G, *make(m, k, h, n, kind, k + h), "silu")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("act", ACTS)
+def test_activations(G, act, kind):
+    for m in (40, 200):
+        check(G, *make(m, 96, 80, 64, KINDS[kind], 1, scale=3.0), act)
+        check(G, *make(m, 96, 80, 64, KINDS[kind], 2, bias=False), act)
+
+
+# Sizes that reach the wide tiles, whole and with an end in either direction, and
+# sums over rows in several parts.
+@pytest.mark.parametrize("m,k,h,n", [
+    (2048, 512, 1024, 512), (2049, 264, 1032, 1048), (20_000, 128, 256, 128), (9001, 65, 130, 259),
+    (513, 1600, 2048, 1304), (300, 2048, 512, 4096), (33_000, 40, 24, 16)])
+def test_large(G, m, k, h, n):
+    check(G, *make(m, k, h, n, torch.float16, m), "silu")
+
+
+def test_many_rows(G):
+    check(G, *make(300_001, 32, 64, 32, torch.bfloat16, 1), "gelu")
+
+
+@pytest.mark.parametrize("m", [20, 150])
+def test_some_biases(G, m):
+    x, w, b, dy = make(m, 48, 56, 64, torch.float16, 3)
+    for keep in ((True, False, False), (False, True, False), (False, False, True)):
+        some = [v if on else None for v, on in zip(b, keep)]
+        y = G.gated(x, *w, biases=some)
+        R.within(y, *R.gated(x, w, some, "silu"))
+        got = G.gated_backward(dy, x, *w, biases=some)
+        want = R.gated_backward(dy, x, w, some, "silu")
+        for have, (v, e), on in zip(got, want, (True,) * 4 + keep):
+            assert (have is not None) == on
+            if on:
+                R.within(have, v, e)
+
+
+@pytest.mark.parametrize("m", [9, 140])
+@pytest.mark.parametrize("k,h,n,px,pd", [(64, 64, 64, 72, 80), (64, 64, 64, 65, 67),
+                                         (33, 40, 35, 40, 43), (128, 72, 24, 128, 25)])
+def test_strides(G, m, k, h, n, px, pd):
+    x, w, b, dy = make(m + 1, k, h, n, torch.bfloat16, 4)
+    plain = check(G, x[1:].clone(), w, b, dy[1:].clone(), "silu")
+    x, dy = wider(x, px)[1:], wider(dy, pd)[1:]
+    y, got = check(G, x, w, b, dy, "silu")
+    assert torch.equal(y, plain[0])
+    assert all(torch.equal(p, q) for p, q in zip(got, plain[1]))
+    out = torch.full((m, pd), 5.0, dtype=x.dtype, device="cuda")
+    assert torch.equal(G.gated(x, *w, biases=b, out=out[:, :n]), y) and (out[:, n:] == 5).all()
+    out = torch.full((m, px), 5.0, dtype=x.dtype, device="cuda")
+    dx = G.gated_backward(dy, x, *w, biases=b, out=out[:, :k])[0]
+    assert torch.equal(dx, got[0]) and (out[:, k:] == 5).all()
+
+
+def test_weights_at_any_element(G):
+    """Weights and biases that start at odd elements of a larger buffer."""
+    x, w, b, dy = make(200, 64, 72, 80, torch.float16, 5)
+    y, got = check(G, x, w, b, dy, "silu")
+
+    def moved(t):
+        flat = torch.zeros(t.numel() + 3, dtype=t.dtype, device="cuda")
+        flat[3:] = t.flatten()
+        return flat[3:].view(t.shape)
+
+    w2, b2 = [moved(t) for t in w], [moved(t) for t in b]
+    assert torch.equal(G.gated(x, *w2, biases=b2), y)
+    assert all(torch.equal(p, q) for p, q in zip(G.gated_backward(dy, x, *w2, biases=b2), got))
+
+
+@pytest.mark.parametrize("m", [30, 170])
+@pytest.mark.parametrize("k,h,n", [(64, 64, 64), (35, 43, 27)])
+def test_bad_rows_keep_to_themselves(G, m, k, h, n):
+    """A NaN or infinity in a row is in no other row's result; what lies between
+    rows is not read at all."""
+    x, w, b, dy = make(m, k, h, n, torch.bfloat16, 6)
+    x, dy = wider(x, k + 9), wider(dy, n + 7)
+    y, got = check(G, x, w, b, dy, "silu")
+    for t in (x, dy):
+        t._base[:, t.shape[1]:] = float("nan")
+    assert torch.equal(G.gated(x, *w, biases=b), y)
+    assert all(torch.equal(p, q) for p, q in zip(G.gated_backward(dy, x, *w, biases=b), got))
+    x[3, k - 1], x[m - 1, 0] = float("nan"), float("inf")
+    y2, got2 = G.gated(x, *w, biases=b), G.gated_backward(dy, x, *w, biases=b)
+    good = torch.ones(m, dtype=torch.bool, device="cuda")
+    good[[3, m - 1]] = False
+    assert torch.equal(y2[good], y[good]) and torch.equal(got2[0][good], got[0][good])
+    assert y2[3].isnan().all() and not y2[m - 1].isfinite().all()
+    assert got2[1].isnan().any()
+
+
+def test_no_rows(G):
+    x, w, b, dy = make(0, 24, 35, 16, torch.float16, 7)
+    assert G.gated(x, *w, biases=b).shape == (0, 16)
+    dx, *grads = G.gated_backward(dy, x, *w, biases=b)
+    assert dx.shape == (0, 24)
+    assert all((g == 0).all() and g.shape == t.shape for g, t in zip(grads, w + b))
+
+
+def test_same_bits_every_time(G):
+    a = make(20_000, 136, 264, 72, torch.bfloat16, 8)
+    one, two = (check(G, *a, "gelu") for _ in range(2))
+    assert torch.equal(one[0], two[0])
+    assert all(torch.equal(p, q) for p, q in zip(one[1], two[1]))
+
+
+def test_gradients_are_the_forward_passes_slope(G):
+    """Differences of the 64-bit forward pass, along a step in every input."""
+    x, w, b, dy = make(90, 24, 40, 16, torch.float16, 9)
+    grads = G.gated_backward(dy, x, *w, biases=b)
+    bounds = R.gated_backward(dy, x, w, b, "silu")
+    leaves = [x, *w, *b]
+    for i, (leaf, grad, (want, e)) in enumerate(zip(leaves, grads, bounds)):
+        g = torch.Generator(device="cuda").manual_seed(i)
+        way = torch.randn(leaf.shape, device="cuda", generator=g).double()
+
+        def loss(t):
+            at = [v.double() for v in leaves]
+            at[i] = at[i] + t * way
+            gate, up = at[0] @ at[1].t() + at[4], at[0] @ at[2].t() + at[5]
+            return float((((gate * torch.sigmoid(gate)) * up) @ at[3].t() + at[6]).mul(dy.double()).sum())
+
+        t = 1e-5
+        slope = (loss(t) - loss(-t)) / (2 * t)
+        limit = float((R.stored(want, e, torch.float16) * way.abs()).sum()) + 1e-5
+        assert abs(float((grad.double() * way).sum()) - slope) <= limit
