@@ -87,12 +87,17 @@ __device__ __forceinline__ void stage_barrier() {
 // k contiguous: rows of 128 bytes, whose eight 16-byte pieces are exchanged by
 // the row's number, piece c of row r at c ^ (r & 7), so that the 16 rows that a
 // read touches spread over all banks.
-// k outermost: BK rows of R numbers, whose 32-byte units are exchanged by f(k) =
-// k & 3 | (k >> 3 & 1) << 2: a transposing read takes one unit from each of
-// eight k at a time, which differ in f.
+// k outermost: BK rows of R numbers, whose 32-byte units are exchanged by f(k): a
+// transposing read takes one unit from each of eight k at a time (k & 3 and k >> 3
+// & 1 differ), which then lie in different banks; of R = 64 two rows fill the
+// banks, and their place tells k & 1 apart.
+template <int R>
+__device__ __forceinline__ int unit_of(int k) {
+  return R == 64 ? ((k >> 1) & 1) | ((k >> 3) & 1) << 1 : (k & 3) | ((k >> 3) & 1) << 2;
+}
 template <int R, int NW, bool KS>
 struct Staged {
-  static constexpr int BYTES = R * BK * 2, LOADS = BYTES / 1024 / NW;
+  static constexpr int WIDTH = R, BYTES = R * BK * 2, LOADS = BYTES / 1024 / NW;
   uint32_t off[LOADS];  // a lane's offsets from the stage's first element
 
   // ext: how many of the R lie in the operand (a multiple of 8 with KS)
@@ -105,12 +110,11 @@ struct Staged {
         off[i] = row < ext ? (uint32_t)(row * (int32_t)ld * 2 + c * 16) : OUTSIDE;
       } else {
         const int at = q * 1024 + lane * 16, k = at / (R * 2), p = at % (R * 2);
-        const int col = (((p >> 5) ^ f(k)) << 4) + ((p >> 4) & 1) * 8;
+        const int col = (((p >> 5) ^ unit_of<R>(k)) << 4) + ((p >> 4) & 1) * 8;
         off[i] = col < ext ? (uint32_t)(k * (int32_t)ld * 2 + col * 2) : OUTSIDE;
       }
     }
   }
-  static __device__ __forceinline__ int f(int k) { return (k & 3) | ((k >> 3) & 1) << 2; }
 
   // left: how many k there are from the stage's first on
   __device__ __forceinline__ void issue(uint32_t lds, const i4 &buf, int wave, int lane,
@@ -142,8 +146,8 @@ struct Frag {
       at = (first + i) * 128;
       x = g ^ (i & 7);
     } else {
-      const int fk = (i >> 2) | (g & 1) << 2;
-      at = (g * 8 + (i >> 2)) * (R * 2) + (((first >> 4) ^ fk) << 5) + (i & 3) * 8;
+      const int k = g * 8 + (i >> 2);
+      at = k * (R * 2) + (((first >> 4) ^ unit_of<R>(k)) << 5) + (i & 3) * 8;
       x = 0;
     }
   }
@@ -187,7 +191,9 @@ __device__ __forceinline__ f4 load4(const elem_t<T> *p, int32_t n) {
 // WM x WN waves, each with MI x NI blocks of 16 x 16.  The n are the MFMA's
 // first operand, so that a lane holds four neighbouring n of one m.
 // GATE and GRAD: B is the gate's and the up projection's rows in turn, 16 NI / 2 of
-// each to a wave, so that a wave has g and u of the same elements.
+// each to a wave, so that a wave has g and u of the same elements.  GRAD goes on
+// with dh = dy Wd (k outermost) of these elements in registers of its own: dh is
+// never rounded, nor in memory.
 template <int T, int WM, int WN, int MI, int NI, bool AKS, bool BKS, int EPI>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) {
   constexpr int NW = WM * WN, TM = WM * MI * 16, TN = WN * NI * 16;
@@ -215,6 +221,15 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
 
   SA sa;
   SB sb;
+  // the third product's operands
+  typedef Staged<EPI == EPI_GRAD ? CN : 128, NW, true> SD;
+  static_assert(SD::BYTES <= SB::BYTES || EPI != EPI_GRAD, "its stages take the others' place");
+  SA sy;
+  SD sd;
+  if constexpr (EPI == EPI_GRAD) {
+    sy.init(wave, lane, a.lda2, (int32_t)min((int64_t)TM, a.M - m0));
+    sd.init(wave, lane, a.ldb2, min(CN, a.N - n0));
+  }
   sa.init(wave, lane, a.lda, (int32_t)min((int64_t)TM, a.M - m0));
   if constexpr (DUAL) {
     // stage row r: part (r / U) & 1 of column n0 + r / (2 U) * U + r % U
@@ -229,7 +244,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
     sb.init(wave, lane, a.ldb, min(TN, a.N - n0));
   }
 
-  const int32_t seg_steps = (a.K + BK - 1) / BK, steps = seg_steps * a.segs;
+  const int32_t seg_steps = (a.K + BK - 1) / BK;
+  const int32_t steps = EPI == EPI_GRAD ? seg_steps + (a.K2 + BK - 1) / BK : seg_steps * a.segs;
   const int32_t first = (int32_t)min((int64_t)steps, (int64_t)split * a.split_steps);
   const int32_t end = (int32_t)min((int64_t)steps, (int64_t)first + a.split_steps);
 
@@ -237,6 +253,14 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
     const int32_t seg = step >= seg_steps ? 1 : 0, k = (step - seg * seg_steps) * BK;
     const int32_t left = a.K - k;
     const uint32_t to = lds + buf * STAGE;
+    if constexpr (EPI == EPI_GRAD) {
+      if (seg) {
+        sy.issue(to, buffer_of((const E *)a.a[1] + m0 * a.lda2 + k), wave, lane, a.K2 - k);
+        sd.issue(to + SA::BYTES, buffer_of((const E *)a.b2 + k * a.ldb2 + n0), wave, lane,
+                 a.K2 - k);
+        return;
+      }
+    }
     const E *pa = (const E *)a.a[seg] + (AKS ? k * a.lda + m0 : m0 * a.lda + k);
     sa.issue(to, buffer_of(pa), wave, lane, left);
     if constexpr (DUAL) {
@@ -264,8 +288,11 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
+  constexpr int HN = NI / 2;
+  f4 third[EPI == EPI_GRAD ? MI : 1][EPI == EPI_GRAD ? HN : 1];
+  const int32_t end1 = EPI == EPI_GRAD ? seg_steps : end;
   if (first < end) issue(first, 0);
-  for (int32_t step = first; step < end; ++step) {
+  for (int32_t step = first; step < end1; ++step) {
     const int buf = (step - first) & 1;
     stage_barrier();
     if (step + 1 < end) issue(step + 1, buf ^ 1);
@@ -283,13 +310,38 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
         for (int j = 0; j < NI; ++j) acc[i][j] = mfma16<T>(xb[j], xa[i], acc[i][j]);
     }
   }
+  if constexpr (EPI == EPI_GRAD) {
+    Frag<SD::WIDTH, true> fd;
+    fd.init(wn * HN * 16, lane);
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+      for (int j = 0; j < HN; ++j) third[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+    for (int32_t step = end1; step < end; ++step) {
+      const int buf = step & 1;
+      stage_barrier();
+      if (step + 1 < end) issue(step + 1, buf ^ 1);
+      const uint32_t la = lds + buf * STAGE, lb = la + SA::BYTES;
+#pragma unroll
+      for (int s = 0; s < BK / 32; ++s) {
+        s8v xb[HN], xa[MI];
+#pragma unroll
+        for (int j = 0; j < HN; ++j) xb[j] = fd.load(lb, j, s);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) xa[i] = fa.load(la, i, s);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < HN; ++j) third[i][j] = mfma16<T>(xb[j], xa[i], third[i][j]);
+      }
+    }
+  }
 
   // A lane's part of block (i, j): row mrow(i), columns 4 (lane / 16) .. + 3 of
   // the block's.
   const int li = lane & 15, lg = lane >> 4;
   const int64_t mw = m0 + wm * MI * 16 + li;
   if constexpr (DUAL) {
-    constexpr int HN = NI / 2;
     const int32_t c0 = n0 + wn * HN * 16 + lg * 4;
     f4 bg[HN], bu[HN], sg[HN], su[HN];
 #pragma unroll
@@ -314,8 +366,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
             for (int v = 0; v < 4; ++v) h[v] = activate<false>(a.act, g[v], nullptr) * u[v];
             store4<T>(ph, h, 4, true);
           } else {
-            typedef E e4 __attribute__((ext_vector_type(4)));
-            const f4 dh = __builtin_convertvector(*(const e4 *)ph, f4);
+            const f4 dh = third[i][j];
             f4 dg, du;
 #pragma unroll
             for (int v = 0; v < 4; ++v) {

@@ -446,10 +446,10 @@ hipError_t launch_linear(const LinearArgs &a, const LinearPlan &p, hipStream_t s
 // Products C[m][n] = sum_k A(m, k) B(n, k) of 16-bit numbers (gated.hip).
 constexpr int ACT_SILU = 0, ACT_GELU = 1, ACT_SIGMOID = 2, ACT_RELU = 3;
 // What is done with a tile: stored as rows (with a bias), or in fp32 as one of
-// several parts; h = act(g) u; h and the gradients of g and u from that of h.
+// several parts; h = act(g) u; h and the gradients of g and u.
 constexpr int EPI_ROWS = 0, EPI_PART = 1, EPI_GATE = 2, EPI_GRAD = 3;
-// Which product: A and B with k contiguous (GATE, GRAD, DOWN), B with k
-// outermost (ROWS), both (WEIGHTS).
+// Which product: A and B with k contiguous (GATE, GRAD but for its third, DOWN), B
+// with k outermost (ROWS), both (WEIGHTS).
 constexpr int PRODUCT_GATE = 0, PRODUCT_GRAD = 1, PRODUCT_DOWN = 2, PRODUCT_ROWS = 3,
               PRODUCT_WEIGHTS = 4;
 constexpr int TILE_128 = 0, TILE_256x128 = 1, TILE_256 = 2;
@@ -459,14 +459,18 @@ struct ProductArgs {
   // contiguous extents of 8 elements, or zeros fill up to that.
   const void *a[2] = {nullptr, nullptr}, *b[2] = {nullptr, nullptr};
   int64_t lda = 0, ldb = 0;
+  // GRAD: a[1] is dy (stride lda2) and b2 the down projection [K2][N], whose
+  // product is the gradient of h
+  const void *b2 = nullptr;
+  int64_t lda2 = 0, ldb2 = 0;
+  int32_t K2 = 0;
   int64_t M = 0;
   int32_t N = 0, K = 0, segs = 1;
   int32_t mt = 0, nt = 0;        // tiles (set by the launch)
   int32_t splits = 1, split_steps = INT32_MAX;
   const void *bias[2] = {nullptr, nullptr};
   // Rows: m < c_rows to c, the others to c2 (from row 0), each up to c_valid.
-  // GATE, GRAD: h (GRAD: it holds the gradient of h before), ldc its padded
-  // width; c2: [dg | du], 2 ldc wide.  Parts: fp32 [splits][M][ldc].
+  // GATE, GRAD: h, ldc its padded width; GRAD's c2: [dg | du], 2 ldc wide.  Parts: fp32 [splits][M][ldc].
   void *c = nullptr, *c2 = nullptr;
   int64_t ldc = 0;
   int64_t c_rows = INT64_MAX, c_valid = INT64_MAX;

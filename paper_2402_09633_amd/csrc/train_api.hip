@@ -304,7 +304,7 @@ struct GatedForward {
 
 struct GatedBackward {
   Operand x, dy, gate, up, down;
-  ProductPlan dh, grad, dx, dgu, dd;
+  ProductPlan grad, dx, dgu, dd;
   size_t h = 0, g = 0, part = 0, sums = 0, colsum = 0;
   int64_t sum_rows = 0;
   Carve c;
@@ -317,7 +317,6 @@ struct GatedBackward {
         down(w ? w->down : nullptr, d.hidden, d.out_features, d.hidden, w_in) {
     const int64_t hp = up8(d.hidden), kp = up8(d.in_features);
     for (Operand *o : {&x, &dy, &gate, &up, &down}) o->place(c);
-    dh = product_plan(PRODUCT_ROWS, n, hp, d.out_features, n_cu);
     grad = product_plan(PRODUCT_GRAD, n, d.hidden, d.in_features, n_cu);
     dx = product_plan(PRODUCT_ROWS, n, d.in_features, 2 * hp, n_cu);
     dgu = product_plan(PRODUCT_WEIGHTS, 2 * hp, d.in_features, n, n_cu);
@@ -443,23 +442,15 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     if ((rc = o->fetch(ws, t, stream))) return rc;
   void *h = ws + f.h, *g = ws + f.g;
   if (n_rows > 0) {
-    // dh = dy Wd, rounded to the rows' type where h will lie
-    ProductArgs a;
-    a.a[0] = f.dy.p;
-    a.lda = f.dy.stride;
-    a.b[0] = f.down.p;
-    a.ldb = f.down.stride;
-    a.M = n_rows;
-    a.N = (int32_t)hp;
-    a.K = d->out_features;
-    a.c = h;
-    a.ldc = hp;
-    if ((rc = launched(launch_product(a, PRODUCT_ROWS, t, f.dh.tile, stream), "gradient of h")))
-      return rc;
-    // g and u again; h, dg and du
+    // g and u again, and dh; from them h, dg and du
     ProductArgs b;
     b.a[0] = f.x.p;
+    b.a[1] = f.dy.p;
     b.lda = f.x.stride;
+    b.lda2 = f.dy.stride;
+    b.b2 = f.down.p;
+    b.ldb2 = f.down.stride;
+    b.K2 = d->out_features;
     b.b[0] = f.gate.p;
     b.b[1] = f.up.p;
     b.ldb = f.gate.stride;

@@ -151,7 +151,7 @@ def gated_backward(dy, x, w, b, name):
     h = a * u
     eh = _half(h, a.abs() * eu + u.abs() * e_a + e_a * eu + 2 * U * h.abs(), kind)
     dh = _mm(dy, wd)
-    edh = _half(dh, (dy.shape[1] + 2) * 2 * U * _mm(dy.abs(), wd.abs()), kind)
+    edh = (dy.shape[1] + 2) * 2 * U * _mm(dy.abs(), wd.abs())
     dh_ = dh.abs() + edh
     dg, du = dh * u * slope, dh * a
     edg0 = edh * (u * slope).abs() + dh_ * (slope.abs() * eu + (u.abs() + eu) * e_s) + \
