@@ -8,6 +8,9 @@
 // backward pass, and everything of the weights' gradients, whose k are the
 // rows).  The former goes to the matrix cores by 16-byte LDS reads, the latter
 // by LDS reads that transpose 4 x 16 numbers: no operand is transposed in memory.
+#include <type_traits>
+#include <utility>
+
 #include "rows_common.h"
 
 namespace gnn {
@@ -68,9 +71,10 @@ __device__ __forceinline__ float activate(int act, float g, float *slope) {
 // and 1 KB a wave's load.  The load is written in assembly because the compiler
 // would let every LDS read wait for it; the stage's own wait stands before the
 // barrier that ends a stage.
-__device__ __forceinline__ i4 buffer_of(const void *p) {
+// `on` false: nothing lies in range, so that a load only clears its place.
+__device__ __forceinline__ i4 buffer_of(const void *p, bool on) {
   const uint64_t a = (uint64_t)p;
-  return i4{(int32_t)a, (int32_t)(a >> 32), (int32_t)OUTSIDE, 0x00020000};
+  return i4{(int32_t)a, (int32_t)(a >> 32) & 0xffff, on ? (int32_t)OUTSIDE : 0, 0x00020000};
 }
 __device__ __forceinline__ void load_lds(uint32_t lds, uint32_t off, const i4 &buf) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
@@ -78,8 +82,12 @@ __device__ __forceinline__ void load_lds(uint32_t lds, uint32_t off, const i4 &b
                : "s"(lds), "v"(off), "s"(buf)
                : "memory");
 }
+// All but the last N loads of this wave have come, and all waves are here.
+template <int N>
 __device__ __forceinline__ void stage_barrier() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // One operand's part of a stage: R (m or n) by BK.
@@ -116,21 +124,11 @@ struct Staged {
     }
   }
 
-  // left: how many k there are from the stage's first on
-  __device__ __forceinline__ void issue(uint32_t lds, const i4 &buf, int wave, int lane,
-                                        int32_t left) const {
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) issue1(i, lds, buf, wave, lane, left);
-  }
-  __device__ __forceinline__ void issue1(int i, uint32_t lds, const i4 &buf, int wave, int lane,
-                                         int32_t left) const {
-    uint32_t o = off[i];
-    if (left < BK) {
-      const int k = KS ? ((wave * LOADS + i) * 1024 + lane * 16) / (R * 2)
-                       : ((lane & 7) ^ (lane >> 3)) * 8;
-      if (k >= left) o = OUTSIDE;
-    }
-    load_lds(lds + (wave * LOADS + i) * 1024, o, buf);
+  // Load i of a stage from whose first k on there are `left`.
+  __device__ __forceinline__ uint32_t from(int i, int wave, int lane, int32_t left) const {
+    const int k = KS ? ((wave * LOADS + i) * 1024 + lane * 16) / (R * 2)
+                     : ((lane & 7) ^ (lane >> 3)) * 8;
+    return k < left ? off[i] : OUTSIDE;
   }
 };
 
@@ -188,14 +186,57 @@ __device__ __forceinline__ f4 load4(const elem_t<T> *p, int32_t n) {
 }
 
 // ---- the product ----
+// Half a stage (k of one MFMA) of a wave's blocks, while the operands of the next
+// half come from LDS and, in every second half, a stage from memory: loads stand
+// between the MFMAs in the order in which they are written here, so that the
+// matrix cores never wait for a run of them.
+template <int N, typename F, int... Q>
+__device__ __forceinline__ void each(F &&f, std::integer_sequence<int, Q...>) {
+  (f(std::integral_constant<int, Q>{}), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F &&f) {
+  each<N>(f, std::make_integer_sequence<int, N>{});
+}
+
+template <int T, int MI, int NI, int D, typename LA, typename LB, typename DMA>
+__device__ __forceinline__ void half_stage(f4 (&acc)[MI][NI], const s8v (&xa)[MI],
+                                           const s8v (&xb)[NI], s8v (&ya)[MI], s8v (&yb)[NI],
+                                           LA &&load_a, LB &&load_b, DMA &&dma) {
+  constexpr int MF = MI * NI, R = MI + NI;
+  each<MF>([&](auto at) {
+    constexpr int q = at.value, i = q % MI, j = q / MI;
+    // reads in the order in which the MFMAs need them, done by three quarters
+    constexpr int r0 = (4 * R * q + 3 * MF - 1) / (3 * MF), r1 = (4 * R * (q + 1) + 3 * MF - 1) / (3 * MF);
+    each<(r1 < R ? r1 : R) - (r0 < R ? r0 : R)>([&](auto n) {
+      constexpr int r = r0 + n.value;
+      if constexpr (r == 0)
+        yb[0] = load_b(0);
+      else if constexpr (r <= MI)
+        ya[r - 1] = load_a(r - 1);
+      else
+        yb[r - MI] = load_b(r - MI);
+    });
+    constexpr int d0 = (D * q + MF - 1) / MF, d1 = (D * (q + 1) + MF - 1) / MF;
+    each<d1 - d0>([&](auto n) { dma(d0 + n.value); });
+    acc[i][j] = mfma16<T>(xb[j], xa[i], acc[i][j]);
+    if constexpr (d1 > d0 || (r1 > r0 && r0 < R)) __builtin_amdgcn_sched_barrier(0);
+  });
+}
+
 // WM x WN waves, each with MI x NI blocks of 16 x 16.  The n are the MFMA's
-// first operand, so that a lane holds four neighbouring n of one m.
+// first operand, so that a lane holds four neighbouring n of one m.  S stages lie
+// in LDS; a stage's place is filled again as soon as its second half is in
+// registers, so that memory has S - 1/2 stages' time.  Where two waves share a SIMD
+// and their sums leave no room for two halves' operands (!AHEAD), a half's operands
+// are read just before it, and the other wave's MFMAs cover that.
 // GATE and GRAD: B is the gate's and the up projection's rows in turn, 16 NI / 2 of
 // each to a wave, so that a wave has g and u of the same elements.  GRAD goes on
 // with dh = dy Wd (k outermost) of these elements in registers of its own: dh is
 // never rounded, nor in memory.
-template <int T, int WM, int WN, int MI, int NI, bool AKS, bool BKS, int EPI>
-__global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) {
+template <int T, int WM, int WN, int MI, int NI, int S, bool AKS, bool BKS, int EPI>
+__global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 && (MI * NI > 16 || S > 2) ? 1 : 2) void
+gated_product(ProductArgs a) {
   constexpr int NW = WM * WN, TM = WM * MI * 16, TN = WN * NI * 16;
   constexpr bool DUAL = EPI == EPI_GATE || EPI == EPI_GRAD;
   constexpr int CN = DUAL ? TN / 2 : TN;  // columns of C in a tile
@@ -203,6 +244,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
   typedef Staged<TN, NW, BKS> SB;
   constexpr int STAGE = SA::BYTES + SB::BYTES;
   typedef elem_t<T> E;
+  constexpr bool AHEAD = !(NW == 8 && MI * NI >= 32 && EPI == EPI_GRAD);
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)shared;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -249,31 +291,55 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
   const int32_t first = (int32_t)min((int64_t)steps, (int64_t)split * a.split_steps);
   const int32_t end = (int32_t)min((int64_t)steps, (int64_t)first + a.split_steps);
 
-  auto issue = [&](int32_t step, int buf) {
-    const int32_t seg = step >= seg_steps ? 1 : 0, k = (step - seg * seg_steps) * BK;
-    const int32_t left = a.K - k;
-    const uint32_t to = lds + buf * STAGE;
-    if constexpr (EPI == EPI_GRAD) {
-      if (seg) {
-        sy.issue(to, buffer_of((const E *)a.a[1] + m0 * a.lda2 + k), wave, lane, a.K2 - k);
-        sd.issue(to + SA::BYTES, buffer_of((const E *)a.b2 + k * a.ldb2 + n0), wave, lane,
-                 a.K2 - k);
-        return;
-      }
+  // A stage on its way.
+  struct Coming {
+    i4 a, b, b2;
+    int32_t left;
+    uint32_t to;
+    bool second;  // of GRAD's third product
+  };
+  constexpr int LOADS = SA::LOADS + SB::LOADS;
+  auto coming = [&](int32_t step, uint32_t to) {
+    Coming c;
+    const bool on = step < end, seg = step >= seg_steps;
+    const int32_t k = (step - (seg ? seg_steps : 0)) * BK;
+    c.to = to;
+    c.second = EPI == EPI_GRAD && seg;
+    c.left = (c.second ? a.K2 : a.K) - k;
+    const E *pa = (const E *)a.a[seg ? 1 : 0], *pb = (const E *)a.b[!DUAL && seg ? 1 : 0];
+    const int64_t lda = c.second ? a.lda2 : a.lda;
+    c.a = buffer_of(pa + (AKS ? k * lda + m0 : m0 * lda + k), on);
+    c.b = buffer_of(pb + (BKS ? k * a.ldb + n0 : n0 * a.ldb + k), on);
+    if constexpr (DUAL) c.b2 = buffer_of((const E *)a.b[1] + n0 * a.ldb + k, on);
+    if (EPI == EPI_GRAD && c.second) c.b = buffer_of((const E *)a.b2 + k * a.ldb2 + n0, on);
+    return c;
+  };
+  auto load = [&](int i, const Coming &c) {
+    if (i < SA::LOADS) {
+      uint32_t o = sa.from(i, wave, lane, c.left);
+      if constexpr (EPI == EPI_GRAD) o = c.second ? sy.from(i, wave, lane, c.left) : o;
+      load_lds(c.to + (wave * SA::LOADS + i) * 1024, o, c.a);
+      return;
     }
-    const E *pa = (const E *)a.a[seg] + (AKS ? k * a.lda + m0 : m0 * a.lda + k);
-    sa.issue(to, buffer_of(pa), wave, lane, left);
+    i -= SA::LOADS;
+    uint32_t o = sb.from(i, wave, lane, c.left);
     if constexpr (DUAL) {
-      const i4 g = buffer_of((const E *)a.b[0] + n0 * a.ldb + k);
-      const i4 u = buffer_of((const E *)a.b[1] + n0 * a.ldb + k);
-#pragma unroll
-      for (int i = 0; i < SB::LOADS; ++i) {
-        const bool up = (8 * (wave * SB::LOADS + i) / (NI * 8)) & 1;
-        sb.issue1(i, to + SA::BYTES, up ? u : g, wave, lane, left);
+      const bool up = (8 * (wave * SB::LOADS + i) / (NI * 8)) & 1;
+      const i4 buf = up && !c.second ? c.b2 : c.b;
+      int32_t at = wave * SB::LOADS + i;
+      if constexpr (EPI == EPI_GRAD) {
+        // the third product's part is smaller: the loads left over clear the rest
+        if (i < SD::LOADS) {
+          o = c.second ? sd.from(i, wave, lane, c.left) : o;
+          at = c.second ? wave * SD::LOADS + i : at;
+        } else {
+          o = c.second ? OUTSIDE : o;
+          at = c.second ? NW * SD::LOADS + wave * (SB::LOADS - SD::LOADS) + i - SD::LOADS : at;
+        }
       }
+      load_lds(c.to + SA::BYTES + at * 1024, o, buf);
     } else {
-      const E *pb = (const E *)a.b[seg] + (BKS ? k * a.ldb + n0 : n0 * a.ldb + k);
-      sb.issue(to + SA::BYTES, buffer_of(pb), wave, lane, left);
+      load_lds(c.to + SA::BYTES + (wave * SB::LOADS + i) * 1024, o, c.b);
     }
   };
 
@@ -290,51 +356,73 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gated_product(ProductArgs a) 
 
   constexpr int HN = NI / 2;
   f4 third[EPI == EPI_GRAD ? MI : 1][EPI == EPI_GRAD ? HN : 1];
-  const int32_t end1 = EPI == EPI_GRAD ? seg_steps : end;
-  if (first < end) issue(first, 0);
-  for (int32_t step = first; step < end1; ++step) {
-    const int buf = (step - first) & 1;
-    stage_barrier();
-    if (step + 1 < end) issue(step + 1, buf ^ 1);
-    const uint32_t la = lds + buf * STAGE, lb = la + SA::BYTES;
+  if (first < end) {
+    uint32_t now = lds;  // the stage that is multiplied
+    auto after = [&](uint32_t p) { return p + STAGE == lds + S * STAGE ? lds : p + STAGE; };
 #pragma unroll
-    for (int s = 0; s < BK / 32; ++s) {
-      s8v xb[NI], xa[MI];
+    for (int i = 0; i < (AHEAD ? S : S - 1); ++i) {
+      const Coming c = coming(first + i, lds + i * STAGE);
 #pragma unroll
-      for (int j = 0; j < NI; ++j) xb[j] = fb.load(lb, j, s);
+      for (int d = 0; d < LOADS; ++d) load(d, c);
+    }
+    if constexpr (AHEAD) stage_barrier<(S - 1) * LOADS>();
+    auto stages = [&](auto &sum, auto &fb, int32_t from, int32_t to) {
+      constexpr int N = sizeof(sum[0]) / sizeof(f4);
+      if constexpr (!AHEAD) {
+        for (int32_t step = from; step < to; ++step) {
+          stage_barrier<(S - 2) * LOADS>();
+          const uint32_t last = now == lds ? lds + (S - 1) * STAGE : now - STAGE;
+          const Coming c = coming(step + S - 1, last);
 #pragma unroll
-      for (int i = 0; i < MI; ++i) xa[i] = fa.load(la, i, s);
+          for (int d = 0; d < LOADS; ++d) load(d, c);
+#pragma unroll
+          for (int s = 0; s < BK / 32; ++s) {
+            s8v xa[MI], xb[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) xb[j] = fb.load(now + SA::BYTES, j, s);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) xa[i] = fa.load(now, i, s);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+              for (int j = 0; j < N; ++j) sum[i][j] = mfma16<T>(xb[j], xa[i], sum[i][j]);
+          }
+          now = after(now);
+        }
+        return;
+      }
+      s8v xa[MI], ya[MI], xb[N], yb[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) xb[j] = fb.load(now + SA::BYTES, j, 0);
+#pragma unroll
+      for (int i = 0; i < MI; ++i) xa[i] = fa.load(now, i, 0);
+      for (int32_t step = from; step < to; ++step) {
+        const uint32_t next = after(now);
+        half_stage<T, MI, N, 0>(
+            sum, xa, xb, ya, yb, [&](int i) { return fa.load(now, i, 1); },
+            [&](int j) { return fb.load(now + SA::BYTES, j, 1); }, [](int) {});
+        stage_barrier<(S - 2) * LOADS>();
+        const Coming c = coming(step + S, now);
+        // after the last of these stages, what is read here is not used
+        half_stage<T, MI, N, LOADS>(
+            sum, ya, yb, xa, xb, [&](int i) { return fa.load(next, i, 0); },
+            [&](int j) { return fb.load(next + SA::BYTES, j, 0); }, [&](int d) { load(d, c); });
+        now = next;
+      }
+    };
+    if constexpr (EPI == EPI_GRAD) {
+      Frag<SD::WIDTH, true> fd;
+      fd.init(wn * HN * 16, lane);
 #pragma unroll
       for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = mfma16<T>(xb[j], xa[i], acc[i][j]);
+        for (int j = 0; j < HN; ++j) third[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+      stages(acc, fb, 0, seg_steps);
+      stages(third, fd, seg_steps, end);
+    } else {
+      stages(acc, fb, first, end);
     }
-  }
-  if constexpr (EPI == EPI_GRAD) {
-    Frag<SD::WIDTH, true> fd;
-    fd.init(wn * HN * 16, lane);
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-      for (int j = 0; j < HN; ++j) third[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-    for (int32_t step = end1; step < end; ++step) {
-      const int buf = step & 1;
-      stage_barrier();
-      if (step + 1 < end) issue(step + 1, buf ^ 1);
-      const uint32_t la = lds + buf * STAGE, lb = la + SA::BYTES;
-#pragma unroll
-      for (int s = 0; s < BK / 32; ++s) {
-        s8v xb[HN], xa[MI];
-#pragma unroll
-        for (int j = 0; j < HN; ++j) xb[j] = fd.load(lb, j, s);
-#pragma unroll
-        for (int i = 0; i < MI; ++i) xa[i] = fa.load(la, i, s);
-#pragma unroll
-        for (int i = 0; i < MI; ++i)
-#pragma unroll
-          for (int j = 0; j < HN; ++j) third[i][j] = mfma16<T>(xb[j], xa[i], third[i][j]);
-      }
-    }
+    stage_barrier<0>();  // no load is under way when the workgroup ends
   }
 
   // A lane's part of block (i, j): row mrow(i), columns 4 (lane / 16) .. + 3 of
@@ -537,7 +625,7 @@ __global__ __launch_bounds__(256) void join_parts(JoinArgs a) {
   }
 }
 
-template <int T, int WM, int WN, int MI, int NI, bool AKS, bool BKS, int EPI>
+template <int T, int WM, int WN, int MI, int NI, int S, bool AKS, bool BKS, int EPI>
 hipError_t product_go(const ProductArgs &in, hipStream_t stream) {
   ProductArgs a = in;
   constexpr int TM = WM * MI * 16, TN = WN * NI * 16;
@@ -546,15 +634,25 @@ hipError_t product_go(const ProductArgs &in, hipStream_t stream) {
   a.nt = (a.N + CN - 1) / CN;
   const int64_t grid = (int64_t)a.mt * a.nt * a.splits;
   if (grid * 64 * WM * WN >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
-  return launch_lds(gated_product<T, WM, WN, MI, NI, AKS, BKS, EPI>, dim3((unsigned)grid),
-                    dim3(64 * WM * WN), (TM + TN) * BK * 2 * 2, stream, a);
+  return launch_lds(gated_product<T, WM, WN, MI, NI, S, AKS, BKS, EPI>, dim3((unsigned)grid),
+                    dim3(64 * WM * WN), (TM + TN) * BK * 2 * S, stream, a);
 }
 
 template <int T, bool AKS, bool BKS, int EPI>
 hipError_t product_tile(const ProductArgs &a, int tile, hipStream_t stream) {
-  if (tile == TILE_256) return product_go<T, 2, 4, 8, 4, AKS, BKS, EPI>(a, stream);
-  if (tile == TILE_256x128) return product_go<T, 4, 2, 4, 4, AKS, BKS, EPI>(a, stream);
-  return product_go<T, 2, 2, 4, 4, AKS, BKS, EPI>(a, stream);
+  // Four waves of 128 x 128 read least from LDS, eight of 128 x 64 hide more.  Two
+  // projections of 8192 x 2048 -> 8192 take 523 us with eight, 610 with four; the
+  // gradients of their weights and rows, whose LDS reads are twice as many, 458 and
+  // 452 with four, 580 and 534 with eight.
+  if (tile == TILE_256) {
+    if constexpr (EPI == EPI_ROWS && BKS)
+      return product_go<T, 2, 2, 8, 8, 2, AKS, BKS, EPI>(a, stream);
+    else
+      return product_go<T, 2, 4, 8, 4, 2, AKS, BKS, EPI>(a, stream);
+  }
+  if (tile == TILE_256x128) return product_go<T, 4, 2, 4, 4, 3, AKS, BKS, EPI>(a, stream);
+  if (tile == TILE_128) return product_go<T, 2, 2, 4, 4, 2, AKS, BKS, EPI>(a, stream);
+  return product_go<T, 2, 2, 4, 4, 4, AKS, BKS, EPI>(a, stream);
 }
 
 template <int T>
@@ -612,6 +710,8 @@ ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu) {
     p.splits = 1;
     p.split_steps = INT32_MAX;
   }
+  // one workgroup to a CU at most: more stages on their way in place of a second one
+  if (p.tile == TILE_128 && tiles(128, 128) * p.splits <= n_cu) p.tile = TILE_128_DEEP;
   return p;
 }
 

@@ -452,7 +452,7 @@ constexpr int EPI_ROWS = 0, EPI_PART = 1, EPI_GATE = 2, EPI_GRAD = 3;
 // with k outermost (ROWS), both (WEIGHTS).
 constexpr int PRODUCT_GATE = 0, PRODUCT_GRAD = 1, PRODUCT_DOWN = 2, PRODUCT_ROWS = 3,
               PRODUCT_WEIGHTS = 4;
-constexpr int TILE_128 = 0, TILE_256x128 = 1, TILE_256 = 2;
+constexpr int TILE_128 = 0, TILE_256x128 = 1, TILE_256 = 2, TILE_128_DEEP = 3;
 struct ProductArgs {
   // Operands of one or two segments of k (GATE, GRAD: b[1] is the up projection).
   // Addresses are multiples of 16 bytes, strides (in elements, below 2^21) and
@@ -484,7 +484,7 @@ struct ProductPlan {
 ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu);
 // Rows of `sums` that a GRAD product writes.
 inline int64_t product_sum_rows(int tile, int64_t M) {
-  const int64_t tm = tile == TILE_128 ? 128 : 256;
+  const int64_t tm = tile == TILE_128 || tile == TILE_128_DEEP ? 128 : 256;
   return (M + tm - 1) / tm * (tile == TILE_256x128 ? 4 : 2);
 }
 hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hipStream_t stream);
