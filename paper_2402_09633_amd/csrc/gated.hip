@@ -525,30 +525,37 @@ gated_product(ProductArgs a) {
 
 // ---- few rows ----
 // Up to 16 MB rows: every weight is read once, from memory straight into the
-// MFMA's registers, and there is nothing else to wait for.  A workgroup takes 16
+// MFMA's registers, and there is nothing else to wait for.  A workgroup takes 16 NC
 // columns (of gate and of up alike, GATE), its waves a share of the k each; their
 // sums meet in LDS.  k of a step go to the lanes in a different order than in
 // memory, the same for both operands, so that the four lanes of a row read 128
 // neighbouring bytes.
-template <int T, int MB, int NW, bool GATE>
+//
+// The down projection has few columns and many k, so several workgroups (gridDim.y)
+// share a column's k, and few_join adds up what they leave: 8192 -> 2048, one row,
+// 12.3 us without.  (One kernel whose last workgroup adds up took 99: a fence
+// between compute dies writes their caches back.)
+template <int T, int MB, int NC, int NW, bool GATE>
 __global__ __launch_bounds__(64 * NW) void gated_few(ProductArgs a) {
   typedef elem_t<T> E;
-  constexpr int NB = GATE ? 2 : 1;
+  constexpr int NB = GATE ? 2 * NC : NC;
+  __shared__ f4 sum[NW][MB * NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
-  const int32_t n0 = blockIdx.x * 16;
+  const int32_t n0 = blockIdx.x * 16 * NC;
   const E *pa[MB], *pb[NB];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
     pa[i] = (const E *)a.a[0] + min((int64_t)(i * 16 + li), a.M - 1) * a.lda;
 #pragma unroll
-  for (int j = 0; j < NB; ++j) pb[j] = (const E *)a.b[j] + (int64_t)min(n0 + li, a.N - 1) * a.ldb;
+  for (int j = 0; j < NB; ++j)
+    pb[j] = (const E *)a.b[j / NC] + (int64_t)min(n0 + j % NC * 16 + li, a.N - 1) * a.ldb;
   f4 acc[MB][NB];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
-  const int32_t whole = a.K / BK;
+  const int32_t whole = a.K / BK, step_k = NW * gridDim.y;
   auto step = [&](int32_t k, bool end) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -568,41 +575,72 @@ __global__ __launch_bounds__(64 * NW) void gated_few(ProductArgs a) {
                                 acc[i][j]);
     }
   };
-  int32_t st = wave;
-#pragma unroll 4
-  for (; st < whole; st += NW) step(st * BK, false);
+  int32_t st = wave + NW * blockIdx.y;
+#pragma unroll(MB == 1 ? 8 : 4)
+  for (; st < whole; st += step_k) step(st * BK, false);
   if (st == whole && a.K % BK) step(st * BK, true);
 
-  __shared__ f4 sum[NW][MB * NB][64];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
     for (int j = 0; j < NB; ++j) sum[wave][i * NB + j][lane] = acc[i][j];
   __syncthreads();
-  for (int i = wave; i < MB; i += NW) {
-    f4 v[NB];
+  if (!GATE && gridDim.y > 1) {
+    f4 *mine = (f4 *)a.part + ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (MB * NB * 64);
+    for (int q = wave; q < MB * NB; q += NW) {
+      f4 v = sum[0][q][lane];
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      v[j] = sum[0][i * NB + j][lane];
-      for (int w = 1; w < NW; ++w) v[j] += sum[w][i * NB + j][lane];
+      for (int w = 1; w < NW; ++w) v += sum[w][q][lane];
+      mine[q * 64 + lane] = v;
+    }
+    return;
+  }
+  for (int q = wave; q < MB * NC; q += NW) {
+    const int i = q / NC, j0 = q % NC;
+    f4 v[GATE ? 2 : 1];
+#pragma unroll
+    for (int p = 0; p < (GATE ? 2 : 1); ++p) {
+      const int at = i * NB + p * NC + j0;
+      v[p] = sum[0][at][lane];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) v[p] += sum[w][at][lane];
     }
     const int64_t m = i * 16 + li;
-    const int32_t c = n0 + lg * 4;
+    const int32_t c = n0 + j0 * 16 + lg * 4;
 #pragma unroll
-    for (int j = 0; j < NB; ++j)
-      v[j] += load4<T>((const E *)a.bias[j] ? (const E *)a.bias[j] + c : nullptr, a.N - c);
+    for (int p = 0; p < (GATE ? 2 : 1); ++p)
+      v[p] += load4<T>((const E *)a.bias[p] ? (const E *)a.bias[p] + c : nullptr, a.N - c);
     if (m >= a.M) continue;
     if constexpr (GATE) {
       f4 h;
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        h[q] = c + q < a.N ? activate<false>(a.act, v[0][q], nullptr) * v[1][q] : 0.f;
+      for (int e = 0; e < 4; ++e)
+        h[e] = c + e < a.N ? activate<false>(a.act, v[0][e], nullptr) * v[1][e] : 0.f;
       if (c < a.ldc) store4<T>((E *)a.c + m * a.ldc + c, h, 4, true);
     } else {
       store4<T>((E *)a.c + m * a.ldc + c, v[0], a.N - c,
                 a.ldc % 4 == 0 && (uintptr_t)a.c % 8 == 0);
     }
   }
+}
+
+// A wave adds up one block of 16 x 16: `parts` sums of it, `blocks` blocks apart.
+template <int T>
+__global__ __launch_bounds__(64) void few_join(ProductArgs a, int32_t parts, int32_t mb,
+                                               int32_t nc) {
+  typedef elem_t<T> E;
+  const int lane = threadIdx.x, blk = blockIdx.x, blocks = gridDim.x;
+  f4 v = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int32_t y = 0; y < parts; ++y)
+    v += ((const f4 *)a.part)[((int64_t)y * blocks + blk) * 64 + lane];
+  // blocks lie as gated_few's workgroups have them: [column group][m][column]
+  const int in = blk % (mb * nc);
+  const int64_t m = in / nc * 16 + (lane & 15);
+  const int32_t c = (blk / (mb * nc) * nc + in % nc) * 16 + (lane >> 4) * 4;
+  if (m >= a.M) return;
+  v += load4<T>((const E *)a.bias[0] ? (const E *)a.bias[0] + c : nullptr, a.N - c);
+  store4<T>((E *)a.c + m * a.ldc + c, v, a.N - c, a.ldc % 4 == 0 && (uintptr_t)a.c % 8 == 0);
 }
 
 // Sums of the parts of a product whose k were shared out: part [splits][M][ldp]
@@ -668,15 +706,23 @@ hipError_t product_t(const ProductArgs &a, int kind, int tile, hipStream_t strea
   }
 }
 
+template <int T, bool GATE, int MB, int NC>
+hipError_t few_go(const ProductArgs &a, int splits, hipStream_t stream) {
+  const int n = (a.N + 16 * NC - 1) / (16 * NC);
+  constexpr int NW = MB == 1 && !GATE ? 16 : 8;
+  const hipError_t e =
+      launch(gated_few<T, MB, NC, NW, GATE>, dim3(n, splits), dim3(64 * NW), 0, stream, a);
+  if (e != hipSuccess || splits == 1) return e;
+  return launch(few_join<T>, dim3(n * MB * NC), dim3(64), 0, stream, a, splits, MB, NC);
+}
+
 template <int T, bool GATE>
-hipError_t few_t(const ProductArgs &a, hipStream_t stream) {
-  const dim3 grid((a.N + 15) / 16);
-  constexpr int NW = GATE ? 8 : 16;
+hipError_t few_t(const ProductArgs &a, int splits, hipStream_t stream) {
   switch ((a.M + 15) / 16) {
-    case 1: return launch(gated_few<T, 1, NW, GATE>, grid, dim3(64 * NW), 0, stream, a);
-    case 2: return launch(gated_few<T, 2, 8, GATE>, grid, dim3(512), 0, stream, a);
-    case 3: return launch(gated_few<T, 3, 8, GATE>, grid, dim3(512), 0, stream, a);
-    default: return launch(gated_few<T, 4, 8, GATE>, grid, dim3(512), 0, stream, a);
+    case 1: return few_go<T, GATE, 1, 1>(a, splits, stream);
+    case 2: return few_go<T, GATE, 2, FEW_COLUMNS>(a, splits, stream);
+    case 3: return few_go<T, GATE, 3, FEW_COLUMNS>(a, splits, stream);
+    default: return few_go<T, GATE, 4, FEW_COLUMNS>(a, splits, stream);
   }
 }
 
@@ -720,9 +766,20 @@ hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hi
                         : product_t<T_F16>(a, kind, tile, stream);
 }
 
-hipError_t launch_few(const ProductArgs &a, bool gate, int type, hipStream_t stream) {
-  if (type == T_BF16) return gate ? few_t<T_BF16, true>(a, stream) : few_t<T_BF16, false>(a, stream);
-  return gate ? few_t<T_F16, true>(a, stream) : few_t<T_F16, false>(a, stream);
+// Workgroups that share a column block's k: as many as fill the chip, of two
+// steps to a wave at least.  Up to 16 rows a workgroup has 16 waves, and the sums'
+// own launch pays for itself only where few have work (8192 -> 2048, one row: 11.2
+// and 3.6 us shared, 12.3 alone; 48 rows 15.1 and 4.0, 31.8 alone).
+int few_splits(int64_t M, int64_t N, int64_t K, int n_cu) {
+  const int64_t n = few_blocks(M, N), steps = (K + BK - 1) / BK;
+  if (M <= 16 && n >= n_cu / 4) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(2 * n_cu / n, steps / 16));
+}
+
+hipError_t launch_few(const ProductArgs &a, bool gate, int type, int splits, hipStream_t stream) {
+  if (type == T_BF16)
+    return gate ? few_t<T_BF16, true>(a, 1, stream) : few_t<T_BF16, false>(a, splits, stream);
+  return gate ? few_t<T_F16, true>(a, 1, stream) : few_t<T_F16, false>(a, splits, stream);
 }
 
 hipError_t launch_join(const JoinArgs &a, int type, hipStream_t stream) {

@@ -474,6 +474,7 @@ struct ProductArgs {
   void *c = nullptr, *c2 = nullptr;
   int64_t ldc = 0;
   int64_t c_rows = INT64_MAX, c_valid = INT64_MAX;
+  float *part = nullptr;         // few rows: sums of workgroups that share their k
   float *sums = nullptr;         // GRAD: column sums [row tiles * waves of m][2 ldc]
   int32_t act = 0;
 };
@@ -490,7 +491,19 @@ inline int64_t product_sum_rows(int tile, int64_t M) {
 hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hipStream_t stream);
 // Up to FEW_ROWS rows; operands of any alignment (GATE or DOWN).
 constexpr int FEW_ROWS = 64;
-hipError_t launch_few(const ProductArgs &a, bool gate, int type, hipStream_t stream);
+constexpr int FEW_COLUMNS = 2;   // column blocks to a workgroup (1 up to 16 rows)
+inline int64_t few_blocks(int64_t M, int64_t N) {
+  const int64_t n = M <= 16 ? 16 : 16 * FEW_COLUMNS;
+  return (N + n - 1) / n;
+}
+int few_splits(int64_t M, int64_t N, int64_t K, int n_cu);
+// DOWN's sums of `splits` workgroups: bytes of `part`.
+inline size_t few_part_bytes(int64_t M, int64_t N, int splits) {
+  return splits == 1 ? 0
+                     : (size_t)few_blocks(M, N) * splits * ((M + 15) / 16) *
+                           (M <= 16 ? 1 : FEW_COLUMNS) * 1024;
+}
+hipError_t launch_few(const ProductArgs &a, bool gate, int type, int splits, hipStream_t stream);
 struct JoinArgs {
   const float *part = nullptr;   // [splits][M][ldp]
   int32_t splits = 1;

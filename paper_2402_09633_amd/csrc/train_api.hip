@@ -283,20 +283,21 @@ bool lies_aligned(const void *p, int64_t stride) {
 struct GatedForward {
   bool few = false;
   Operand x, gate, up, down;
-  size_t h = 0;
+  size_t h = 0, part = 0;
+  int splits = 1;
   Carve c;
-  GatedForward(const gnn_gated_dims &d, int64_t n, const void *xp, int64_t ld, bool x_in,
+  GatedForward(const gnn_gated_dims &d, int64_t n, int n_cu, const void *xp, int64_t ld, bool x_in,
                const gnn_gated_weights *w, bool w_in)
       : x(xp, ld, n, d.in_features, x_in),
         gate(w ? w->gate : nullptr, d.in_features, d.hidden, d.in_features, w_in),
         up(w ? w->up : nullptr, d.in_features, d.hidden, d.in_features, w_in),
         down(w ? w->down : nullptr, d.hidden, d.out_features, d.hidden, w_in) {
     few = n <= FEW_ROWS;
-    if (!few) {
-      x.place(c);
-      gate.place(c);
-      up.place(c);
-      down.place(c);
+    if (few && n > 0) {
+      splits = few_splits(n, d.out_features, d.hidden, n_cu);
+      part = c.take(few_part_bytes(n, d.out_features, splits));
+    } else {
+      for (Operand *o : {&x, &gate, &up, &down}) o->place(c);
     }
     h = c.take((size_t)n * up8(d.hidden) * 2);
   }
@@ -335,10 +336,11 @@ struct GatedBackward {
   }
 };
 
+// Where no device is visible, sizes are those of one with 256 compute units.
 int devices_cu(int *n_cu) {
   int dev = 0;
   const int rc = current_device(&dev);
-  if (!rc) *n_cu = cu_count(dev);
+  *n_cu = rc ? 256 : cu_count(dev);
   return rc;
 }
 
@@ -354,10 +356,10 @@ extern "C" {
 size_t gnn_gated_workspace(const gnn_gated_dims *d, int64_t n_rows, int32_t backward,
                            int32_t aligned) {
   if (check_gated_dims(d) || check_rows(n_rows)) return 0;
+  if (n_rows == 0 && !backward) return 0;
   int n_cu = 0;
-  if (!backward)
-    return n_rows ? GatedForward(*d, n_rows, nullptr, 0, aligned, nullptr, aligned).c.total : 0;
-  if (devices_cu(&n_cu)) return 0;
+  (void)devices_cu(&n_cu);
+  if (!backward) return GatedForward(*d, n_rows, n_cu, nullptr, 0, aligned, nullptr, aligned).c.total;
   return GatedBackward(*d, n_rows, n_cu, nullptr, 0, nullptr, 0, aligned, nullptr, aligned).c.total;
 }
 
@@ -370,10 +372,12 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   if ((rc = check_table("x", x, d->dtype, x_stride, d->in_features)) ||
       (rc = check_table("y", y, d->dtype, y_stride, d->out_features)))
     return rc;
-  GatedForward f(*d, n_rows, x, x_stride, lies_aligned(x, x_stride), w, weights_aligned(*d, *w));
-  if ((rc = check_scratch(workspace, workspace_bytes, f.c.total))) return rc;
   int n_cu = 0;
-  if ((rc = devices_cu(&n_cu))) return rc;
+  const int none = devices_cu(&n_cu);
+  GatedForward f(*d, n_rows, n_cu, x, x_stride, lies_aligned(x, x_stride), w,
+                 weights_aligned(*d, *w));
+  if ((rc = check_scratch(workspace, workspace_bytes, f.c.total))) return rc;
+  if (none) return none;
   unsigned char *ws = (unsigned char *)workspace;
   const int t = d->dtype;
   const int64_t hp = up8(d->hidden);
@@ -394,7 +398,7 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   a.c = ws + f.h;
   a.ldc = hp;
   a.act = d->activation;
-  rc = launched(f.few ? launch_few(a, true, t, stream)
+  rc = launched(f.few ? launch_few(a, true, t, 1, stream)
                       : launch_product(a, PRODUCT_GATE, t,
                                        product_plan(PRODUCT_GATE, a.M, a.N, a.K, n_cu).tile, stream),
                 "gate");
@@ -410,7 +414,8 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   b.bias[0] = w->down_bias;
   b.c = y;
   b.ldc = y_stride;
-  return launched(f.few ? launch_few(b, false, t, stream)
+  b.part = (float *)(ws + f.part);
+  return launched(f.few ? launch_few(b, false, t, f.splits, stream)
                         : launch_product(b, PRODUCT_DOWN, t,
                                          product_plan(PRODUCT_DOWN, b.M, b.N, b.K, n_cu).tile,
                                          stream),
@@ -430,11 +435,12 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
                      (rc = check_table("dx", dx, d->dtype, dx_stride, d->in_features))))
     return rc;
   int n_cu = 0;
-  if ((rc = devices_cu(&n_cu))) return rc;
+  const int none = devices_cu(&n_cu);
   GatedBackward f(*d, n_rows, n_cu, x, x_stride, dy, dy_stride,
                   n_rows == 0 || (lies_aligned(x, x_stride) && lies_aligned(dy, dy_stride)), w,
                   weights_aligned(*d, *w));
   if ((rc = check_scratch(workspace, workspace_bytes, f.c.total))) return rc;
+  if (none) return none;
   unsigned char *ws = (unsigned char *)workspace;
   const int t = d->dtype;
   const int64_t hp = up8(d->hidden);

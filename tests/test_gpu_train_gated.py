@@ -79,6 +79,16 @@ def test_large(G, m, k, h, n):
     check(G, *make(m, k, h, n, torch.float16, m), "silu")
 
 
+# Few rows and many hidden elements: several workgroups share the sums of the down
+# projection.
+@pytest.mark.parametrize("m", [1, 16, 17, 40, 64])
+@pytest.mark.parametrize("k,h,n", [(96, 4096, 160), (40, 8200, 33), (2048, 2049, 1040)])
+def test_few_rows_of_wide_blocks(G, m, k, h, n):
+    x, w, b, _ = make(m, k, h, n, torch.float16, m)
+    y, _ = check(G, x, w, b, None, "silu", backward=False)
+    assert torch.equal(G.gated(x, *w, biases=b), y)
+
+
 def test_many_rows(G):
     check(G, *make(300_001, 32, 64, 32, torch.bfloat16, 1), "gelu")
 
