@@ -39,13 +39,13 @@ __device__ __forceinline__ f4 mfma16(const s8v &a, const s8v &b, const f4 &c) {
 // act(g) and its derivative.  gelu is g Phi(g); 1 - erf(z) for z >= 0 is taken
 // as t P(t) exp(-z^2), t = 1 / (1 + 0.3275911 z) (Abramowitz and Stegun, 7.1.26;
 // off by at most 1.5e-7, a hundredth of a 16-bit number's last place at 1).
-template <bool SLOPE>
-__device__ __forceinline__ float activate(int act, float g, float *slope) {
-  if (act == ACT_RELU) {
+template <int act, bool SLOPE>
+__device__ __forceinline__ float activate(float g, float *slope) {
+  if constexpr (act == ACT_RELU) {
     if (SLOPE) *slope = g > 0.f ? 1.f : 0.f;
     return g > 0.f || g != g ? g : 0.f;
   }
-  if (act == ACT_GELU) {
+  if constexpr (act == ACT_GELU) {
     const float z = fabsf(g) * 0.70710678118654752f;
     const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * z);
     const float e = __expf(-z * z);
@@ -58,12 +58,24 @@ __device__ __forceinline__ float activate(int act, float g, float *slope) {
     return g * phi;
   }
   const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
-  if (act == ACT_SIGMOID) {
+  if constexpr (act == ACT_SIGMOID) {
     if (SLOPE) *slope = s * (1.f - s);
     return s;
   }
   if (SLOPE) *slope = s * (1.f + g * (1.f - s));
   return g * s;
+}
+
+// f with the activation as a constant: one branch for all elements, between which
+// the instructions of several then overlap.
+template <typename F>
+__host__ __device__ __forceinline__ auto with_activation(int act, F &&f) {
+  switch (act) {
+    case ACT_GELU: return f(std::integral_constant<int, ACT_GELU>{});
+    case ACT_SIGMOID: return f(std::integral_constant<int, ACT_SIGMOID>{});
+    case ACT_RELU: return f(std::integral_constant<int, ACT_RELU>{});
+    default: return f(std::integral_constant<int, ACT_SILU>{});
+  }
 }
 
 // ---- memory to LDS ----
@@ -234,7 +246,8 @@ __device__ __forceinline__ void half_stage(f4 (&acc)[MI][NI], const s8v (&xa)[MI
 // each to a wave, so that a wave has g and u of the same elements.  GRAD goes on
 // with dh = dy Wd (k outermost) of these elements in registers of its own: dh is
 // never rounded, nor in memory.
-template <int T, int WM, int WN, int MI, int NI, int S, bool AKS, bool BKS, int EPI>
+// ACT: GRAD's activation; its sums leave no registers for a choice among four.
+template <int T, int WM, int WN, int MI, int NI, int S, bool AKS, bool BKS, int EPI, int ACT>
 __global__ __launch_bounds__(64 * WM * WN, WM * WN == 4 && (MI * NI > 16 || S > 2) ? 1 : 2) void
 gated_product(ProductArgs a) {
   constexpr int NW = WM * WN, TM = WM * MI * 16, TN = WN * NI * 16;
@@ -439,41 +452,48 @@ gated_product(ProductArgs a) {
       bu[j] = load4<T>((const E *)a.bias[1] ? (const E *)a.bias[1] + c : nullptr, a.N - c);
       sg[j] = su[j] = f4{0.f, 0.f, 0.f, 0.f};
     }
+    auto elements = [&](auto which) {
+      constexpr int A = which.value;
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-      const int64_t m = mw + i * 16;
+      for (int i = 0; i < MI; ++i) {
+        const int64_t m = mw + i * 16;
 #pragma unroll
-      for (int j = 0; j < HN; ++j) {
-        const int32_t c = c0 + j * 16;
-        if (m < a.M && c < a.ldc) {  // ldc: N and its padding, in which everything is zero
-          const f4 g = acc[i][j] + bg[j], u = acc[i][j + HN] + bu[j];
-          E *ph = (E *)a.c + m * a.ldc + c;
-          f4 h;
-          if constexpr (EPI == EPI_GATE) {
+        for (int j = 0; j < HN; ++j) {
+          const int32_t c = c0 + j * 16;
+          if (m < a.M && c < a.ldc) {  // ldc: N and its padding, in which everything is zero
+            const f4 g = acc[i][j] + bg[j], u = acc[i][j + HN] + bu[j];
+            E *ph = (E *)a.c + m * a.ldc + c;
+            f4 h;
+            if constexpr (EPI == EPI_GATE) {
 #pragma unroll
-            for (int v = 0; v < 4; ++v) h[v] = activate<false>(a.act, g[v], nullptr) * u[v];
-            store4<T>(ph, h, 4, true);
-          } else {
-            const f4 dh = third[i][j];
-            f4 dg, du;
+              for (int v = 0; v < 4; ++v) h[v] = activate<A, false>(g[v], nullptr) * u[v];
+              store4<T>(ph, h, 4, true);
+            } else {
+              const f4 dh = third[i][j];
+              f4 dg, du;
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              float slope;
-              const float s = activate<true>(a.act, g[v], &slope);
-              h[v] = s * u[v];
-              dg[v] = dh[v] * u[v] * slope;
-              du[v] = dh[v] * s;
+              for (int v = 0; v < 4; ++v) {
+                float slope;
+                const float s = activate<A, true>(g[v], &slope);
+                h[v] = s * u[v];
+                dg[v] = dh[v] * u[v] * slope;
+                du[v] = dh[v] * s;
+              }
+              sg[j] += dg;
+              su[j] += du;
+              E *pd = (E *)a.c2 + m * 2 * a.ldc + c;
+              store4<T>(ph, h, 4, true);
+              store4<T>(pd, dg, 4, true);
+              store4<T>(pd + a.ldc, du, 4, true);
             }
-            sg[j] += dg;
-            su[j] += du;
-            E *pd = (E *)a.c2 + m * 2 * a.ldc + c;
-            store4<T>(ph, h, 4, true);
-            store4<T>(pd, dg, 4, true);
-            store4<T>(pd + a.ldc, du, 4, true);
           }
         }
       }
-    }
+    };
+    if constexpr (EPI == EPI_GRAD)
+      elements(std::integral_constant<int, ACT>{});
+    else
+      with_activation(a.act, elements);
     // Column sums of dg and du over the wave's rows (the biases' gradients),
     // from the numbers before they are rounded.
     if (EPI == EPI_GRAD && a.sums) {
@@ -519,6 +539,284 @@ gated_product(ProductArgs a) {
         if (m < a.M && r < a.c_valid)
           store4<T>((one ? (E *)a.c : (E *)a.c2) + r * a.ldc + c, acc[i][j] + b, a.N - c, whole);
       }
+    }
+  }
+}
+
+// ---- narrow blocks in one pass ----
+// Rows of up to 128 elements in and out: what lies between them stays in registers.
+// A wave keeps its 16 MI rows of x and its sums of y, and goes through the hidden
+// elements 32 at a time, whose weights (32 rows of gate and of up, 32 columns of
+// down) come to LDS a step ahead.  A lane's sums of g and u are, for one row, four
+// neighbouring hidden elements of either block of 16; their products in 16 bits
+// are the eight k that the MFMA of the down projection wants of a lane, if Wd's
+// are read in the same order (4 lg + j and 16 + 4 lg + j).
+//
+// GRAD: dh from the rows of dy, which a wave keeps too, then h, dg and du, which go to
+// memory for the weights' gradients, and dx from dg and du as y from h; Wd, Wg and
+// Wu are read from the same places by transposing reads.
+//
+// Bound by the activation's instructions and the LDS reads more than by the matrix
+// cores; GRAD by the rows that it writes.  Two workgroups of four waves to a CU run
+// out of step: 300000 x 128 -> 512 -> 128 bf16 240 us, one of eight waves 278, through
+// the products above 411.
+constexpr int THIN_STAGES = 3, THIN_WAVES = 4, THIN_HIDDEN = 2048;
+
+// The sum over the 16 lanes of one lg, in all of them.
+__device__ __forceinline__ float lanes16_sum(float v) {
+  auto other = [](float x, auto ctrl) {
+    return __uint_as_float(
+        __builtin_amdgcn_mov_dpp(__float_as_uint(x), ctrl.value, 0xf, 0xf, true));
+  };
+  v += other(v, std::integral_constant<int, 0xb1>{});   // lane ^ 1
+  v += other(v, std::integral_constant<int, 0x4e>{});   // lane ^ 2
+  v += other(v, std::integral_constant<int, 0x141>{});  // 7 - lane of 8
+  v += other(v, std::integral_constant<int, 0x140>{});  // 15 - lane of 16
+  return v;
+}
+
+// KS, NS: 32s of elements of x and of y (2 or 4).
+template <int T, int MI, int KS, int NS, bool GRAD, int ACT>
+__global__ __launch_bounds__(64 * THIN_WAVES, 2) void gated_thin(ProductArgs a) {
+  typedef elem_t<T> E;
+  typedef E e4 __attribute__((ext_vector_type(4)));
+  typedef typename Raw8<T>::vec e8;
+  typedef __attribute__((address_space(3))) s8v *p8;
+  typedef __attribute__((address_space(3))) s4v *p4;
+  constexpr int NW = THIN_WAVES;
+  constexpr int ROW = KS * 64;  // bytes of a gate or up row in LDS
+  constexpr int UP = 32 * ROW, DOWN = 2 * UP, STAGE = DOWN + 8192;
+  constexpr int LG = DOWN / 1024 / NW, LD = 8 / NW, LOADS = LG + LD;  // loads of a wave
+  constexpr int OUT = GRAD ? 2 * KS : 2 * NS;  // blocks of 16 of dx or y
+  extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
+  const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)shared;
+  const uint32_t bias = lds + THIN_STAGES * STAGE;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 15, lg = lane >> 4;
+  const int32_t steps = (a.N + 31) / 32;  // N: hidden elements, K2: columns of y
+
+  // biases of gate and up as they are, [2][steps * 32], zeros where there are none
+  for (int32_t i = threadIdx.x; i < 2 * 32 * steps; i += 64 * NW) {
+    const int32_t p = i >= 32 * steps, h = i - p * 32 * steps;
+    const E *b = (const E *)a.bias[p];
+    ((__attribute__((address_space(3))) E *)(uintptr_t)bias)[i] = b && h < a.N ? b[h] : (E)0.f;
+  }
+
+  // A wave's loads: gate and up rows of ROW bytes, then rows of down of 64 bytes.
+  // Their 16-byte pieces are exchanged by the row's number so that the eight rows
+  // that a read touches at a time, or the eight pairs of pieces that a transposing
+  // one does, lie in different banks.
+  auto swap_k = [](int r) { return KS == 4 ? (r & 7) << 1 : ((r >> 1) & 3) << 1; };
+  auto swap_d = [](int r) { return (r >> 2) & 3; };
+  uint32_t off[LOADS];
+  int32_t at[LOADS];  // hidden element of the load's lane, from the step's first
+#pragma unroll
+  for (int i = 0; i < LG; ++i) {
+    const int p = (wave * LG + i) * 1024 + lane * 16, r = p / ROW, c = (p % ROW / 16) ^ swap_k(r);
+    at[i] = r % 32;
+    off[i] = c * 8 < a.K ? (uint32_t)((r % 32) * (int32_t)a.ldb * 2 + c * 16) : OUTSIDE;
+  }
+#pragma unroll
+  for (int i = 0; i < LD; ++i) {
+    const int p = (wave * LD + i) * 1024 + lane * 16, r = p / 64, c = (p % 64 / 16) ^ swap_d(r);
+    at[LG + i] = c * 8;
+    off[LG + i] = r < a.K2 ? (uint32_t)(r * (int32_t)a.ldb2 * 2 + c * 16) : OUTSIDE;
+  }
+  auto issue = [&](int32_t step, uint32_t to) {
+    const bool on = step < steps;
+    const int32_t left = a.N - step * 32;
+#pragma unroll
+    for (int i = 0; i < LG; ++i) {
+      const bool up = (wave * LG + i) * 1024 >= UP;
+      load_lds(to + (wave * LG + i) * 1024, at[i] < left ? off[i] : OUTSIDE,
+               buffer_of((const E *)a.b[up ? 1 : 0] + (int64_t)step * 32 * a.ldb, on));
+    }
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+      load_lds(to + DOWN + (wave * LD + i) * 1024, at[LG + i] < left ? off[LG + i] : OUTSIDE,
+               buffer_of((const E *)a.b2 + step * 32, on));
+  };
+
+  const int64_t m0 = ((int64_t)blockIdx.x * NW + wave) * (16 * MI) + li;
+  auto rows = [&](const void *p, int64_t ld, int32_t width, auto &to) {
+    constexpr int S = sizeof(to[0]) / sizeof(s8v);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const E *row = (const E *)p + min(m0 + i * 16, a.M - 1) * ld;
+#pragma unroll
+      for (int k = 0; k < S; ++k) {
+        const int c = k * 32 + lg * 8;
+        to[i][k] = __builtin_bit_cast(
+            s8v, (width == S * 32 ? load8<T>(row, c) : load8_end<T>(row, c, width)).v);
+      }
+    }
+  };
+  s8v x[MI][KS], dy[MI][GRAD ? NS : 1];
+  rows(a.a[0], a.lda, a.K, x);
+  if constexpr (GRAD) rows(a.a[1], a.lda2, a.K2, dy);
+  f4 y[MI][OUT];  // GRAD: dx
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int n = 0; n < OUT; ++n) y[i][n] = f4{0.f, 0.f, 0.f, 0.f};
+  // the compiler's own loads are counted with the stages': none may be under way
+  __syncthreads();
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+  for (int s = 0; s < THIN_STAGES - 1; ++s) issue(s, lds + s * STAGE);
+
+  uint32_t now = lds;
+  for (int32_t step = 0; step < steps; ++step) {
+    // Loads come back in their order, so this stage is here when no more operations
+    // are under way than the next ones have loads, whatever the stores do.
+    stage_barrier<(THIN_STAGES - 2) * LOADS>();
+    issue(step + THIN_STAGES - 1, now == lds ? lds + (THIN_STAGES - 1) * STAGE : now - STAGE);
+    f4 sum[2][2][MI], dh[2][MI];  // g, u and dh of two blocks of 16 hidden elements
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const s4v raw = *(p4)(uintptr_t)(bias + 2 * (32 * (p * steps + step) + b * 16 + lg * 4));
+        const f4 v = __builtin_convertvector(__builtin_bit_cast(e4, raw), f4);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sum[p][b][i] = v;
+      }
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const s8v w = *(p8)(uintptr_t)(now + p * UP + (b * 16 + li) * ROW +
+                                         (((k * 4 + lg) ^ swap_k(li)) << 4));
+#pragma unroll
+          for (int i = 0; i < MI; ++i) sum[p][b][i] = mfma16<T>(w, x[i][k], sum[p][b][i]);
+        }
+    // rows r .. r + 3, 16 columns from piece 2 b on, to a lane's column
+    const int tr = li >> 2, tc = (li >> 1) & 1, tb = (li & 1) * 8;
+    if constexpr (GRAD) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) dh[b][i] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < NS; ++k) {
+          const int r = k * 32 + lg * 8 + tr;
+          const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)(
+              now + DOWN + r * 64 + (((2 * b + tc) ^ swap_d(r)) << 4) + tb));
+          const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)(
+              now + DOWN + (r + 4) * 64 + (((2 * b + tc) ^ swap_d(r + 4)) << 4) + tb));
+          const s8v w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) dh[b][i] = mfma16<T>(w, dy[i][k], dh[b][i]);
+        }
+      }
+    }
+    s8v h[MI], dg[MI], du[MI];
+    f8 sg = f8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, su = sg;
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      f8 v, vg, vu;
+      const bool in = m0 + i * 16 < a.M;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float g = sum[0][j / 4][i][j % 4], u = sum[1][j / 4][i][j % 4];
+        if constexpr (GRAD) {
+          float slope;
+          const float s = activate<ACT, true>(g, &slope), d = dh[j / 4][i][j % 4];
+          v[j] = s * u;
+          vg[j] = d * u * slope;
+          vu[j] = d * s;
+          if (in) {
+            sg[j] += vg[j];
+            su[j] += vu[j];
+          }
+        } else {
+          v[j] = activate<ACT, false>(g, nullptr) * u;
+        }
+      }
+      h[i] = __builtin_bit_cast(s8v, __builtin_convertvector(v, e8));
+      if constexpr (GRAD) {
+        dg[i] = __builtin_bit_cast(s8v, __builtin_convertvector(vg, e8));
+        du[i] = __builtin_bit_cast(s8v, __builtin_convertvector(vu, e8));
+      }
+    }
+    if constexpr (GRAD) {
+      // Lanes of odd lg trade with those before them, so that each has eight
+      // neighbouring elements: 4 lg .. of the first 16 (even), of the second (odd).
+      const int32_t c = step * 32 + (lg & 1) * 16 + (lg & 2) * 4;
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int64_t m = m0 + i * 16;
+        auto store = [&](const s8v &v, E *to) {
+          u4 w = __builtin_bit_cast(u4, v);
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            const auto t = __builtin_amdgcn_permlane16_swap(w[q], w[q + 2], false, false);
+            w[q] = t[0];
+            w[q + 2] = t[1];
+          }
+          if (m < a.M && c < a.ldc2) *(u4 *)(to + c) = w;
+        };
+        store(h[i], (E *)a.c2 + m * a.ldc2);
+        store(dg[i], (E *)a.c3 + m * 2 * a.ldc2);
+        store(du[i], (E *)a.c3 + m * 2 * a.ldc2 + a.ldc2);
+      }
+      if (a.sums) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sg[j] = lanes16_sum(sg[j]);
+          su[j] = lanes16_sum(su[j]);
+        }
+        // lanes li = 0 .. 3: both blocks of dg, then of du
+        f4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float one = li & 1 ? sg[j + 4] : sg[j], two = li & 1 ? su[j + 4] : su[j];
+          v[j] = li & 2 ? two : one;
+        }
+        const int32_t e = step * 32 + (li & 1) * 16 + lg * 4;
+        float *to = a.sums + ((int64_t)blockIdx.x * NW + wave) * 2 * a.ldc2;
+        if (li < 4 && e < a.ldc2) *(f4 *)(to + (li & 2 ? a.ldc2 : 0) + e) = v;
+      }
+#pragma unroll
+      for (int n = 0; n < OUT; ++n)
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+          const int r = lg * 4 + tr;
+          const uint32_t row = now + p * UP + r * ROW + (((2 * n + tc) ^ swap_k(r)) << 4) + tb;
+          const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)row);
+          // sixteen rows on, where the pieces are exchanged alike
+          const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((p4)(uintptr_t)(row + 16 * ROW));
+          const s8v w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+          for (int i = 0; i < MI; ++i) y[i][n] = mfma16<T>(w, p ? du[i] : dg[i], y[i][n]);
+        }
+    } else {
+#pragma unroll
+      for (int n = 0; n < OUT; ++n) {
+        const uint32_t row = now + DOWN + (n * 16 + li) * 64 + (lg & 1) * 8;
+        const s4v lo = *(p4)(uintptr_t)(row + (((lg >> 1) ^ swap_d(li)) << 4));
+        const s4v hi = *(p4)(uintptr_t)(row + (((2 + (lg >> 1)) ^ swap_d(li)) << 4));
+        const s8v w = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) y[i][n] = mfma16<T>(w, h[i], y[i][n]);
+      }
+    }
+    now = now + STAGE == bias ? lds : now + STAGE;
+  }
+  stage_barrier<0>();  // no load is under way when the workgroup ends
+
+  const int32_t width = GRAD ? a.K : a.K2;
+  const bool whole = a.ldc % 4 == 0 && (uintptr_t)a.c % 8 == 0;
+#pragma unroll
+  for (int n = 0; n < OUT; ++n) {
+    const int32_t c = n * 16 + lg * 4;
+    const f4 b = load4<T>(!GRAD && a.bias2 ? (const E *)a.bias2 + c : nullptr, width - c);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) {
+      const int64_t m = m0 + i * 16;
+      if (m < a.M) store4<T>((E *)a.c + m * a.ldc + c, y[i][n] + b, width - c, whole);
     }
   }
 }
@@ -613,9 +911,11 @@ __global__ __launch_bounds__(64 * NW) void gated_few(ProductArgs a) {
     if (m >= a.M) continue;
     if constexpr (GATE) {
       f4 h;
+      with_activation(a.act, [&](auto act) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        h[e] = c + e < a.N ? activate<false>(a.act, v[0][e], nullptr) * v[1][e] : 0.f;
+        for (int e = 0; e < 4; ++e)
+          h[e] = c + e < a.N ? activate<act.value, false>(v[0][e], nullptr) * v[1][e] : 0.f;
+      });
       if (c < a.ldc) store4<T>((E *)a.c + m * a.ldc + c, h, 4, true);
     } else {
       store4<T>((E *)a.c + m * a.ldc + c, v[0], a.N - c,
@@ -644,23 +944,29 @@ __global__ __launch_bounds__(64) void few_join(ProductArgs a, int32_t parts, int
 }
 
 // Sums of the parts of a product whose k were shared out: part [splits][M][ldp]
-// to 16-bit rows, those from c_rows on to c2.
+// to 16-bit rows, those from c_rows on to c2.  Sixteen waves share the parts of 64
+// quads of columns: 253 parts of 128 x 256 took 73 us with a thread to a quad.
 template <int T>
-__global__ __launch_bounds__(256) void join_parts(JoinArgs a) {
+__global__ __launch_bounds__(1024) void join_parts(JoinArgs a) {
   typedef elem_t<T> E;
+  __shared__ f4 sum[16][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t quads = a.ldp / 4, total = a.M * quads;
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total;
-       q += (int64_t)gridDim.x * 256) {
-    const int64_t m = q / quads;
-    const int32_t c = (int32_t)(q - m * quads) * 4;
-    const bool one = m < a.c_rows;
-    const int64_t r = one ? m : m - a.c_rows;
-    if (r >= a.c_valid) continue;
-    const float *p = a.part + m * a.ldp + c;
-    f4 v = f4{0.f, 0.f, 0.f, 0.f};
-    for (int32_t s = 0; s < a.splits; ++s) v += *(const f4 *)(p + s * a.M * a.ldp);
-    store4<T>((one ? (E *)a.c : (E *)a.c2) + r * a.ldc + c, v, a.N - c, false);
+  const int64_t q = (int64_t)blockIdx.x * 64 + lane;
+  f4 v = f4{0.f, 0.f, 0.f, 0.f};
+  if (q < total) {
+    const f4 *p = (const f4 *)a.part + q;
+#pragma unroll 4
+    for (int32_t s = wave; s < a.splits; s += 16) v += p[s * total];
   }
+  sum[wave][lane] = v;
+  __syncthreads();
+  const int64_t m = q / quads, r = m < a.c_rows ? m : m - a.c_rows;
+  const int32_t c = (int32_t)(q - m * quads) * 4;
+  if (wave || q >= total || r >= a.c_valid) return;
+  const int n = min(a.splits, 16);
+  for (int w = 1; w < n; ++w) v += sum[w][lane];
+  store4<T>((m < a.c_rows ? (E *)a.c : (E *)a.c2) + r * a.ldc + c, v, a.N - c, false);
 }
 
 template <int T, int WM, int WN, int MI, int NI, int S, bool AKS, bool BKS, int EPI>
@@ -672,8 +978,14 @@ hipError_t product_go(const ProductArgs &in, hipStream_t stream) {
   a.nt = (a.N + CN - 1) / CN;
   const int64_t grid = (int64_t)a.mt * a.nt * a.splits;
   if (grid * 64 * WM * WN >= (int64_t)1 << 32) return hipErrorInvalidConfiguration;
-  return launch_lds(gated_product<T, WM, WN, MI, NI, S, AKS, BKS, EPI>, dim3((unsigned)grid),
-                    dim3(64 * WM * WN), (TM + TN) * BK * 2 * S, stream, a);
+  auto go = [&](auto act) {
+    return launch_lds(gated_product<T, WM, WN, MI, NI, S, AKS, BKS, EPI, act.value>,
+                      dim3((unsigned)grid), dim3(64 * WM * WN), (TM + TN) * BK * 2 * S, stream, a);
+  };
+  if constexpr (EPI == EPI_GRAD)
+    return with_activation(a.act, go);
+  else
+    return go(std::integral_constant<int, ACT_SILU>{});
 }
 
 template <int T, bool AKS, bool BKS, int EPI>
@@ -704,6 +1016,23 @@ hipError_t product_t(const ProductArgs &a, int kind, int tile, hipStream_t strea
       if (a.splits > 1) return product_tile<T, true, true, EPI_PART>(a, tile, stream);
       return product_tile<T, true, true, EPI_ROWS>(a, tile, stream);
   }
+}
+
+template <int T, int KS, int NS, bool GRAD>
+hipError_t thin_go(const ProductArgs &a, hipStream_t stream) {
+  constexpr int MI = THIN_ROWS / 16 / THIN_WAVES;
+  const size_t lds = THIN_STAGES * (2 * 32 * KS * 64 + 8192) + (size_t)(a.N + 31) / 32 * 128;
+  const dim3 grid((unsigned)((a.M + THIN_ROWS - 1) / THIN_ROWS)), block(64 * THIN_WAVES);
+  return with_activation(a.act, [&](auto act) {
+    return launch_lds(gated_thin<T, MI, KS, NS, GRAD, act.value>, grid, block, lds, stream, a);
+  });
+}
+
+template <int T, bool GRAD>
+hipError_t thin_t(const ProductArgs &a, hipStream_t stream) {
+  if (a.K > 64)
+    return a.K2 > 64 ? thin_go<T, 4, 4, GRAD>(a, stream) : thin_go<T, 4, 2, GRAD>(a, stream);
+  return a.K2 > 64 ? thin_go<T, 2, 4, GRAD>(a, stream) : thin_go<T, 2, 2, GRAD>(a, stream);
 }
 
 template <int T, bool GATE, int MB, int NC>
@@ -782,11 +1111,22 @@ hipError_t launch_few(const ProductArgs &a, bool gate, int type, int splits, hip
   return gate ? few_t<T_F16, true>(a, 1, stream) : few_t<T_F16, false>(a, splits, stream);
 }
 
+bool thin_fits(int64_t M, int64_t K, int64_t H, int64_t N, int n_cu) {
+  return K <= 128 && N <= 128 && H <= THIN_HIDDEN && (M + THIN_ROWS - 1) / THIN_ROWS >= n_cu;
+}
+
+hipError_t launch_thin(const ProductArgs &a, bool grad, int type, hipStream_t stream) {
+  if (type == T_BF16)
+    return grad ? thin_t<T_BF16, true>(a, stream) : thin_t<T_BF16, false>(a, stream);
+  return grad ? thin_t<T_F16, true>(a, stream) : thin_t<T_F16, false>(a, stream);
+}
+
+int64_t thin_sum_rows(int64_t M) { return (M + THIN_ROWS - 1) / THIN_ROWS * THIN_WAVES; }
+
 hipError_t launch_join(const JoinArgs &a, int type, hipStream_t stream) {
-  const int64_t quads = a.M * (a.ldp / 4);
-  const dim3 grid((unsigned)std::min<int64_t>((quads + 255) / 256, 4096));
-  return type == T_BF16 ? launch(join_parts<T_BF16>, grid, dim3(256), 0, stream, a)
-                        : launch(join_parts<T_F16>, grid, dim3(256), 0, stream, a);
+  const dim3 grid((unsigned)((a.M * (a.ldp / 4) + 63) / 64));
+  return type == T_BF16 ? launch(join_parts<T_BF16>, grid, dim3(1024), 0, stream, a)
+                        : launch(join_parts<T_F16>, grid, dim3(1024), 0, stream, a);
 }
 
 }  // namespace gnn

@@ -468,11 +468,11 @@ struct ProductArgs {
   int32_t N = 0, K = 0, segs = 1;
   int32_t mt = 0, nt = 0;        // tiles (set by the launch)
   int32_t splits = 1, split_steps = INT32_MAX;
-  const void *bias[2] = {nullptr, nullptr};
+  const void *bias[2] = {nullptr, nullptr}, *bias2 = nullptr;
   // Rows: m < c_rows to c, the others to c2 (from row 0), each up to c_valid.
   // GATE, GRAD: h, ldc its padded width; GRAD's c2: [dg | du], 2 ldc wide.  Parts: fp32 [splits][M][ldc].
-  void *c = nullptr, *c2 = nullptr;
-  int64_t ldc = 0;
+  void *c = nullptr, *c2 = nullptr, *c3 = nullptr;
+  int64_t ldc = 0, ldc2 = 0;
   int64_t c_rows = INT64_MAX, c_valid = INT64_MAX;
   float *part = nullptr;         // few rows: sums of workgroups that share their k
   float *sums = nullptr;         // GRAD: column sums [row tiles * waves of m][2 ldc]
@@ -504,6 +504,14 @@ inline size_t few_part_bytes(int64_t M, int64_t N, int splits) {
                            (M <= 16 ? 1 : FEW_COLUMNS) * 1024;
 }
 hipError_t launch_few(const ProductArgs &a, bool gate, int type, int splits, hipStream_t stream);
+// A whole narrow block in one pass: b the gate's and up projection's weights, b2 the
+// down projection's [K2][N], N hidden elements, bias2 the down projection's; x at any
+// address.  From as many tiles of THIN_ROWS as there are CUs.
+constexpr int THIN_ROWS = 128;
+bool thin_fits(int64_t M, int64_t K, int64_t H, int64_t N, int n_cu);
+// grad: c is dx, c2 h and c3 [dg | du], ldc2 h's padded width; a[1] and lda2 are dy's.
+hipError_t launch_thin(const ProductArgs &a, bool grad, int type, hipStream_t stream);
+int64_t thin_sum_rows(int64_t M);  // rows of `sums` that it writes
 struct JoinArgs {
   const float *part = nullptr;   // [splits][M][ldp]
   int32_t splits = 1;

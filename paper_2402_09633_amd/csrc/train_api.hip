@@ -281,7 +281,7 @@ bool lies_aligned(const void *p, int64_t stride) {
 }
 
 struct GatedForward {
-  bool few = false;
+  bool few = false, thin = false;
   Operand x, gate, up, down;
   size_t h = 0, part = 0;
   int splits = 1;
@@ -296,6 +296,9 @@ struct GatedForward {
     if (few && n > 0) {
       splits = few_splits(n, d.out_features, d.hidden, n_cu);
       part = c.take(few_part_bytes(n, d.out_features, splits));
+    } else if ((thin = thin_fits(n, d.in_features, d.hidden, d.out_features, n_cu))) {
+      for (Operand *o : {&gate, &up, &down}) o->place(c);
+      return;
     } else {
       for (Operand *o : {&x, &gate, &up, &down}) o->place(c);
     }
@@ -306,6 +309,7 @@ struct GatedForward {
 struct GatedBackward {
   Operand x, dy, gate, up, down;
   ProductPlan grad, dx, dgu, dd;
+  bool thin = false;
   size_t h = 0, g = 0, part = 0, sums = 0, colsum = 0;
   int64_t sum_rows = 0;
   Carve c;
@@ -329,7 +333,8 @@ struct GatedBackward {
     if (dgu.splits > 1) most = (size_t)dgu.splits * 2 * hp * kp * 4;
     if (dd.splits > 1) most = std::max(most, (size_t)dd.splits * d.out_features * hp * 4);
     part = c.take(most);
-    sum_rows = product_sum_rows(grad.tile, n);
+    thin = thin_fits(n, d.in_features, d.hidden, d.out_features, n_cu);
+    sum_rows = thin ? thin_sum_rows(n) : product_sum_rows(grad.tile, n);
     sums = c.take((size_t)sum_rows * 2 * hp * 4);
     colsum = c.take(std::max(colsum_scratch(sum_rows, (int32_t)(2 * hp)),
                              colsum_scratch(n, d.out_features)));
@@ -381,8 +386,9 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   unsigned char *ws = (unsigned char *)workspace;
   const int t = d->dtype;
   const int64_t hp = up8(d->hidden);
+  if (!f.few && !f.thin && (rc = f.x.fetch(ws, t, stream))) return rc;
   if (!f.few)
-    for (Operand *o : {&f.x, &f.gate, &f.up, &f.down})
+    for (Operand *o : {&f.gate, &f.up, &f.down})
       if ((rc = o->fetch(ws, t, stream))) return rc;
   ProductArgs a;
   a.a[0] = f.x.p;
@@ -395,9 +401,18 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   a.K = d->in_features;
   a.bias[0] = w->gate_bias;
   a.bias[1] = w->up_bias;
+  a.act = d->activation;
+  if (f.thin) {
+    a.b2 = f.down.p;
+    a.ldb2 = f.down.stride;
+    a.K2 = d->out_features;
+    a.bias2 = w->down_bias;
+    a.c = y;
+    a.ldc = y_stride;
+    return launched(launch_thin(a, false, t, stream), "gated block");
+  }
   a.c = ws + f.h;
   a.ldc = hp;
-  a.act = d->activation;
   rc = launched(f.few ? launch_few(a, true, t, 1, stream)
                       : launch_product(a, PRODUCT_GATE, t,
                                        product_plan(PRODUCT_GATE, a.M, a.N, a.K, n_cu).tile, stream),
@@ -470,7 +485,16 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     b.ldc = hp;
     b.sums = dw->gate_bias || dw->up_bias ? (float *)(ws + f.sums) : nullptr;
     b.act = d->activation;
-    if ((rc = launched(launch_product(b, PRODUCT_GRAD, t, f.grad.tile, stream), "gate gradient")))
+    if (f.thin) {
+      b.c = dx;
+      b.ldc = dx_stride;
+      b.c2 = h;
+      b.c3 = g;
+      b.ldc2 = hp;
+      rc = launched(launch_thin(b, true, t, stream), "gated block's gradients");
+      if (rc) return rc;
+    }
+    if (!f.thin && (rc = launched(launch_product(b, PRODUCT_GRAD, t, f.grad.tile, stream), "gate gradient")))
       return rc;
     // dx = dg Wg + du Wu
     ProductArgs e;
@@ -486,7 +510,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     e.segs = 2;
     e.c = dx;
     e.ldc = dx_stride;
-    if ((rc = launched(launch_product(e, PRODUCT_ROWS, t, f.dx.tile, stream), "gradient of x")))
+    if (!f.thin && (rc = launched(launch_product(e, PRODUCT_ROWS, t, f.dx.tile, stream), "gradient of x")))
       return rc;
   }
   // The weights' gradients: the rows are the k.

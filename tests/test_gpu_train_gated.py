@@ -89,6 +89,28 @@ def test_few_rows_of_wide_blocks(G, m, k, h, n):
     assert torch.equal(G.gated(x, *w, biases=b), y)
 
 
+# Many rows of narrow blocks, whose forward pass is one kernel and whose backward pass
+# has one for dx, and sizes next to them.
+@pytest.mark.parametrize("k,h,n", [
+    (1, 1, 1), (8, 32, 8), (64, 64, 64), (65, 33, 63), (128, 512, 128), (127, 100, 65), (64, 31, 128),
+    (128, 2048, 64), (40, 2049, 40), (129, 64, 128), (128, 64, 129)])
+def test_many_narrow_rows(G, k, h, n):
+    for kind, act in ((torch.float16, "silu"), (torch.bfloat16, "gelu")):
+        x, w, b, dy = make(33_003, k, h, n, kind, k + h)
+        y, got = check(G, x, w, b, dy, act)
+        # the same bits in tables of odd rows, from odd addresses
+        out = torch.full((33_003, n + 3), 5.0, dtype=kind, device="cuda")
+        G.gated(wider(x, k + 2, 1), *w, biases=b, activation=act, out=out[:, 1:n + 1])
+        assert torch.equal(out[:, 1:n + 1], y)
+        assert (out[:, 0] == 5).all() and (out[:, n + 1:] == 5).all()
+        out.fill_(5.0)
+        wide = torch.full((33_003, k + 1), 5.0, dtype=kind, device="cuda")
+        back = G.gated_backward(wider(dy, n + 2, 1), wider(x, k + 2, 1), *w, biases=b,
+                                activation=act, out=wide[:, 1:])
+        assert all(torch.equal(p, q) for p, q in zip(back, got)) and (wide[:, 0] == 5).all()
+        check(G, x, w, [None] * 3, dy, act)
+
+
 def test_many_rows(G):
     check(G, *make(300_001, 32, 64, 32, torch.bfloat16, 1), "gelu")
 
