@@ -45,6 +45,16 @@ __device__ __forceinline__ float activate(float g, float *slope) {
     if (SLOPE) *slope = g > 0.f ? 1.f : 0.f;
     return g > 0.f || g != g ? g : 0.f;
   }
+  if constexpr (act == ACT_GELU && !SLOPE) {
+    // g Phi(g) = max(g, 0) - |g| Phi(-|g|)
+    const float t = __builtin_amdgcn_rcpf(1.f + 0.23164188f * fabsf(g));
+    const float e = __builtin_amdgcn_exp2f(g * g * -0.72134752f);
+    const float p = t * (0.127414796f +
+                         t * (-0.142248368f +
+                              t * (0.7107068705f + t * (-0.7265760135f + t * 0.5307027145f))));
+    // (the product has vanished long before 100, and an infinite g shall not undo that)
+    return __builtin_fmaf(-fminf(fabsf(g), 100.f), p * e, 0.5f * (g + fabsf(g)));
+  }
   if constexpr (act == ACT_GELU) {
     const float z = fabsf(g) * 0.70710678118654752f;
     const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * z);
@@ -560,7 +570,8 @@ gated_product(ProductArgs a) {
 // cores; GRAD by the rows that it writes.  Two workgroups of four waves to a CU run
 // out of step: 300000 x 128 -> 512 -> 128 bf16 240 us, one of eight waves 278, through
 // the products above 411.
-constexpr int THIN_STAGES = 3, THIN_WAVES = 4, THIN_HIDDEN = 2048;
+constexpr int THIN_WAVES = 4, THIN_HIDDEN = 2048;
+constexpr int thin_stages(bool grad) { return grad ? 3 : 2; }
 
 // The sum over the 16 lanes of one lg, in all of them.
 __device__ __forceinline__ float lanes16_sum(float v) {
@@ -577,7 +588,8 @@ __device__ __forceinline__ float lanes16_sum(float v) {
 
 // KS, NS: 32s of elements of x and of y (2 or 4).
 template <int T, int MI, int KS, int NS, bool GRAD, int ACT>
-__global__ __launch_bounds__(64 * THIN_WAVES, 2) void gated_thin(ProductArgs a) {
+__global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(ProductArgs a) {
+  constexpr int STAGES = thin_stages(GRAD);
   typedef elem_t<T> E;
   typedef E e4 __attribute__((ext_vector_type(4)));
   typedef typename Raw8<T>::vec e8;
@@ -590,7 +602,7 @@ __global__ __launch_bounds__(64 * THIN_WAVES, 2) void gated_thin(ProductArgs a) 
   constexpr int OUT = GRAD ? 2 * KS : 2 * NS;  // blocks of 16 of dx or y
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)shared;
-  const uint32_t bias = lds + THIN_STAGES * STAGE;
+  const uint32_t bias = lds + STAGES * STAGE;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
   const int32_t steps = (a.N + 31) / 32;  // N: hidden elements, K2: columns of y
@@ -663,14 +675,14 @@ __global__ __launch_bounds__(64 * THIN_WAVES, 2) void gated_thin(ProductArgs a) 
   __syncthreads();
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-  for (int s = 0; s < THIN_STAGES - 1; ++s) issue(s, lds + s * STAGE);
+  for (int s = 0; s < STAGES - 1; ++s) issue(s, lds + s * STAGE);
 
   uint32_t now = lds;
   for (int32_t step = 0; step < steps; ++step) {
     // Loads come back in their order, so this stage is here when no more operations
     // are under way than the next ones have loads, whatever the stores do.
-    stage_barrier<(THIN_STAGES - 2) * LOADS>();
-    issue(step + THIN_STAGES - 1, now == lds ? lds + (THIN_STAGES - 1) * STAGE : now - STAGE);
+    stage_barrier<(STAGES - 2) * LOADS>();
+    issue(step + STAGES - 1, now == lds ? lds + (STAGES - 1) * STAGE : now - STAGE);
     f4 sum[2][2][MI], dh[2][MI];  // g, u and dh of two blocks of 16 hidden elements
 #pragma unroll
     for (int p = 0; p < 2; ++p)
@@ -1021,7 +1033,7 @@ hipError_t product_t(const ProductArgs &a, int kind, int tile, hipStream_t strea
 template <int T, int KS, int NS, bool GRAD>
 hipError_t thin_go(const ProductArgs &a, hipStream_t stream) {
   constexpr int MI = THIN_ROWS / 16 / THIN_WAVES;
-  const size_t lds = THIN_STAGES * (2 * 32 * KS * 64 + 8192) + (size_t)(a.N + 31) / 32 * 128;
+  const size_t lds = thin_stages(GRAD) * (2 * 32 * KS * 64 + 8192) + (size_t)(a.N + 31) / 32 * 128;
   const dim3 grid((unsigned)((a.M + THIN_ROWS - 1) / THIN_ROWS)), block(64 * THIN_WAVES);
   return with_activation(a.act, [&](auto act) {
     return launch_lds(gated_thin<T, MI, KS, NS, GRAD, act.value>, grid, block, lds, stream, a);

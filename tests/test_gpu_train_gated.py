@@ -70,6 +70,32 @@ def test_activations(G, act, kind):
         check(G, *make(m, 96, 80, 64, KINDS[kind], 2, bias=False), act)
 
 
+@pytest.mark.parametrize("m", [30, 200, 33_000])
+def test_infinite_and_large_gates(G, m):
+    """One hidden element whose gate is x, up 1 and down 1: y is act(x)."""
+    x = torch.tensor([float("inf"), -float("inf"), float("nan"), 60000.0, -60000.0, 90.0, -90.0,
+                      12.0, -12.0, 0.0, -0.0, 3e-5, -3e-5, 1.0, -1.0], device="cuda").half()
+    x = x.repeat(m // 15 + 1)[:m]
+    x = torch.stack([x, torch.ones_like(x)], 1).contiguous()
+    x[x[:, 0].isinf() | x[:, 0].isnan(), 1] = 1.0
+    wg = torch.tensor([[1.0, 0.0]], device="cuda").half()
+    wu, wd = torch.zeros_like(wg), torch.ones(1, 1, device="cuda").half()
+    bu = torch.ones(1, device="cuda").half()
+    plain = {"silu": torch.nn.functional.silu, "gelu": torch.nn.functional.gelu,
+             "sigmoid": torch.sigmoid, "relu": torch.relu}
+    fine = x[:, 0].isfinite()
+    for name, f in plain.items():
+        y = G.gated(x, wg, wu, wd, biases=(None, bu, None), activation=name)[:, 0]
+        want = f(x[:, 0].double())
+        assert y[fine].isfinite().all()
+        # two roundings to 16 bits, and the kernel's activation
+        bound = R.act(name, x[fine, 0].double())[2]
+        off = (y[fine].double() - want[fine]).abs()
+        assert (off <= 2 * R.stored(want[fine], bound, torch.float16)).all()
+        # 0 * inf in the up projection
+        assert y[~fine].isnan().all()
+
+
 # Sizes that reach the wide tiles, whole and with an end in either direction, and
 # sums over rows in several parts.
 @pytest.mark.parametrize("m,k,h,n", [
