@@ -1014,7 +1014,7 @@ hipError_t product_tile(const ProductArgs &a, int tile, hipStream_t stream) {
   }
   if (tile == TILE_256x128) return product_go<T, 4, 2, 4, 4, 3, AKS, BKS, EPI>(a, stream);
   if (tile == TILE_128) return product_go<T, 2, 2, 4, 4, 2, AKS, BKS, EPI>(a, stream);
-  return product_go<T, 2, 2, 4, 4, 4, AKS, BKS, EPI>(a, stream);
+  return product_go<T, 4, 2, 2, 4, 4, AKS, BKS, EPI>(a, stream);
 }
 
 template <int T>
@@ -1077,17 +1077,33 @@ ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu) {
     if (dual) tn /= 2;
     return ((M + tm - 1) / tm) * ((N + tn - 1) / tn);
   };
-  const int64_t wide = dual ? 2 * N : N;
-  if (wide > 128 && M > 128 && (tiles(256, 256) >= n_cu || kind == PRODUCT_WEIGHTS))
-    p.tile = TILE_256;
-  else if (M > 128 && (tiles(256, 128) >= n_cu || kind == PRODUCT_WEIGHTS))
-    p.tile = TILE_256x128;
-  else
-    p.tile = TILE_128;
-  const int64_t tm = p.tile == TILE_128 ? 128 : 256, tn = p.tile == TILE_256 ? 256 : 128;
+  // The tile whose rounds over the chip take least, by the time of a stage next to
+  // that of two workgroups of 128 x 128 on a CU (COST).
+  static constexpr struct {
+    int tile, tm, tn, to_cu;
+    double cost;
+  } all[] = {{TILE_256, 256, 256, 1, 1.6},
+             {TILE_256x128, 256, 128, 1, 1.0},
+             {TILE_128, 128, 128, 2, 1.0},
+             {TILE_128_DEEP, 128, 128, 1, 0.6}};
+  const int64_t steps = (K + BK - 1) / BK;
+  double best = 0.0;
+  for (const auto &t : all) {
+    const int64_t n = tiles(t.tm, t.tn), slots = (int64_t)t.to_cu * n_cu;
+    // the weights' gradients share out their k, and fill the chip that way
+    const double rounds = kind == PRODUCT_WEIGHTS && n < slots
+                              ? std::max((double)n / slots, 8.0 / std::max<int64_t>(steps, 8))
+                              : (double)((n + slots - 1) / slots);
+    if (best == 0.0 || rounds * t.cost < best) {
+      best = rounds * t.cost;
+      p.tile = t.tile;
+    }
+  }
+  const bool small = p.tile == TILE_128 || p.tile == TILE_128_DEEP;
+  const int64_t tm = small ? 128 : 256, tn = p.tile == TILE_256 ? 256 : 128;
   if (kind == PRODUCT_WEIGHTS) {
     // as many parts as fill the chip, of eight stages at least
-    const int64_t steps = (K + BK - 1) / BK, n = tiles(tm, tn);
+    const int64_t n = tiles(tm, tn);
     const int64_t fill = p.tile == TILE_128 ? 2 * (int64_t)n_cu : n_cu;
     int64_t s = std::min(fill / n, steps / 8);
     if (s < 1) s = 1;
@@ -1097,8 +1113,6 @@ ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu) {
     p.splits = 1;
     p.split_steps = INT32_MAX;
   }
-  // one workgroup to a CU at most: more stages on their way in place of a second one
-  if (p.tile == TILE_128 && tiles(128, 128) * p.splits <= n_cu) p.tile = TILE_128_DEEP;
   return p;
 }
 

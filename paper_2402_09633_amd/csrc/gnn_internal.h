@@ -486,7 +486,7 @@ ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu);
 // Rows of `sums` that a GRAD product writes.
 inline int64_t product_sum_rows(int tile, int64_t M) {
   const int64_t tm = tile == TILE_128 || tile == TILE_128_DEEP ? 128 : 256;
-  return (M + tm - 1) / tm * (tile == TILE_256x128 ? 4 : 2);
+  return (M + tm - 1) / tm * (tile == TILE_256x128 || tile == TILE_128_DEEP ? 4 : 2);
 }
 hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hipStream_t stream);
 // Up to FEW_ROWS rows; operands of any alignment (GATE or DOWN).
