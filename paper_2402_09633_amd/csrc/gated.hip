@@ -38,7 +38,7 @@ __device__ __forceinline__ f4 mfma16(const s8v &a, const s8v &b, const f4 &c) {
 // ---- activations ----
 // act(g) and its derivative.  gelu is g Phi(g); 1 - erf(z) for z >= 0 is taken
 // as t P(t) exp(-z^2), t = 1 / (1 + 0.3275911 z) (Abramowitz and Stegun, 7.1.26;
-// off by at most 1.5e-7, a hundredth of a 16-bit number's last place at 1).
+// off by at most 1.5e-7, a 6000th of the last place of an fp16 number next to 1).
 template <int act, bool SLOPE>
 __device__ __forceinline__ float activate(float g, float *slope) {
   if constexpr (act == ACT_RELU) {
@@ -102,7 +102,7 @@ __device__ __forceinline__ void load_lds(uint32_t lds, uint32_t off, const i4 &b
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                :
                : "s"(lds), "v"(off), "s"(buf)
-               : "memory");
+               : "memory", "m0");
 }
 // All but the last N loads of this wave have come, and all waves are here.
 template <int N>
@@ -955,6 +955,26 @@ __global__ __launch_bounds__(64) void few_join(ProductArgs a, int32_t parts, int
   store4<T>((E *)a.c + m * a.ldc + c, v, a.N - c, a.ldc % 4 == 0 && (uintptr_t)a.c % 8 == 0);
 }
 
+// Tables that the products cannot read as they lie (at odd addresses, or with rows
+// of odd lengths) to aligned rows with zeros behind them, all in one launch (63 x 65
+// -> 523 -> 8 forward and backward: 50 us, with a launch to each 60).
+template <int T>
+__global__ __launch_bounds__(256) void pack_tables(PackArgs a) {
+  typedef elem_t<T> E;
+  typedef typename Raw8<T>::vec e8;
+  int t = 0;
+  while (t + 1 < a.count && blockIdx.x >= (uint32_t)a.first[t + 1]) ++t;
+  const int64_t units = (a.width[t] + 7) / 8, total = a.rows[t] * units;
+  const int64_t blocks = a.first[t + 1] - a.first[t];
+  for (int64_t u = (blockIdx.x - a.first[t]) * 256 + threadIdx.x; u < total; u += blocks * 256) {
+    const int64_t r = u / units;
+    const int k = (int)(u - r * units) * 8;
+    const E *row = (const E *)a.x[t] + r * a.stride[t];
+    const Raw8<T> v = k + 8 <= a.width[t] ? load8<T>(row, k) : load8_end<T>(row, k, a.width[t]);
+    *(e8 *)((E *)a.y[t] + u * 8) = v.v;
+  }
+}
+
 // Sums of the parts of a product whose k were shared out: part [splits][M][ldp]
 // to 16-bit rows, those from c_rows on to c2.  Sixteen waves share the parts of 64
 // quads of columns: 253 parts of 128 x 256 took 73 us with a thread to a quad.
@@ -1148,6 +1168,18 @@ hipError_t launch_thin(const ProductArgs &a, bool grad, int type, hipStream_t st
 }
 
 int64_t thin_sum_rows(int64_t M) { return (M + THIN_ROWS - 1) / THIN_ROWS * THIN_WAVES; }
+
+hipError_t launch_pack(PackArgs a, int type, hipStream_t stream) {
+  a.first[0] = 0;
+  for (int t = 0; t < a.count; ++t) {
+    const int64_t units = a.rows[t] * ((a.width[t] + 7) / 8);
+    a.first[t + 1] = a.first[t] + (int32_t)std::min<int64_t>((units + 255) / 256, 8192);
+  }
+  if (a.first[a.count] == 0) return hipSuccess;
+  const dim3 grid((unsigned)a.first[a.count]);
+  return type == T_BF16 ? launch(pack_tables<T_BF16>, grid, dim3(256), 0, stream, a)
+                        : launch(pack_tables<T_F16>, grid, dim3(256), 0, stream, a);
+}
 
 hipError_t launch_join(const JoinArgs &a, int type, hipStream_t stream) {
   const dim3 grid((unsigned)((a.M * (a.ldp / 4) + 63) / 64));

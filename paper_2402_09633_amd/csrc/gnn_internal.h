@@ -512,6 +512,16 @@ bool thin_fits(int64_t M, int64_t K, int64_t H, int64_t N, int n_cu);
 // grad: c is dx, c2 h and c3 [dg | du], ldc2 h's padded width; a[1] and lda2 are dy's.
 hipError_t launch_thin(const ProductArgs &a, bool grad, int type, hipStream_t stream);
 int64_t thin_sum_rows(int64_t M);  // rows of `sums` that it writes
+// Up to five tables of 16-bit rows to aligned rows of a multiple of eight elements.
+struct PackArgs {
+  const void *x[5];
+  void *y[5];
+  int64_t stride[5], rows[5];
+  int32_t width[5];
+  int32_t first[6];  // first workgroup of each (set by the launch)
+  int32_t count = 0;
+};
+hipError_t launch_pack(PackArgs a, int type, hipStream_t stream);
 struct JoinArgs {
   const float *part = nullptr;   // [splits][M][ldp]
   int32_t splits = 1;

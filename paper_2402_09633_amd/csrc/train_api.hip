@@ -260,19 +260,16 @@ struct Operand {
   void place(Carve &c) {
     if (copy) at = c.take((size_t)rows * up8(width) * 2);
   }
-  int fetch(unsigned char *ws, int type, hipStream_t stream) {
-    if (!copy) return GNN_OK;
-    ConvertArgs a;
-    a.x = p;
-    a.x_type = a.y_type = type;
-    a.x_stride = stride;
-    a.n = rows;
-    a.K = width;
-    a.pad = (int)up8(width);
-    a.y = ws + at;
-    p = a.y;
-    stride = a.pad;
-    return rows ? launched(launch_convert(a, stream), "row copy") : GNN_OK;
+  // What the products read from here on, and what has to be copied for it.
+  void fetch(unsigned char *ws, PackArgs *a) {
+    if (!copy) return;
+    a->x[a->count] = p;
+    a->y[a->count] = ws + at;
+    a->stride[a->count] = stride;
+    a->rows[a->count] = rows;
+    a->width[a->count++] = width;
+    p = ws + at;
+    stride = up8(width);
   }
 };
 
@@ -386,10 +383,11 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   unsigned char *ws = (unsigned char *)workspace;
   const int t = d->dtype;
   const int64_t hp = up8(d->hidden);
-  if (!f.few && !f.thin && (rc = f.x.fetch(ws, t, stream))) return rc;
+  PackArgs pack;
+  if (!f.few && !f.thin) f.x.fetch(ws, &pack);
   if (!f.few)
-    for (Operand *o : {&f.gate, &f.up, &f.down})
-      if ((rc = o->fetch(ws, t, stream))) return rc;
+    for (Operand *o : {&f.gate, &f.up, &f.down}) o->fetch(ws, &pack);
+  if ((rc = launched(launch_pack(pack, t, stream), "row copy"))) return rc;
   ProductArgs a;
   a.a[0] = f.x.p;
   a.lda = f.x.stride;
@@ -459,8 +457,9 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
   unsigned char *ws = (unsigned char *)workspace;
   const int t = d->dtype;
   const int64_t hp = up8(d->hidden);
-  for (Operand *o : {&f.x, &f.dy, &f.gate, &f.up, &f.down})
-    if ((rc = o->fetch(ws, t, stream))) return rc;
+  PackArgs pack;
+  for (Operand *o : {&f.x, &f.dy, &f.gate, &f.up, &f.down}) o->fetch(ws, &pack);
+  if ((rc = launched(launch_pack(pack, t, stream), "row copy"))) return rc;
   void *h = ws + f.h, *g = ws + f.g;
   if (n_rows > 0) {
     // g and u again, and dh; from them h, dg and du
