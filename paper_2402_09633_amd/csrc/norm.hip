@@ -318,7 +318,12 @@ hipError_t ln_go(const LayerNormArgs &a, int L, bool backward, hipStream_t strea
                       dim3((unsigned)layer_norm_parts(a.n, a.width)), block, lds, stream, a, L);
   }
   const int64_t rows = WIDE ? 1 : LN_WAVES * (64 / L);
-  const int64_t grid = std::min<int64_t>((a.n + rows - 1) / rows, 256 * (WIDE ? 4 : 16));
+  // four rows to a wave before there are more than 1024 workgroups: gamma and beta
+  // are loaded once for all of them
+  const int64_t all = (a.n + rows - 1) / rows;
+  const int64_t grid =
+      WIDE ? std::min<int64_t>(all, 1024)
+           : std::min<int64_t>(all, std::min<int64_t>(4096, std::max<int64_t>(1024, all / 4)));
   return launch(layer_norm<T, C, WIDE, FULL>, dim3((unsigned)grid), block, 0, stream, a, L);
 }
 
