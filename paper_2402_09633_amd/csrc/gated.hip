@@ -267,6 +267,8 @@ gated_product(ProductArgs a) {
   typedef Staged<TN, NW, BKS> SB;
   constexpr int STAGE = SA::BYTES + SB::BYTES;
   typedef elem_t<T> E;
+  // WEIGHTS of tiles whose sums leave room: also sums of A over k, by MFMAs with ones
+  constexpr bool SUMS = AKS && MI * NI <= 16;
   constexpr bool AHEAD = !(NW == 8 && MI * NI >= 32 && EPI == EPI_GRAD);
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)shared;
@@ -377,6 +379,18 @@ gated_product(ProductArgs a) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
+  f4 over_k[SUMS ? MI : 1];
+  const bool sums = SUMS && a.sums && tn == 0 && wn == 0;
+  typedef E e8v __attribute__((ext_vector_type(8)));
+  const s8v ones = __builtin_bit_cast(s8v, e8v{1, 1, 1, 1, 1, 1, 1, 1});
+#pragma unroll
+  for (f4 &v : over_k) v = f4{0.f, 0.f, 0.f, 0.f};
+  auto add_up = [&](const s8v(&xa)[MI]) {
+    if constexpr (SUMS)
+      if (sums)
+#pragma unroll
+        for (int i = 0; i < MI; ++i) over_k[i] = mfma16<T>(ones, xa[i], over_k[i]);
+  };
   constexpr int HN = NI / 2;
   f4 third[EPI == EPI_GRAD ? MI : 1][EPI == EPI_GRAD ? HN : 1];
   if (first < end) {
@@ -424,12 +438,14 @@ gated_product(ProductArgs a) {
         half_stage<T, MI, N, 0>(
             sum, xa, xb, ya, yb, [&](int i) { return fa.load(now, i, 1); },
             [&](int j) { return fb.load(now + SA::BYTES, j, 1); }, [](int) {});
+        add_up(xa);
         stage_barrier<(S - 2) * LOADS>();
         const Coming c = coming(step + S, now);
         // after the last of these stages, what is read here is not used
         half_stage<T, MI, N, LOADS>(
             sum, ya, yb, xa, xb, [&](int i) { return fa.load(next, i, 0); },
             [&](int j) { return fb.load(next + SA::BYTES, j, 0); }, [&](int d) { load(d, c); });
+        add_up(ya);
         now = next;
       }
     };
@@ -452,15 +468,20 @@ gated_product(ProductArgs a) {
   // the block's.
   const int li = lane & 15, lg = lane >> 4;
   const int64_t mw = m0 + wm * MI * 16 + li;
+  if constexpr (SUMS) {
+    if (sums && lg == 0)
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        if (mw + i * 16 < a.M) a.sums[split * a.M + mw + i * 16] = over_k[i][0];
+  }
   if constexpr (DUAL) {
     const int32_t c0 = n0 + wn * HN * 16 + lg * 4;
-    f4 bg[HN], bu[HN], sg[HN], su[HN];
+    f4 bg[HN], bu[HN];
 #pragma unroll
     for (int j = 0; j < HN; ++j) {
       const int32_t c = c0 + j * 16;
       bg[j] = load4<T>((const E *)a.bias[0] ? (const E *)a.bias[0] + c : nullptr, a.N - c);
       bu[j] = load4<T>((const E *)a.bias[1] ? (const E *)a.bias[1] + c : nullptr, a.N - c);
-      sg[j] = su[j] = f4{0.f, 0.f, 0.f, 0.f};
     }
     auto elements = [&](auto which) {
       constexpr int A = which.value;
@@ -489,8 +510,6 @@ gated_product(ProductArgs a) {
                 dg[v] = dh[v] * u[v] * slope;
                 du[v] = dh[v] * s;
               }
-              sg[j] += dg;
-              su[j] += du;
               E *pd = (E *)a.c2 + m * 2 * a.ldc + c;
               store4<T>(ph, h, 4, true);
               store4<T>(pd, dg, 4, true);
@@ -504,26 +523,6 @@ gated_product(ProductArgs a) {
       elements(std::integral_constant<int, ACT>{});
     else
       with_activation(a.act, elements);
-    // Column sums of dg and du over the wave's rows (the biases' gradients),
-    // from the numbers before they are rounded.
-    if (EPI == EPI_GRAD && a.sums) {
-      float *ps = a.sums + ((int64_t)tm * WM + wm) * 2 * a.ldc;
-#pragma unroll
-      for (int j = 0; j < HN; ++j) {
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int o = 1; o < 16; o *= 2) {
-            sg[j][v] += __shfl_xor(sg[j][v], o);
-            su[j][v] += __shfl_xor(su[j][v], o);
-          }
-        const int32_t c = c0 + j * 16;
-        if (li == 0 && c < a.ldc) {
-          *(f4 *)(ps + c) = sg[j];
-          *(f4 *)(ps + a.ldc + c) = su[j];
-        }
-      }
-    }
   } else if constexpr (EPI == EPI_PART) {
     float *part = (float *)a.c + (int64_t)split * a.M * a.ldc;
 #pragma unroll
@@ -572,19 +571,6 @@ gated_product(ProductArgs a) {
 // the products above 411.
 constexpr int THIN_WAVES = 4, THIN_HIDDEN = 2048;
 constexpr int thin_stages(bool grad) { return grad ? 3 : 2; }
-
-// The sum over the 16 lanes of one lg, in all of them.
-__device__ __forceinline__ float lanes16_sum(float v) {
-  auto other = [](float x, auto ctrl) {
-    return __uint_as_float(
-        __builtin_amdgcn_mov_dpp(__float_as_uint(x), ctrl.value, 0xf, 0xf, true));
-  };
-  v += other(v, std::integral_constant<int, 0xb1>{});   // lane ^ 1
-  v += other(v, std::integral_constant<int, 0x4e>{});   // lane ^ 2
-  v += other(v, std::integral_constant<int, 0x141>{});  // 7 - lane of 8
-  v += other(v, std::integral_constant<int, 0x140>{});  // 15 - lane of 16
-  return v;
-}
 
 // KS, NS: 32s of elements of x and of y (2 or 4).
 template <int T, int MI, int KS, int NS, bool GRAD, int ACT>
@@ -725,11 +711,9 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
       }
     }
     s8v h[MI], dg[MI], du[MI];
-    f8 sg = f8{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, su = sg;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       f8 v, vg, vu;
-      const bool in = m0 + i * 16 < a.M;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float g = sum[0][j / 4][i][j % 4], u = sum[1][j / 4][i][j % 4];
@@ -739,10 +723,6 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
           v[j] = s * u;
           vg[j] = d * u * slope;
           vu[j] = d * s;
-          if (in) {
-            sg[j] += vg[j];
-            su[j] += vu[j];
-          }
         } else {
           v[j] = activate<ACT, false>(g, nullptr) * u;
         }
@@ -773,23 +753,6 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
         store(h[i], (E *)a.c2 + m * a.ldc2);
         store(dg[i], (E *)a.c3 + m * 2 * a.ldc2);
         store(du[i], (E *)a.c3 + m * 2 * a.ldc2 + a.ldc2);
-      }
-      if (a.sums) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          sg[j] = lanes16_sum(sg[j]);
-          su[j] = lanes16_sum(su[j]);
-        }
-        // lanes li = 0 .. 3: both blocks of dg, then of du
-        f4 v;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float one = li & 1 ? sg[j + 4] : sg[j], two = li & 1 ? su[j + 4] : su[j];
-          v[j] = li & 2 ? two : one;
-        }
-        const int32_t e = step * 32 + (li & 1) * 16 + lg * 4;
-        float *to = a.sums + ((int64_t)blockIdx.x * NW + wave) * 2 * a.ldc2;
-        if (li < 4 && e < a.ldc2) *(f4 *)(to + (li & 2 ? a.ldc2 : 0) + e) = v;
       }
 #pragma unroll
       for (int n = 0; n < OUT; ++n)
@@ -1166,8 +1129,6 @@ hipError_t launch_thin(const ProductArgs &a, bool grad, int type, hipStream_t st
     return grad ? thin_t<T_BF16, true>(a, stream) : thin_t<T_BF16, false>(a, stream);
   return grad ? thin_t<T_F16, true>(a, stream) : thin_t<T_F16, false>(a, stream);
 }
-
-int64_t thin_sum_rows(int64_t M) { return (M + THIN_ROWS - 1) / THIN_ROWS * THIN_WAVES; }
 
 hipError_t launch_pack(PackArgs a, int type, hipStream_t stream) {
   a.first[0] = 0;

@@ -475,7 +475,7 @@ struct ProductArgs {
   int64_t ldc = 0, ldc2 = 0;
   int64_t c_rows = INT64_MAX, c_valid = INT64_MAX;
   float *part = nullptr;         // few rows: sums of workgroups that share their k
-  float *sums = nullptr;         // GRAD: column sums [row tiles * waves of m][2 ldc]
+  float *sums = nullptr;         // WEIGHTS (product_sums): sums of A over k [splits][M]
   int32_t act = 0;
 };
 struct ProductPlan {
@@ -483,11 +483,8 @@ struct ProductPlan {
   int32_t splits = 1, split_steps = INT32_MAX;
 };
 ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu);
-// Rows of `sums` that a GRAD product writes.
-inline int64_t product_sum_rows(int tile, int64_t M) {
-  const int64_t tm = tile == TILE_128 || tile == TILE_128_DEEP ? 128 : 256;
-  return (M + tm - 1) / tm * (tile == TILE_256x128 || tile == TILE_128_DEEP ? 4 : 2);
-}
+// Whether a WEIGHTS product also gives the sums of A over k.
+inline bool product_sums(int tile) { return tile != TILE_256; }
 hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hipStream_t stream);
 // Up to FEW_ROWS rows; operands of any alignment (GATE or DOWN).
 constexpr int FEW_ROWS = 64;
@@ -511,7 +508,6 @@ constexpr int THIN_ROWS = 128;
 bool thin_fits(int64_t M, int64_t K, int64_t H, int64_t N, int n_cu);
 // grad: c is dx, c2 h and c3 [dg | du], ldc2 h's padded width; a[1] and lda2 are dy's.
 hipError_t launch_thin(const ProductArgs &a, bool grad, int type, hipStream_t stream);
-int64_t thin_sum_rows(int64_t M);  // rows of `sums` that it writes
 // Up to five tables of 16-bit rows to aligned rows of a multiple of eight elements.
 struct PackArgs {
   const void *x[5];
