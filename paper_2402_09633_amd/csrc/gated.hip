@@ -207,6 +207,30 @@ __device__ __forceinline__ f4 load4(const elem_t<T> *p, int32_t n) {
   return v;
 }
 
+// Sixteen values of each of 16 neighbouring lanes: lane i's result is the sum of
+// value i over the 16.  Every step trades half of the values that are left.
+__device__ __forceinline__ float sums16(const float (&v)[16]) {
+  const int li = threadIdx.x & 15;
+  float w[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) w[j] = v[j];
+  auto step = [&](auto half, auto ctrl) {
+    constexpr int H = half.value;
+    const bool up = li & H;
+#pragma unroll
+    for (int j = 0; j < H; ++j) {
+      const float mine = up ? w[j + H] : w[j], theirs = up ? w[j] : w[j + H];
+      w[j] = mine + __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(theirs), ctrl.value,
+                                                             0xf, 0xf, true));
+    }
+  };
+  step(std::integral_constant<int, 8>{}, std::integral_constant<int, 0x140>{});  // 15 - lane of 16
+  step(std::integral_constant<int, 4>{}, std::integral_constant<int, 0x141>{});  // 7 - lane of 8
+  step(std::integral_constant<int, 2>{}, std::integral_constant<int, 0x4e>{});   // lane ^ 2
+  step(std::integral_constant<int, 1>{}, std::integral_constant<int, 0xb1>{});   // lane ^ 1
+  return w[0];
+}
+
 // ---- the product ----
 // Half a stage (k of one MFMA) of a wave's blocks, while the operands of the next
 // half come from LDS and, in every second half, a stage from memory: loads stand
@@ -477,6 +501,10 @@ gated_product(ProductArgs a) {
   if constexpr (DUAL) {
     const int32_t c0 = n0 + wn * HN * 16 + lg * 4;
     f4 bg[HN], bu[HN];
+    float over_m[16];  // GRAD: dg, then du of the lane's columns, over its rows
+    static_assert(EPI != EPI_GRAD || HN == 2, "sums16");
+#pragma unroll
+    for (float &v : over_m) v = 0.f;
 #pragma unroll
     for (int j = 0; j < HN; ++j) {
       const int32_t c = c0 + j * 16;
@@ -509,6 +537,8 @@ gated_product(ProductArgs a) {
                 h[v] = s * u[v];
                 dg[v] = dh[v] * u[v] * slope;
                 du[v] = dh[v] * s;
+                over_m[j * 4 + v] += dg[v];
+                over_m[8 + j * 4 + v] += du[v];
               }
               E *pd = (E *)a.c2 + m * 2 * a.ldc + c;
               store4<T>(ph, h, 4, true);
@@ -523,6 +553,14 @@ gated_product(ProductArgs a) {
       elements(std::integral_constant<int, ACT>{});
     else
       with_activation(a.act, elements);
+    // Sums over the wave's rows (for the biases' gradients), from the numbers before
+    // they are rounded.
+    if (EPI == EPI_GRAD && a.sums) {
+      const float v = sums16(over_m);
+      const int32_t c = n0 + wn * HN * 16 + ((li >> 2) & 1) * 16 + lg * 4 + (li & 3);
+      if (c < a.ldc)
+        a.sums[((int64_t)tm * WM + wm) * 2 * a.ldc + (li >> 3) * a.ldc + c] = v;
+    }
   } else if constexpr (EPI == EPI_PART) {
     float *part = (float *)a.c + (int64_t)split * a.M * a.ldc;
 #pragma unroll
@@ -565,10 +603,12 @@ gated_product(ProductArgs a) {
 // memory for the weights' gradients, and dx from dg and du as y from h; Wd, Wg and
 // Wu are read from the same places by transposing reads.
 //
-// Bound by the activation's instructions and the LDS reads more than by the matrix
-// cores; GRAD by the rows that it writes.  Two workgroups of four waves to a CU run
-// out of step: 300000 x 128 -> 512 -> 128 bf16 240 us, one of eight waves 278, through
-// the products above 411.
+// Bound by the activation's instructions (half of the issue slots of 300000 x 128 ->
+// 512 -> 128 bf16 gelu; MFMAs a fifth); GRAD also by the rows that it writes, 2.3 GB
+// for 1000513 x 128 -> 256 -> 128.  Workgroups of four waves, three to a CU (GRAD: two)
+// run out of step and cover one another's waits: 188 us for the former, 240 with two,
+// 278 with one of eight waves, 411 through the products above.  GRAD of the latter
+// takes 700, the products 1093.
 constexpr int THIN_WAVES = 4, THIN_HIDDEN = 2048;
 constexpr int thin_stages(bool grad) { return grad ? 3 : 2; }
 
@@ -711,6 +751,9 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
       }
     }
     s8v h[MI], dg[MI], du[MI];
+    float over_m[16];  // dg, then du of the lane's columns, over its rows
+#pragma unroll
+    for (float &v : over_m) v = 0.f;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       f8 v, vg, vu;
@@ -723,6 +766,10 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
           v[j] = s * u;
           vg[j] = d * u * slope;
           vu[j] = d * s;
+          if (m0 + i * 16 < a.M) {
+            over_m[j] += vg[j];
+            over_m[8 + j] += vu[j];
+          }
         } else {
           v[j] = activate<ACT, false>(g, nullptr) * u;
         }
@@ -753,6 +800,12 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
         store(h[i], (E *)a.c2 + m * a.ldc2);
         store(dg[i], (E *)a.c3 + m * 2 * a.ldc2);
         store(du[i], (E *)a.c3 + m * 2 * a.ldc2 + a.ldc2);
+      }
+      if (a.sums) {
+        const float v = sums16(over_m);
+        const int32_t e = step * 32 + ((li >> 2) & 1) * 16 + lg * 4 + (li & 3);
+        if (e < a.ldc2)
+          a.sums[((int64_t)blockIdx.x * NW + wave) * 2 * a.ldc2 + (li >> 3) * a.ldc2 + e] = v;
       }
 #pragma unroll
       for (int n = 0; n < OUT; ++n)
@@ -986,9 +1039,11 @@ hipError_t product_go(const ProductArgs &in, hipStream_t stream) {
 template <int T, bool AKS, bool BKS, int EPI>
 hipError_t product_tile(const ProductArgs &a, int tile, hipStream_t stream) {
   // Four waves of 128 x 128 read least from LDS, eight of 128 x 64 hide more.  Two
-  // projections of 8192 x 2048 -> 8192 take 523 us with eight, 610 with four; the
+  // projections of 8192 x 2048 -> 8192 take 512 us with eight, 610 with four; the
   // gradients of their weights and rows, whose LDS reads are twice as many, 458 and
-  // 452 with four, 580 and 534 with eight.
+  // 452 with four, 580 and 534 with eight.  GRAD takes 890 to 1030 so (0.8 to 0.93
+  // PFLOP/s, its operands read just before their use), 1105 in tiles of 256 x 128 with
+  // operands ahead.
   if (tile == TILE_256) {
     if constexpr (EPI == EPI_ROWS && BKS)
       return product_go<T, 2, 2, 8, 8, 2, AKS, BKS, EPI>(a, stream);
@@ -1060,8 +1115,14 @@ ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu) {
     if (dual) tn /= 2;
     return ((M + tm - 1) / tm) * ((N + tn - 1) / tn);
   };
-  // The tile whose rounds over the chip take least, by the time of a stage next to
-  // that of two workgroups of 128 x 128 on a CU (COST).
+  // The tile whose rounds over the chip take least; a round's cost is next to that of
+  // two workgroups of 128 x 128 on a CU.  us of a forward / backward call by the rule,
+  // and with 128 x 128, 256 x 128, 256 x 256 and four stages of 128 x 128 throughout:
+  // 4097 x 391 -> 1031 -> 259     45 / 115   50 / 124  56 / 136  68 / 165  50 / 119
+  // 8192 x 2048 -> 8192 -> 2048   702 / 1987 826 / 2535 732 / 2248 663 / 1981 945 / 2868
+  // 1622 x 5084 -> 2893 -> 1191   159 / 485  216 / 560 210 / 537 219 / 503 191 / 550
+  // 30000 x 256 -> 1024 -> 256    77 / 248   81 / 240  87 / 247  86 / 269  114 / 284
+  // 300 x 2048 -> 2048 -> 2048    38 / 99    49 / 119  54 / 129  87 / 227  39 / 103
   static constexpr struct {
     int tile, tm, tn, to_cu;
     double cost;
@@ -1141,6 +1202,8 @@ hipError_t launch_pack(PackArgs a, int type, hipStream_t stream) {
   return type == T_BF16 ? launch(pack_tables<T_BF16>, grid, dim3(256), 0, stream, a)
                         : launch(pack_tables<T_F16>, grid, dim3(256), 0, stream, a);
 }
+
+int64_t thin_sum_rows(int64_t M) { return (M + THIN_ROWS - 1) / THIN_ROWS * THIN_WAVES; }
 
 hipError_t launch_join(const JoinArgs &a, int type, hipStream_t stream) {
   const dim3 grid((unsigned)((a.M * (a.ldp / 4) + 63) / 64));

@@ -475,7 +475,9 @@ struct ProductArgs {
   int64_t ldc = 0, ldc2 = 0;
   int64_t c_rows = INT64_MAX, c_valid = INT64_MAX;
   float *part = nullptr;         // few rows: sums of workgroups that share their k
-  float *sums = nullptr;         // WEIGHTS (product_sums): sums of A over k [splits][M]
+  // GRAD: sums of dg and du over the rows of a wave [product_sum_rows][2 ldc];
+  // WEIGHTS (product_sums): sums of A over k [splits][M].  May be null
+  float *sums = nullptr;
   int32_t act = 0;
 };
 struct ProductPlan {
@@ -483,6 +485,11 @@ struct ProductPlan {
   int32_t splits = 1, split_steps = INT32_MAX;
 };
 ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu);
+// Rows of `sums` that a GRAD product writes.
+inline int64_t product_sum_rows(int tile, int64_t M) {
+  const int64_t tm = tile == TILE_128 || tile == TILE_128_DEEP ? 128 : 256;
+  return (M + tm - 1) / tm * (tile == TILE_256x128 || tile == TILE_128_DEEP ? 4 : 2);
+}
 // Whether a WEIGHTS product also gives the sums of A over k.
 inline bool product_sums(int tile) { return tile != TILE_256; }
 hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hipStream_t stream);
@@ -508,6 +515,7 @@ constexpr int THIN_ROWS = 128;
 bool thin_fits(int64_t M, int64_t K, int64_t H, int64_t N, int n_cu);
 // grad: c is dx, c2 h and c3 [dg | du], ldc2 h's padded width; a[1] and lda2 are dy's.
 hipError_t launch_thin(const ProductArgs &a, bool grad, int type, hipStream_t stream);
+int64_t thin_sum_rows(int64_t M);  // rows of `sums` that it writes
 // Up to five tables of 16-bit rows to aligned rows of a multiple of eight elements.
 struct PackArgs {
   const void *x[5];

@@ -307,7 +307,8 @@ struct GatedBackward {
   Operand x, dy, gate, up, down;
   ProductPlan grad, dx, dgu, dd;
   bool thin = false;
-  size_t h = 0, g = 0, part = 0, sums = 0, colsum = 0;
+  size_t h = 0, g = 0, part = 0, sums = 0, dy_sums = 0, colsum = 0;
+  int64_t sum_rows = 0;
   Carve c;
   GatedBackward(const gnn_gated_dims &d, int64_t n, int n_cu, const void *xp, int64_t x_ld,
                 const void *dp, int64_t d_ld, bool rows_in, const gnn_gated_weights *w, bool w_in)
@@ -330,9 +331,12 @@ struct GatedBackward {
     if (dd.splits > 1) most = std::max(most, (size_t)dd.splits * d.out_features * hp * 4);
     part = c.take(most);
     thin = thin_fits(n, d.in_features, d.hidden, d.out_features, n_cu);
-    // the biases' gradients come with the weights', or as column sums of their own
-    sums = c.take(std::max((size_t)dgu.splits * 2 * hp, (size_t)dd.splits * d.out_features) * 4);
-    colsum = c.take(std::max(colsum_scratch(n, (int32_t)(2 * hp)), colsum_scratch(n, d.out_features)));
+    // sums of dg and du over rows, and of dy with the down projection's gradient
+    sum_rows = thin ? thin_sum_rows(n) : product_sum_rows(grad.tile, n);
+    sums = c.take((size_t)sum_rows * 2 * hp * 4);
+    dy_sums = c.take((size_t)dd.splits * d.out_features * 4);
+    colsum = c.take(std::max(colsum_scratch(sum_rows, (int32_t)(2 * hp)),
+                             colsum_scratch(n, d.out_features)));
   }
 };
 
@@ -480,6 +484,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     b.c = h;
     b.c2 = g;
     b.ldc = hp;
+    b.sums = dw->gate_bias || dw->up_bias ? (float *)(ws + f.sums) : nullptr;
     b.act = d->activation;
     if (f.thin) {
       b.c = dx;
@@ -528,7 +533,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     a.c = c;
     a.c2 = c2;
     a.ldc = n;
-    if (sums && product_sums(plan.tile)) a.sums = (float *)(ws + f.sums);
+    if (sums && product_sums(plan.tile)) a.sums = (float *)(ws + f.dy_sums);
     if (plan.splits == 1)
       return launched(launch_product(a, PRODUCT_WEIGHTS, t, plan.tile, stream), what);
     a.c = ws + f.part;
@@ -548,33 +553,37 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     j.c_valid = valid;
     return launched(launch_join(j, t, stream), what);
   };
-  // Gradients of biases: the sums over k that came with a product, or the table's.
-  auto biases = [&](const ProductPlan &plan, const void *table, int64_t stride, int32_t width,
-                    void *y0, void *y1, int32_t valid) {
-    if (!y0 && !y1) return (int)GNN_OK;
-    SumArgs s;
-    const bool there = product_sums(plan.tile);
-    s.x = there ? ws + f.sums : table;
-    s.x_type = there ? GNN_FP32 : t;
-    s.x_stride = there ? width : stride;
-    s.width = width;
-    s.n = there ? plan.splits : n_rows;
-    s.y[0] = y0;
-    s.y[1] = y1;
-    s.y_type = t;
-    s.split = valid;
-    s.skip = y1 ? (int32_t)hp : width;
-    return sum_columns(s, ws + f.colsum, "bias gradients", stream);
-  };
-  void *bg = (void *)dw->gate_bias, *bu = (void *)dw->up_bias, *bd = (void *)dw->down_bias;
   if ((rc = weights(g, 2 * hp, 2 * hp, f.x.p, f.x.stride, d->in_features, f.dgu, (void *)dw->gate,
-                    (void *)dw->up, hp, d->hidden, bg || bu, "gradients of gate and up")) ||
-      (rc = biases(f.dgu, g, 2 * hp, (int32_t)(2 * hp), bg, bu, d->hidden)))
+                    (void *)dw->up, hp, d->hidden, false, "gradients of gate and up")) ||
+      (rc = weights(f.dy.p, f.dy.stride, d->out_features, h, hp, d->hidden, f.dd, (void *)dw->down,
+                    (void *)dw->down, d->out_features, d->out_features, dw->down_bias != nullptr,
+                    "gradient of down")))
     return rc;
-  if ((rc = weights(f.dy.p, f.dy.stride, d->out_features, h, hp, d->hidden, f.dd, (void *)dw->down,
-                    (void *)dw->down, d->out_features, d->out_features, bd, "gradient of down")))
-    return rc;
-  return biases(f.dd, dy, dy_stride, d->out_features, bd, nullptr, d->out_features);
+  SumArgs s;
+  s.y_type = t;
+  if (dw->gate_bias || dw->up_bias) {
+    s.x = ws + f.sums;
+    s.x_type = GNN_FP32;
+    s.x_stride = s.width = (int32_t)(2 * hp);
+    s.n = n_rows ? f.sum_rows : 0;
+    s.y[0] = (void *)dw->gate_bias;
+    s.y[1] = (void *)dw->up_bias;
+    s.split = d->hidden;
+    s.skip = (int32_t)hp;
+    if ((rc = sum_columns(s, ws + f.colsum, "bias gradients", stream))) return rc;
+  }
+  if (dw->down_bias) {
+    const bool there = product_sums(f.dd.tile);  // dy itself otherwise
+    s.x = there ? ws + f.dy_sums : dy;
+    s.x_type = there ? GNN_FP32 : t;
+    s.x_stride = there ? d->out_features : dy_stride;
+    s.n = there ? f.dd.splits : n_rows;
+    s.width = s.split = s.skip = d->out_features;
+    s.y[0] = (void *)dw->down_bias;
+    s.y[1] = nullptr;
+    return sum_columns(s, ws + f.colsum, "bias gradients", stream);
+  }
+  return GNN_OK;
 }
 
 }  // extern "C"

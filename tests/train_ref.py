@@ -165,7 +165,7 @@ def gated_backward(dy, x, w, b, name):
         v = _mm(left.t(), right)
         e = _mm(eleft.t(), right.abs() + eright) + _mm(left.abs().t(), eright)
         out.append((v, e + (m + 2) * 2 * U * _mm((left.abs() + eleft).t(), right.abs() + eright)))
-    # sums of dg and du as they are in 16 bits
-    for v, e in ((dg, edg), (du, edu), (dy, 0 * dy)):
+    # sums of dg and du before they are rounded
+    for v, e in ((dg, edg0), (du, edu0), (dy, 0 * dy)):
         out.append((v.sum(0), e.sum(0) + (m + 2) * U * (v.abs() + e).sum(0)))
     return out
