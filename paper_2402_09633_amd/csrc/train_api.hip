@@ -125,6 +125,8 @@ int gnn_layer_norm(const void *x, int32_t type, int64_t x_stride, int64_t n_rows
       (rc = check_table("y", y, type, y_stride, width)) ||
       (rc = check_vector("gamma", gamma, GNN_FP32)) || (rc = check_vector("beta", beta, GNN_FP32)))
     return rc;
+  if (y == x && y_stride != x_stride)
+    return bad(GNN_E_INVALID_ARG, "y overlaps x: in place, the strides have to be equal");
   if (!mean != !rstd) return bad(GNN_E_INVALID_ARG, "mean and rstd go together");
   if (mean && ((rc = check_vector("mean", mean, GNN_FP32)) ||
                (rc = check_vector("rstd", rstd, GNN_FP32))))
@@ -168,6 +170,8 @@ int gnn_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
                      (rc = check_vector("mean", mean, GNN_FP32)) ||
                      (rc = check_vector("rstd", rstd, GNN_FP32))))
     return rc;
+  if (n_rows > 0 && (dx == x || (dx == dy && dx_stride != dy_stride)))
+    return bad(GNN_E_INVALID_ARG, "dx overlaps x, or dy with another stride");
   if ((rc = check_scratch(workspace, workspace_bytes, gnn_layer_norm_workspace(n_rows, width))))
     return rc;
   unsigned char *ws = (unsigned char *)workspace;
@@ -376,6 +380,7 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   if ((rc = check_table("x", x, d->dtype, x_stride, d->in_features)) ||
       (rc = check_table("y", y, d->dtype, y_stride, d->out_features)))
     return rc;
+  if (y == x) return bad(GNN_E_INVALID_ARG, "y overlaps x");
   int n_cu = 0;
   const int none = devices_cu(&n_cu);
   GatedForward f(*d, n_rows, n_cu, x, x_stride, lies_aligned(x, x_stride), w,
@@ -449,6 +454,13 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
                      (rc = check_table("x", x, d->dtype, x_stride, d->in_features)) ||
                      (rc = check_table("dx", dx, d->dtype, dx_stride, d->in_features))))
     return rc;
+  if (n_rows > 0 && (dx == x || dx == dy))
+    return bad(GNN_E_INVALID_ARG, "dx overlaps an input");
+  for (const void *in : {w->gate, w->up, w->down})
+    for (const void *out : {dw->gate, dw->up, dw->down})
+      if (in == out) return bad(GNN_E_INVALID_ARG, "a gradient overlaps a weight");
+  if (dw->gate == dw->up || dw->gate == dw->down || dw->up == dw->down)
+    return bad(GNN_E_INVALID_ARG, "gradients overlap");
   int n_cu = 0;
   const int none = devices_cu(&n_cu);
   GatedBackward f(*d, n_rows, n_cu, x, x_stride, dy, dy_stride,

@@ -1033,6 +1033,7 @@ def gated_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up
     return (out, *grads)
 
 
+_FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
 _GRAD = np.dtype([("grad", np.uint64), ("out", np.uint64), ("count", np.int64),
                   ("type", np.int32), ("reserved", np.int32)])
 
@@ -1052,16 +1053,19 @@ def clip_grads(grads, max_norm: float, out=None, stream=None) -> torch.Tensor:
             return clip_grads(grads, max_norm, out)
     if len(out) != len(grads):
         raise ValueError(f"out: {len(out)} tensors, expected {len(grads)}")
-    for what, ts in (("grads", grads), ("out", out)) if out is not grads else (("grads", grads),):
-        for t in ts:
-            if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES or t.dtype == torch.int8:
-                raise TypeError(f"{what}: expected float32, bfloat16 and float16 tensors")
-            if not t.is_contiguous() or t.device != dev:
-                raise ValueError(f"{what}: expected contiguous tensors on {dev}")
+    # a step has hundreds of tensors: whole lists at a time
+    listed = (("grads", grads),) if out is grads else (("out", out), ("grads", grads))
+    for what, ts in listed:
+        if not all([isinstance(t, torch.Tensor) for t in ts]):
+            raise TypeError(f"{what}: expected tensors")
+        kinds = [t.dtype for t in ts]
+        if not _FLOATS.issuperset(kinds):
+            raise TypeError(f"{what}: expected float32, bfloat16 and float16 tensors")
+        if {t.get_device() for t in ts} != {dev.index} or not all([t.is_contiguous() for t in ts]):
+            raise ValueError(f"{what}: expected contiguous tensors on {dev}")
     table = np.zeros(len(grads), _GRAD)
     table["grad"] = [t.data_ptr() for t in grads]
     table["count"] = counts = [t.numel() for t in grads]
-    kinds = [t.dtype for t in grads]
     table["type"] = [_TYPES[k] for k in kinds]
     if out is grads:
         table["out"] = table["grad"]

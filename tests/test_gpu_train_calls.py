@@ -262,6 +262,12 @@ def test_gated_refuses(G):
         G.gated(x, wg, wg, wd, out=z(4, 9))
     with pytest.raises((TypeError, ValueError)):
         G.gated_backward(z(4, 9), x, wg, wg, wd)
+    dy = z(4, 8)
+    for out in (x, dy):
+        with pytest.raises(G.GnnError, match="overlaps"):
+            G.gated_backward(dy, x, wg, wg, wd, out=out)
+    with pytest.raises(G.GnnError, match="overlaps"):
+        G.gated(x, wg, wg, wd, out=x)
     with pytest.raises(G.GnnError) as e:
         G.gated(z(1, 16_385), z(2, 16_385), z(2, 16_385), z(8, 2))
     assert e.value.code == G.GNN_E_UNSUPPORTED

@@ -70,7 +70,7 @@ def test_gated_refuses(G, kw, code, text):
     d, w = _gated(G, **kw)
     assert G.lib.gnn_gated(d, w, X, 8, 4, Y, 8, W, 1 << 30, None) == code
     assert text in G.gnn_last_error()
-    _, dw = _gated(G)
+    _, dw = _gated(G, gate=V, up=V + 512, down=V + 1024)
     assert G.lib.gnn_gated_backward(d, w, X, 8, X, 8, 4, Y, 8, dw, W, 1 << 30, None) == code
     assert text in G.gnn_last_error()
 
@@ -100,6 +100,25 @@ def test_gated_scratch(G):
                            None) == G.GNN_E_INVALID_ARG
     d.struct_size = 4
     assert G.lib.gnn_gated_workspace(d, 5, 0, 1) == 0
+
+
+def test_overlaps_are_refused(G):
+    bad = G.GNN_E_INVALID_ARG
+    d, w = _gated(G)
+    args = [X, 0, 8, 4, 8, V, V, 1e-5, X, 16, W, W]
+    assert G.lib.gnn_layer_norm(*args, None) == bad and "overlaps" in G.gnn_last_error()
+    for dx, stride in ((X, 8), (Y, 16)):
+        args = [Y, 8, X, 8, 0, 4, 8, V, V, V, dx, stride, W, W, W, 1 << 30]
+        assert G.lib.gnn_layer_norm_backward(*args, None) == bad
+        assert "overlaps" in G.gnn_last_error()
+    assert G.lib.gnn_gated(d, w, X, 8, 4, X, 8, W, 1 << 30, None) == bad
+    assert "overlaps" in G.gnn_last_error()
+    apart = dict(gate=V, up=V + 512, down=V + 1024)
+    for dx, kw in ((X, {}), (Y, {}), (X + 4096, dict(gate=W)), (X + 4096, dict(down=W)),
+                   (X + 4096, dict(up=V)), (X + 4096, dict(down=V + 512))):
+        _, dw = _gated(G, **{**apart, **kw})
+        assert G.lib.gnn_gated_backward(d, w, Y, 8, X, 8, 4, dx, 8, dw, W, 1 << 30, None) == bad
+        assert "overlap" in G.gnn_last_error()
 
 
 def _list(G, *rows):
