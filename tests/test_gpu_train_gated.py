@@ -217,6 +217,35 @@ def test_no_rows(G):
     assert all((g == 0).all() and g.shape == t.shape for g, t in zip(grads, w + b))
 
 
+@pytest.mark.parametrize("m", [3, 70])
+def test_widest(G, m):
+    check(G, *make(m, 16_384, 40, 16_384, torch.float16, 10), "silu")
+    check(G, *make(m, 24, 16_384, 16, torch.float16, 11), "silu")
+
+
+def test_tables_beyond_4_gib(G):
+    """Rows whose addresses need more than 32 bits; gradients of the weights as the
+    sums of those of pieces (a kernel's own sums are of fewer rows than a piece's)."""
+    m, k, h, n, piece = 1_200_000, 2048, 16, 24, 60_000
+    _, w, b, _ = make(1, k, h, n, torch.bfloat16, 12)
+    g = torch.Generator(device="cuda").manual_seed(13)
+    x = torch.empty(m, k, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    dy = torch.empty(m, n, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    y = G.gated(x, *w, biases=b)
+    dx, *grads = G.gated_backward(dy, x, *w, biases=b)
+    sums = [[0.0, 0.0] for _ in grads]
+    for at in range(0, m, piece):
+        rows = slice(at, at + piece)
+        parts = R.gated_backward(dy[rows], x[rows], w, b, "silu")
+        if at in (0, m - piece):
+            R.within(y[rows], *R.gated(x[rows], w, b, "silu"))
+            R.within(dx[rows], *parts[0])
+        for s, (v, e) in zip(sums, parts[1:]):
+            s[0], s[1] = s[0] + v, s[1] + e
+    for have, (v, e) in zip(grads, sums):
+        R.within(have, v, e)
+
+
 def test_same_bits_every_time(G):
     a = make(20_000, 136, 264, 72, torch.bfloat16, 8)
     one, two = (check(G, *a, "gelu") for _ in range(2))

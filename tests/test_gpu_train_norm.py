@@ -68,6 +68,28 @@ def test_many_rows(G):
     _check(G, *_inputs(9_000, 2_056, torch.bfloat16, 1))
 
 
+def test_tables_beyond_4_gib(G):
+    m, k, piece = 1_200_000, 2048, 100_000
+    g = _gen(2)
+    x = torch.empty(m, k, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    dy = torch.empty(m, k, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    gamma, beta = torch.ones(k, device="cuda"), torch.zeros(k, device="cuda")
+    y, mean, rstd = G.layer_norm(x, gamma, beta, save=True)
+    dx, dgamma, dbeta = G.layer_norm_backward(dy, x, gamma, mean, rstd)
+    sums = [[0.0, 0.0], [0.0, 0.0]]
+    for at in range(0, m, piece):
+        rows = slice(at, at + piece)
+        want = R.layer_norm_backward(dy[rows], x[rows], gamma, 1e-5)
+        if at in (0, m - piece):
+            R.within(y[rows], *R.layer_norm(x[rows], gamma, beta, 1e-5))
+            R.within(dx[rows], *want[0])
+        for s, (v, e) in zip(sums, want[1:]):
+            s[0], s[1] = s[0] + v, s[1] + e
+    # a sequence of the whole has at most m / 512 + 100 numbers, twelve times a piece's
+    for have, (v, e) in zip((dgamma, dbeta), sums):
+        R.within(have, v, m / piece * e)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("k,pitch", [(8, 9), (128, 133), (391, 396), (512, 520), (2050, 2051)])
 def test_strides(G, kind, k, pitch):
