@@ -231,6 +231,17 @@ __device__ __forceinline__ float sums16(const float (&v)[16]) {
   return w[0];
 }
 
+// What rounding v to 16 bits leaves (nothing where that is no number).
+template <int T>
+__device__ __forceinline__ f4 rest4(const f4 &v) {
+  typedef elem_t<T> e4 __attribute__((ext_vector_type(4)));
+  const f4 hi = __builtin_convertvector(__builtin_convertvector(v, e4), f4);
+  f4 r;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r[j] = fabsf(hi[j]) < INFINITY ? v[j] - hi[j] : 0.f;
+  return r;
+}
+
 // ---- the product ----
 // Half a stage (k of one MFMA) of a wave's blocks, while the operands of the next
 // half come from LDS and, in every second half, a stage from memory: loads stand
@@ -293,6 +304,7 @@ gated_product(ProductArgs a) {
   typedef elem_t<T> E;
   // WEIGHTS of tiles whose sums leave room: also sums of A over k, by MFMAs with ones
   constexpr bool SUMS = AKS && MI * NI <= 16;
+  constexpr bool LO = EPI == EPI_GRAD && MI * NI <= 8;  // the tile that few rows take
   constexpr bool AHEAD = !(NW == 8 && MI * NI >= 32 && EPI == EPI_GRAD);
   extern __shared__ __attribute__((aligned(1024))) unsigned char shared[];
   const uint32_t lds = (uint32_t)(uintptr_t)(lds_byte *)shared;
@@ -350,12 +362,14 @@ gated_product(ProductArgs a) {
   constexpr int LOADS = SA::LOADS + SB::LOADS;
   auto coming = [&](int32_t step, uint32_t to) {
     Coming c;
-    const bool on = step < end, seg = step >= seg_steps;
-    const int32_t k = (step - (seg ? seg_steps : 0)) * BK;
+    const bool on = step < end;
+    const int32_t seg = (step >= seg_steps) + (EPI != EPI_GRAD && step >= 2 * seg_steps) +
+                        (EPI != EPI_GRAD && step >= 3 * seg_steps);
+    const int32_t k = (step - seg * seg_steps) * BK;
     c.to = to;
-    c.second = EPI == EPI_GRAD && seg;
+    c.second = EPI == EPI_GRAD && seg > 0;
     c.left = (c.second ? a.K2 : a.K) - k;
-    const E *pa = (const E *)a.a[seg ? 1 : 0], *pb = (const E *)a.b[!DUAL && seg ? 1 : 0];
+    const E *pa = (const E *)a.a[seg], *pb = (const E *)a.b[DUAL ? 0 : seg];
     const int64_t lda = c.second ? a.lda2 : a.lda;
     c.a = buffer_of(pa + (AKS ? k * lda + m0 : m0 * lda + k), on);
     c.b = buffer_of(pb + (BKS ? k * a.ldb + n0 : n0 * a.ldb + k), on);
@@ -521,7 +535,8 @@ gated_product(ProductArgs a) {
           const int32_t c = c0 + j * 16;
           if (m < a.M && c < a.ldc) {  // ldc: N and its padding, in which everything is zero
             const f4 g = acc[i][j] + bg[j], u = acc[i][j + HN] + bu[j];
-            E *ph = (E *)a.c + m * a.ldc + c;
+            const int64_t times = LO && a.lo ? 2 : 1;
+            E *ph = (E *)a.c + m * times * a.ldc + c;
             f4 h;
             if constexpr (EPI == EPI_GATE) {
 #pragma unroll
@@ -540,10 +555,15 @@ gated_product(ProductArgs a) {
                 over_m[j * 4 + v] += dg[v];
                 over_m[8 + j * 4 + v] += du[v];
               }
-              E *pd = (E *)a.c2 + m * 2 * a.ldc + c;
+              E *pd = (E *)a.c2 + m * times * 2 * a.ldc + c;
               store4<T>(ph, h, 4, true);
               store4<T>(pd, dg, 4, true);
               store4<T>(pd + a.ldc, du, 4, true);
+              if (LO && a.lo) {
+                store4<T>(ph + a.ldc, rest4<T>(h), 4, true);
+                store4<T>(pd + 2 * a.ldc, rest4<T>(dg), 4, true);
+                store4<T>(pd + 3 * a.ldc, rest4<T>(du), 4, true);
+              }
             }
           }
         }
@@ -857,6 +877,12 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
 // memory, the same for both operands, so that the four lanes of a row read 128
 // neighbouring bytes.
 //
+// With up to 16 rows the errors of h's rounding do not average out over a result (2 x
+// 36 -> 114 -> 4386 bf16: 1.6 times the error of rounding the exact result, where many
+// rows have 1.4), and another operand costs nothing beside the weights: h goes on in
+// two 16-bit numbers, the second what the first one's rounding left.  (48 rows of 2048
+// -> 8192 -> 2048 would take 45.5 us so, 39.5 without.)
+//
 // The down projection has few columns and many k, so several workgroups (gridDim.y)
 // share a column's k, and few_join adds up what they leave: 8192 -> 2048, one row,
 // 12.3 us without.  (One kernel whose last workgroup adds up took 99: a fence
@@ -865,6 +891,7 @@ template <int T, int MB, int NC, int NW, bool GATE>
 __global__ __launch_bounds__(64 * NW) void gated_few(ProductArgs a) {
   typedef elem_t<T> E;
   constexpr int NB = GATE ? 2 * NC : NC;
+  constexpr bool TWO = MB == 1;
   __shared__ f4 sum[NW][MB * NB][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int li = lane & 15, lg = lane >> 4;
@@ -886,19 +913,26 @@ __global__ __launch_bounds__(64 * NW) void gated_few(ProductArgs a) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
       const int32_t kk = k + lg * 16 + s * 8;
-      Raw8<T> xb[NB], xa[MB];
+      Raw8<T> xb[NB], xa[MB], xl[MB];
 #pragma unroll
       for (int j = 0; j < NB; ++j)
         xb[j] = end ? load8_end<T>(pb[j], kk, a.K) : load8<T>(pb[j], kk);
 #pragma unroll
       for (int i = 0; i < MB; ++i)
         xa[i] = end ? load8_end<T>(pa[i], kk, a.K) : load8<T>(pa[i], kk);
+      if constexpr (TWO && !GATE)
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+          xl[i] = end ? load8_end<T>(pa[i] + a.lo, kk, a.K) : load8<T>(pa[i] + a.lo, kk);
 #pragma unroll
       for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-          acc[i][j] = mfma16<T>(__builtin_bit_cast(s8v, xb[j].v), __builtin_bit_cast(s8v, xa[i].v),
-                                acc[i][j]);
+        for (int j = 0; j < NB; ++j) {
+          const s8v w = __builtin_bit_cast(s8v, xb[j].v);
+          acc[i][j] = mfma16<T>(w, __builtin_bit_cast(s8v, xa[i].v), acc[i][j]);
+          if constexpr (TWO && !GATE)
+            acc[i][j] = mfma16<T>(w, __builtin_bit_cast(s8v, xl[i].v), acc[i][j]);
+        }
     }
   };
   int32_t st = wave + NW * blockIdx.y;
@@ -944,7 +978,10 @@ __global__ __launch_bounds__(64 * NW) void gated_few(ProductArgs a) {
         for (int e = 0; e < 4; ++e)
           h[e] = c + e < a.N ? activate<act.value, false>(v[0][e], nullptr) * v[1][e] : 0.f;
       });
-      if (c < a.ldc) store4<T>((E *)a.c + m * a.ldc + c, h, 4, true);
+      if (c < (TWO ? a.lo : a.ldc)) {
+        store4<T>((E *)a.c + m * a.ldc + c, h, 4, true);
+        if (TWO) store4<T>((E *)a.c + m * a.ldc + a.lo + c, rest4<T>(h), 4, true);
+      }
     } else {
       store4<T>((E *)a.c + m * a.ldc + c, v[0], a.N - c,
                 a.ldc % 4 == 0 && (uintptr_t)a.c % 8 == 0);

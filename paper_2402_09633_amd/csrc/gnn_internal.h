@@ -454,10 +454,10 @@ constexpr int PRODUCT_GATE = 0, PRODUCT_GRAD = 1, PRODUCT_DOWN = 2, PRODUCT_ROWS
               PRODUCT_WEIGHTS = 4;
 constexpr int TILE_128 = 0, TILE_256x128 = 1, TILE_256 = 2, TILE_128_DEEP = 3;
 struct ProductArgs {
-  // Operands of one or two segments of k (GATE, GRAD: b[1] is the up projection).
+  // Operands of one to four segments of k (GATE, GRAD: b[1] is the up projection).
   // Addresses are multiples of 16 bytes, strides (in elements, below 2^21) and
   // contiguous extents of 8 elements, or zeros fill up to that.
-  const void *a[2] = {nullptr, nullptr}, *b[2] = {nullptr, nullptr};
+  const void *a[4] = {}, *b[4] = {};
   int64_t lda = 0, ldb = 0;
   // GRAD: a[1] is dy (stride lda2) and b2 the down projection [K2][N], whose
   // product is the gradient of h
@@ -479,6 +479,10 @@ struct ProductArgs {
   // WEIGHTS (product_sums): sums of A over k [splits][M].  May be null
   float *sums = nullptr;
   int32_t act = 0;
+  // What rounding to 16 bits leaves, kept beside the numbers.  GRAD (not 0; tiles
+  // TILE_128_DEEP): h's rows are [h | rest], those of c2 [dg | du | rests].  Up to
+  // TWO_ROWS rows (launch_few): the rest of h lies `lo` elements behind it.
+  int32_t lo = 0;
 };
 struct ProductPlan {
   int tile = 0;
@@ -494,7 +498,7 @@ inline int64_t product_sum_rows(int tile, int64_t M) {
 inline bool product_sums(int tile) { return tile != TILE_256; }
 hipError_t launch_product(const ProductArgs &a, int kind, int type, int tile, hipStream_t stream);
 // Up to FEW_ROWS rows; operands of any alignment (GATE or DOWN).
-constexpr int FEW_ROWS = 64;
+constexpr int FEW_ROWS = 64, TWO_ROWS = 16;
 constexpr int FEW_COLUMNS = 2;   // column blocks to a workgroup (1 up to 16 rows)
 inline int64_t few_blocks(int64_t M, int64_t N) {
   const int64_t n = M <= 16 ? 16 : 16 * FEW_COLUMNS;

@@ -303,14 +303,15 @@ struct GatedForward {
     } else {
       for (Operand *o : {&x, &gate, &up, &down}) o->place(c);
     }
-    h = c.take((size_t)n * up8(d.hidden) * 2);
+    h = c.take((size_t)n * up8(d.hidden) * (n <= TWO_ROWS ? 4 : 2));
   }
 };
 
 struct GatedBackward {
   Operand x, dy, gate, up, down;
   ProductPlan grad, dx, dgu, dd;
-  bool thin = false;
+  // two: h, dg and du in two 16-bit numbers (few rows, as gated_few)
+  bool thin = false, two = false;
   size_t h = 0, g = 0, part = 0, sums = 0, dy_sums = 0, colsum = 0;
   int64_t sum_rows = 0;
   Carve c;
@@ -327,8 +328,10 @@ struct GatedBackward {
     dx = product_plan(PRODUCT_ROWS, n, d.in_features, 2 * hp, n_cu);
     dgu = product_plan(PRODUCT_WEIGHTS, 2 * hp, d.in_features, n, n_cu);
     dd = product_plan(PRODUCT_WEIGHTS, d.out_features, d.hidden, n, n_cu);
-    h = c.take((size_t)n * hp * 2);
-    g = c.take((size_t)n * hp * 4);
+    two = n > 0 && n <= TWO_ROWS;
+    if (two) grad.tile = TILE_128_DEEP;
+    h = c.take((size_t)n * hp * (two ? 4 : 2));
+    g = c.take((size_t)n * hp * (two ? 8 : 4));
     // the parts of one product are joined before the next one's are written
     size_t most = 0;
     if (dgu.splits > 1) most = (size_t)dgu.splits * 2 * hp * kp * 4;
@@ -417,7 +420,8 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
     return launched(launch_thin(a, false, t, stream), "gated block");
   }
   a.c = ws + f.h;
-  a.ldc = hp;
+  a.ldc = n_rows <= TWO_ROWS ? 2 * hp : hp;
+  a.lo = n_rows <= TWO_ROWS ? (int32_t)hp : 0;
   rc = launched(f.few ? launch_few(a, true, t, 1, stream)
                       : launch_product(a, PRODUCT_GATE, t,
                                        product_plan(PRODUCT_GATE, a.M, a.N, a.K, n_cu).tile, stream),
@@ -425,7 +429,8 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   if (rc) return rc;
   ProductArgs b;
   b.a[0] = ws + f.h;
-  b.lda = hp;
+  b.lda = a.ldc;
+  b.lo = a.lo;
   b.b[0] = f.down.p;
   b.ldb = f.down.stride;
   b.M = n_rows;
@@ -498,6 +503,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     b.ldc = hp;
     b.sums = dw->gate_bias || dw->up_bias ? (float *)(ws + f.sums) : nullptr;
     b.act = d->activation;
+    b.lo = f.two;
     if (f.thin) {
       b.c = dx;
       b.ldc = dx_stride;
@@ -511,41 +517,45 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
       return rc;
     // dx = dg Wg + du Wu
     ProductArgs e;
-    e.a[0] = g;
-    e.a[1] = (unsigned char *)g + hp * 2;
-    e.lda = 2 * hp;
-    e.b[0] = f.gate.p;
-    e.b[1] = f.up.p;
+    e.segs = f.two ? 4 : 2;
+    for (int i = 0; i < e.segs; ++i) {
+      e.a[i] = (unsigned char *)g + i * hp * 2;
+      e.b[i] = i % 2 ? f.up.p : f.gate.p;
+    }
+    e.lda = e.segs * hp;
     e.ldb = f.gate.stride;
     e.M = n_rows;
     e.N = d->in_features;
     e.K = d->hidden;
-    e.segs = 2;
     e.c = dx;
     e.ldc = dx_stride;
     if (!f.thin && (rc = launched(launch_product(e, PRODUCT_ROWS, t, f.dx.tile, stream), "gradient of x")))
       return rc;
   }
   // The weights' gradients: the rows are the k.
-  auto weights = [&](const void *pa, int64_t lda, int64_t m, const void *pb, int64_t ldb, int32_t n,
+  auto weights = [&](const void *pa, const void *pa2, int64_t lda, int64_t m, const void *pb,
+                     const void *pb2, int64_t ldb, int32_t n,
                      const ProductPlan &plan, void *c, void *c2, int64_t c_rows, int64_t valid,
                      bool sums, const char *what) {
     ProductArgs a;
     a.a[0] = pa;
+    a.a[1] = pa2;
     a.lda = lda;
     a.b[0] = pb;
+    a.b[1] = pb2;
     a.ldb = ldb;
+    a.segs = f.two ? 2 : 1;
     a.M = m;
     a.N = n;
     a.K = (int32_t)n_rows;
     a.splits = plan.splits;
-    a.split_steps = plan.split_steps;
+    a.split_steps = plan.splits > 1 ? plan.split_steps : INT32_MAX;
     a.c_rows = c_rows;
     a.c_valid = valid;
     a.c = c;
     a.c2 = c2;
     a.ldc = n;
-    if (sums && product_sums(plan.tile)) a.sums = (float *)(ws + f.dy_sums);
+    if (sums) a.sums = (float *)(ws + f.dy_sums);
     if (plan.splits == 1)
       return launched(launch_product(a, PRODUCT_WEIGHTS, t, plan.tile, stream), what);
     a.c = ws + f.part;
@@ -565,11 +575,15 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     j.c_valid = valid;
     return launched(launch_join(j, t, stream), what);
   };
-  if ((rc = weights(g, 2 * hp, 2 * hp, f.x.p, f.x.stride, d->in_features, f.dgu, (void *)dw->gate,
-                    (void *)dw->up, hp, d->hidden, false, "gradients of gate and up")) ||
-      (rc = weights(f.dy.p, f.dy.stride, d->out_features, h, hp, d->hidden, f.dd, (void *)dw->down,
-                    (void *)dw->down, d->out_features, d->out_features, dw->down_bias != nullptr,
-                    "gradient of down")))
+  const unsigned char *g2 = (unsigned char *)g + 2 * hp * 2, *h2 = (unsigned char *)h + hp * 2;
+  const int64_t times = f.two ? 2 : 1;
+  const bool dy_sums = product_sums(f.dd.tile) && !f.two;  // which goes through dy twice
+  if ((rc = weights(g, g2, 2 * hp * times, 2 * hp, f.x.p, f.x.p, f.x.stride, d->in_features, f.dgu,
+                    (void *)dw->gate, (void *)dw->up, hp, d->hidden, false,
+                    "gradients of gate and up")) ||
+      (rc = weights(f.dy.p, f.dy.p, f.dy.stride, d->out_features, h, h2, hp * times, d->hidden,
+                    f.dd, (void *)dw->down, (void *)dw->down, d->out_features, d->out_features,
+                    dw->down_bias && dy_sums, "gradient of down")))
     return rc;
   SumArgs s;
   s.y_type = t;
@@ -585,7 +599,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     if ((rc = sum_columns(s, ws + f.colsum, "bias gradients", stream))) return rc;
   }
   if (dw->down_bias) {
-    const bool there = product_sums(f.dd.tile);  // dy itself otherwise
+    const bool there = dy_sums;  // dy itself otherwise
     s.x = there ? ws + f.dy_sums : dy;
     s.x_type = there ? GNN_FP32 : t;
     s.x_stride = there ? d->out_features : dy_stride;
