@@ -464,7 +464,10 @@ int gnn_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, in
  * h = act(g) u, y = W_down h + b_down.  Rows, weights and biases of one 16-bit
  * type; products and sums in fp32; h is rounded to that type (a GNN_F16 h beyond
  * 65504 is an infinity), and so are the gradients of g and u; up to 16 rows what
- * that rounding leaves goes on beside them. */
+ * that rounding leaves goes on beside them.  The backward pass of GNN_F16 rounds
+ * them times powers of two, 1 at least, that it takes from the sizes of all rows
+ * and weights: small dy or x lose no digits, and no number becomes infinite that
+ * would not be one without them. */
 #define GNN_SILU 0
 #define GNN_GELU 1 /* g Phi(g), Phi the normal distribution (not its tanh form) */
 #define GNN_SIGMOID 2

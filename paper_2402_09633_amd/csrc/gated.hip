@@ -242,6 +242,167 @@ __device__ __forceinline__ f4 rest4(const f4 &v) {
   return r;
 }
 
+// ---- the range of fp16 gradients ----
+// h and the gradients of g and u go on in 16 bits, and fp16 numbers below 2^-14 lose
+// digits: with dy near 1e-5 the weights' gradients of 256 -> 512 -> 256 were off by 4e-3
+// of themselves, 19 times what rounding them costs.  So the backward pass keeps them
+// times a power of two each, the largest with which none can leave the range and never
+// below 1, and its products take it out again, in fp32 and exactly.  By the
+// Cauchy-Schwarz inequality, with the largest sum of squares of a row of each table,
+//   |dh| <= |dy| sqrt(sum over n of max over h of Wd[n][h]^2)
+//   |g| <= |x| |Wg| + |bg|, |u| <= |x| |Wu| + |bu|, |du| <= |dh| |act(g)|
+//   |dg| <= 1.13 |dh| |u|, |h| <= |act(g)| |u|; |act(g)| <= |g|, sigmoid's <= 1.
+// For random rows and weights these bounds are 2^3 to 2^11 times the largest number,
+// which leaves more digits below it than fp16 has.
+// Elements that are no numbers are left out: what they reach is none either.
+//
+// Bound by memory: everything is read once.  A workgroup takes rows of one table and
+// leaves its part of one of the SIZES numbers (of x, dy, gate, up, down, the biases);
+// tables that the products cannot read as they lie are copied on the way, as
+// pack_tables does for bf16.  300000 x 128 -> 256 -> 128: 34 us of 549 forward and
+// backward (4.5 TB/s); 8192 x 2048 -> 8192 -> 2048 31 (5.4 TB/s); 48 x 256 -> 1024 -> 256
+// 6.6; 4097 x 391 -> 1031 -> 259, copies among it, 11 (copies alone 5.3).
+template <int T>
+__global__ __launch_bounds__(1024) void gated_sizes(SizeArgs a) {
+  typedef elem_t<T> E;
+  typedef typename Raw8<T>::vec e8;
+  constexpr int NW = 16, ROWS = 4, LOADS = 4;  // on their way at once
+  __shared__ float parts[NW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int t = 0;
+  while (t + 1 < SIZES && (int)blockIdx.x >= a.first[t + 1]) ++t;
+  const int64_t n = (int)blockIdx.x < a.first[SIZES] ? a.rows[t] : 0;
+  const int32_t K = a.width[t];
+  const bool top = t >= SIZE_DOWN;  // the largest number of a row, not its sum of squares
+  int L = 1;                        // lanes to a row
+  while (L < 64 && 8 * L < K) L *= 2;
+  const int64_t step = (int64_t)(a.first[t + 1] - a.first[t]) * NW * (64 / L);
+  const E *x = (const E *)a.x[t];
+  E *copy = (E *)a.y[t];
+  const int64_t pitch = (K + 7) & ~7;
+  auto add = [&](float s, const Raw8<T> &raw) {
+    float p = 0.f;
+    if (top) {
+      p = top_of<T>(max_bits<T>(raw, 0));
+      p *= p;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p = __builtin_fmaf((float)raw.v[j], (float)raw.v[j], p);
+    }
+    if (!(p < INFINITY)) {  // an element is no number: a branch that is hardly ever taken
+      asm volatile("");
+      p = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float v = (float)raw.v[j], m = fabsf(v) < INFINITY ? v : 0.f;
+        p = top ? fmaxf(p, m * m) : __builtin_fmaf(m, m, p);
+      }
+    }
+    return top ? fmaxf(s, p) : s + p;
+  };
+  auto over_row = [&](float s) {
+    for (int o = 1; o < L; o *= 2) {
+      const float w = __shfl_xor(s, o);
+      s = top ? fmaxf(s, w) : s + w;
+    }
+    return s;
+  };
+  float most = 0.f;
+  // every lane of a wave goes round as often as its first: they add together
+  int64_t r0 = ((int64_t)((int)blockIdx.x - a.first[t]) * NW + wave) * (64 / L);
+  auto row_done = [&](int64_t r, float s) {
+    s = over_row(s);
+    if (t != SIZE_DOWN)
+      most = fmaxf(most, s);
+    else if (r < n && lane % L == 0)
+      most += s;
+  };
+  if (K <= 512) {  // a row is one load of its lanes: four rows at a time
+    const int k = 8 * (lane % L);
+    for (; r0 < n; r0 += ROWS * step) {
+      Raw8<T> raw[ROWS];
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        const int64_t r = r0 + i * step + lane / L;
+        const E *row = x + min(r, n - 1) * a.stride[t];
+        raw[i] = k + 8 <= K ? load8<T>(row, k) : load8_end<T>(row, k, K);
+      }
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        const int64_t r = r0 + i * step + lane / L;
+        if (copy && r < n && k < K) *(e8 *)(copy + r * pitch + k) = raw[i].v;
+        row_done(r, add(0.f, raw[i]));
+      }
+    }
+  } else {  // four loads of a row at a time
+    for (; r0 < n; r0 += step) {
+      const E *row = x + r0 * a.stride[t];
+      float s = 0.f;
+      for (int k0 = 8 * lane; k0 < K; k0 += LOADS * 512) {
+        Raw8<T> raw[LOADS];
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int k = k0 + i * 512;
+          raw[i] = k + 8 <= K ? load8<T>(row, k) : load8_end<T>(row, k, K);
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const int k = k0 + i * 512;
+          if (copy && k < K) *(e8 *)(copy + r0 * pitch + k) = raw[i].v;
+          s = add(s, raw[i]);
+        }
+      }
+      row_done(r0, s);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const float w = __shfl_xor(most, o);
+    most = t == SIZE_DOWN ? most + w : fmaxf(most, w);
+  }
+  if (lane == 0) parts[wave] = most;
+  __syncthreads();
+  if (threadIdx.x < SIZES) {
+    float v = parts[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) v = t == SIZE_DOWN ? v + parts[w] : fmaxf(v, parts[w]);
+    a.part[threadIdx.x * SIZE_PARTS + blockIdx.x] = (int)threadIdx.x == t ? v : 0.f;
+  }
+}
+
+// What the gradients of g and u, and h, are multiplied by, from gated_sizes' parts.
+struct GradScales {
+  float grad, h;
+};
+__device__ __forceinline__ GradScales grad_scales(const float *part, int act) {
+  static_assert(SIZE_PARTS == 4 * 64, "four parts to a lane");
+  const int lane = threadIdx.x & 63;
+  float v[SIZES];
+#pragma unroll
+  for (int q = 0; q < SIZES; ++q) {
+    const f4 p = ((const f4 *)(part + q * SIZE_PARTS))[lane];
+    v[q] = q == SIZE_DOWN ? (p[0] + p[1]) + (p[2] + p[3])
+                          : fmaxf(fmaxf(p[0], p[1]), fmaxf(p[2], p[3]));
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2)
+#pragma unroll
+    for (int q = 0; q < SIZES; ++q) {
+      const float w = __shfl_xor(v[q], o);
+      v[q] = q == SIZE_DOWN ? v[q] + w : fmaxf(v[q], w);
+    }
+  const float dh = sqrtf(v[1]) * sqrtf(v[4]);
+  const float u = sqrtf(v[0]) * sqrtf(v[3]) + sqrtf(v[6]);
+  const float s = act == ACT_SIGMOID ? 1.f : sqrtf(v[0]) * sqrtf(v[2]) + sqrtf(v[5]);
+  // 65504 / 1.05: the sums of up to 16384 products and squares are off by less than that
+  auto scale = [](float most) {
+    const float q = fminf(62384.f / most, 0x1p40f);
+    const float two = __uint_as_float(__float_as_uint(q) & 0x7f800000u);
+    return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(two > 1.f ? two : 1.f)));
+  };
+  return GradScales{scale(dh * fmaxf(1.13f * u, s)), scale(s * u)};
+}
+
 // ---- the product ----
 // Half a stage (k of one MFMA) of a wave's blocks, while the operands of the next
 // half come from LDS and, in every second half, a stage from memory: loads stand
@@ -345,6 +506,17 @@ gated_product(ProductArgs a) {
     }
   } else {
     sb.init(wave, lane, a.ldb, min(TN, a.N - n0));
+  }
+
+  GradScales scales{1.f, 1.f};
+  if constexpr (T == T_F16 && EPI == EPI_GRAD) {
+    scales = grad_scales(a.sizes, ACT);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {  // for the products that follow
+      a.scales[0] = 1.f / scales.grad;
+      a.scales[1] = 1.f / scales.h;
+    }
+    // here, where no other registers are taken
+    asm volatile("" : "+s"(scales.grad), "+s"(scales.h));
   }
 
   const int32_t seg_steps = (a.K + BK - 1) / BK;
@@ -555,6 +727,11 @@ gated_product(ProductArgs a) {
                 over_m[j * 4 + v] += dg[v];
                 over_m[8 + j * 4 + v] += du[v];
               }
+              if constexpr (T == T_F16) {
+                h *= scales.h;
+                dg *= scales.grad;
+                du *= scales.grad;
+              }
               E *pd = (E *)a.c2 + m * times * 2 * a.ldc + c;
               store4<T>(ph, h, 4, true);
               store4<T>(pd, dg, 4, true);
@@ -582,6 +759,7 @@ gated_product(ProductArgs a) {
         a.sums[((int64_t)tm * WM + wm) * 2 * a.ldc + (li >> 3) * a.ldc + c] = v;
     }
   } else if constexpr (EPI == EPI_PART) {
+    const float scale = T == T_F16 && a.scale ? *a.scale : 1.f;
     float *part = (float *)a.c + (int64_t)split * a.M * a.ldc;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
@@ -589,11 +767,12 @@ gated_product(ProductArgs a) {
 #pragma unroll
       for (int j = 0; j < NI; ++j) {
         const int32_t c = n0 + wn * NI * 16 + j * 16 + lg * 4;
-        if (m < a.M && c < a.ldc) *(f4 *)(part + m * a.ldc + c) = acc[i][j];
+        if (m < a.M && c < a.ldc) *(f4 *)(part + m * a.ldc + c) = acc[i][j] * scale;
       }
     }
   } else {
     const bool whole = a.ldc % 4 == 0 && ((uintptr_t)a.c | (uintptr_t)a.c2) % 8 == 0;
+    const float scale = T == T_F16 && BKS && a.scale ? *a.scale : 1.f;
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       const int32_t c = n0 + wn * NI * 16 + j * 16 + lg * 4;
@@ -604,7 +783,8 @@ gated_product(ProductArgs a) {
         const bool one = m < a.c_rows;
         const int64_t r = one ? m : m - a.c_rows;
         if (m < a.M && r < a.c_valid)
-          store4<T>((one ? (E *)a.c : (E *)a.c2) + r * a.ldc + c, acc[i][j] + b, a.N - c, whole);
+          store4<T>((one ? (E *)a.c : (E *)a.c2) + r * a.ldc + c,
+                    (T == T_F16 && BKS ? acc[i][j] * scale : acc[i][j]) + b, a.N - c, whole);
       }
     }
   }
@@ -717,6 +897,14 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int n = 0; n < OUT; ++n) y[i][n] = f4{0.f, 0.f, 0.f, 0.f};
+  GradScales scales{1.f, 1.f};
+  if constexpr (T == T_F16 && GRAD) {
+    scales = grad_scales(a.sizes, ACT);
+    if (blockIdx.x == 0 && threadIdx.x == 0) {  // for the products that follow
+      a.scales[0] = 1.f / scales.grad;
+      a.scales[1] = 1.f / scales.h;
+    }
+  }
   // the compiler's own loads are counted with the stages': none may be under way
   __syncthreads();
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -794,6 +982,11 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
           v[j] = activate<ACT, false>(g, nullptr) * u;
         }
       }
+      if constexpr (T == T_F16 && GRAD) {
+        v *= scales.h;
+        vg *= scales.grad;
+        vu *= scales.grad;
+      }
       h[i] = __builtin_bit_cast(s8v, __builtin_convertvector(v, e8));
       if constexpr (GRAD) {
         dg[i] = __builtin_bit_cast(s8v, __builtin_convertvector(vg, e8));
@@ -856,6 +1049,7 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
   stage_barrier<0>();  // no load is under way when the workgroup ends
 
   const int32_t width = GRAD ? a.K : a.K2;
+  const float undo = 1.f / scales.grad;
   const bool whole = a.ldc % 4 == 0 && (uintptr_t)a.c % 8 == 0;
 #pragma unroll
   for (int n = 0; n < OUT; ++n) {
@@ -864,7 +1058,9 @@ __global__ __launch_bounds__(64 * THIN_WAVES, GRAD ? 2 : 3) void gated_thin(Prod
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
       const int64_t m = m0 + i * 16;
-      if (m < a.M) store4<T>((E *)a.c + m * a.ldc + c, y[i][n] + b, width - c, whole);
+      if (m < a.M)
+        store4<T>((E *)a.c + m * a.ldc + c, (T == T_F16 && GRAD ? y[i][n] * undo : y[i][n]) + b,
+                  width - c, whole);
     }
   }
 }
@@ -1238,6 +1434,20 @@ hipError_t launch_pack(PackArgs a, int type, hipStream_t stream) {
   const dim3 grid((unsigned)a.first[a.count]);
   return type == T_BF16 ? launch(pack_tables<T_BF16>, grid, dim3(256), 0, stream, a)
                         : launch(pack_tables<T_F16>, grid, dim3(256), 0, stream, a);
+}
+
+hipError_t launch_sizes(SizeArgs a, hipStream_t stream) {
+  // workgroups by the bytes of a table, at most as many as it keeps busy
+  int64_t bytes[SIZES], all = 0, last = 0;
+  for (int t = 0; t < SIZES; ++t) all += bytes[t] = a.rows[t] * a.width[t] * 2;
+  for (int t = 0; t < SIZES; ++t) {
+    a.first[t] = (int32_t)last;
+    if (bytes[t] == 0) continue;
+    const int64_t share = (SIZE_PARTS - SIZES) * (bytes[t] / 1024 + 1) / (all / 1024 + SIZES) + 1;
+    last += std::min<int64_t>(share, SIZE_PARTS);
+  }
+  a.first[SIZES] = (int32_t)last;
+  return launch(gated_sizes<T_F16>, dim3(SIZE_PARTS), dim3(1024), 0, stream, a);
 }
 
 int64_t thin_sum_rows(int64_t M) { return (M + THIN_ROWS - 1) / THIN_ROWS * THIN_WAVES; }

@@ -483,7 +483,23 @@ struct ProductArgs {
   // TILE_128_DEEP): h's rows are [h | rest], those of c2 [dg | du | rests].  Up to
   // TWO_ROWS rows (launch_few): the rest of h lies `lo` elements behind it.
   int32_t lo = 0;
+  // fp16 gradients: launch_sizes' parts (GRAD, which writes to scales what the products
+  // of [dg | du], and of h, are to be multiplied by); that factor (ROWS, WEIGHTS)
+  const float *sizes = nullptr, *scale = nullptr;
+  float *scales = nullptr;
 };
+// Numbers from which the range of fp16 gradients follows, each of a table: x, dy, gate,
+// up, down, and the biases of gate and up as rows of one.
+constexpr int SIZES = 7, SIZE_PARTS = 256, SIZE_DOWN = 4;
+struct SizeArgs {
+  const void *x[SIZES];
+  void *y[SIZES];        // aligned rows of a multiple of eight elements, or null: no copy
+  int64_t stride[SIZES], rows[SIZES];
+  int32_t width[SIZES];
+  int32_t first[SIZES + 1];  // first workgroup of each (set by the launch)
+  float *part;           // [SIZES][SIZE_PARTS]
+};
+hipError_t launch_sizes(SizeArgs a, hipStream_t stream);
 struct ProductPlan {
   int tile = 0;
   int32_t splits = 1, split_steps = INT32_MAX;

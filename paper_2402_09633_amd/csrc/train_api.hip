@@ -264,14 +264,16 @@ struct Operand {
   void place(Carve &c) {
     if (copy) at = c.take((size_t)rows * up8(width) * 2);
   }
-  // What the products read from here on, and what has to be copied for it.
+  // What the products read from here on, and (a) what has to be copied for it.
   void fetch(unsigned char *ws, PackArgs *a) {
     if (!copy) return;
-    a->x[a->count] = p;
-    a->y[a->count] = ws + at;
-    a->stride[a->count] = stride;
-    a->rows[a->count] = rows;
-    a->width[a->count++] = width;
+    if (a) {
+      a->x[a->count] = p;
+      a->y[a->count] = ws + at;
+      a->stride[a->count] = stride;
+      a->rows[a->count] = rows;
+      a->width[a->count++] = width;
+    }
     p = ws + at;
     stride = up8(width);
   }
@@ -312,7 +314,9 @@ struct GatedBackward {
   ProductPlan grad, dx, dgu, dd;
   // two: h, dg and du in two 16-bit numbers (few rows, as gated_few)
   bool thin = false, two = false;
-  size_t h = 0, g = 0, part = 0, sums = 0, dy_sums = 0, colsum = 0;
+  // half: fp16, whose h, dg and du are multiplied by powers of two
+  bool half = false;
+  size_t h = 0, g = 0, part = 0, sums = 0, dy_sums = 0, colsum = 0, sizes = 0, scales = 0;
   int64_t sum_rows = 0;
   Carve c;
   GatedBackward(const gnn_gated_dims &d, int64_t n, int n_cu, const void *xp, int64_t x_ld,
@@ -344,6 +348,10 @@ struct GatedBackward {
     dy_sums = c.take((size_t)dd.splits * d.out_features * 4);
     colsum = c.take(std::max(colsum_scratch(sum_rows, (int32_t)(2 * hp)),
                              colsum_scratch(n, d.out_features)));
+    if ((half = d.dtype == GNN_F16 && n > 0)) {
+      sizes = c.take(SIZES * SIZE_PARTS * 4);
+      scales = c.take(2 * 4);
+    }
   }
 };
 
@@ -476,10 +484,28 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
   unsigned char *ws = (unsigned char *)workspace;
   const int t = d->dtype;
   const int64_t hp = up8(d->hidden);
-  PackArgs pack;
-  for (Operand *o : {&f.x, &f.dy, &f.gate, &f.up, &f.down}) o->fetch(ws, &pack);
-  if ((rc = launched(launch_pack(pack, t, stream), "row copy"))) return rc;
+  Operand *const tables[] = {&f.x, &f.dy, &f.gate, &f.up, &f.down};
+  if (f.half) {
+    SizeArgs z;
+    for (int i = 0; i < SIZES; ++i) {
+      const void *bias = i == 5 ? w->gate_bias : i == 6 ? w->up_bias : nullptr;
+      const Operand *o = i < 5 ? tables[i] : nullptr;
+      z.x[i] = o ? o->p : bias;
+      z.y[i] = o && o->copy ? ws + o->at : nullptr;
+      z.stride[i] = o ? o->stride : 1;
+      z.rows[i] = o ? o->rows : bias ? d->hidden : 0;
+      z.width[i] = o ? o->width : 1;
+    }
+    z.part = (float *)(ws + f.sizes);
+    if ((rc = launched(launch_sizes(z, stream), "sizes"))) return rc;
+    for (Operand *o : tables) o->fetch(ws, nullptr);
+  } else {
+    PackArgs pack;
+    for (Operand *o : tables) o->fetch(ws, &pack);
+    if ((rc = launched(launch_pack(pack, t, stream), "row copy"))) return rc;
+  }
   void *h = ws + f.h, *g = ws + f.g;
+  float *scales = f.half ? (float *)(ws + f.scales) : nullptr;
   if (n_rows > 0) {
     // g and u again, and dh; from them h, dg and du
     ProductArgs b;
@@ -504,6 +530,8 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     b.sums = dw->gate_bias || dw->up_bias ? (float *)(ws + f.sums) : nullptr;
     b.act = d->activation;
     b.lo = f.two;
+    b.sizes = f.half ? (const float *)(ws + f.sizes) : nullptr;
+    b.scales = scales;
     if (f.thin) {
       b.c = dx;
       b.ldc = dx_stride;
@@ -529,6 +557,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     e.K = d->hidden;
     e.c = dx;
     e.ldc = dx_stride;
+    e.scale = scales;
     if (!f.thin && (rc = launched(launch_product(e, PRODUCT_ROWS, t, f.dx.tile, stream), "gradient of x")))
       return rc;
   }
@@ -536,7 +565,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
   auto weights = [&](const void *pa, const void *pa2, int64_t lda, int64_t m, const void *pb,
                      const void *pb2, int64_t ldb, int32_t n,
                      const ProductPlan &plan, void *c, void *c2, int64_t c_rows, int64_t valid,
-                     bool sums, const char *what) {
+                     bool sums, const float *scale, const char *what) {
     ProductArgs a;
     a.a[0] = pa;
     a.a[1] = pa2;
@@ -555,6 +584,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     a.c = c;
     a.c2 = c2;
     a.ldc = n;
+    a.scale = scale;
     if (sums) a.sums = (float *)(ws + f.dy_sums);
     if (plan.splits == 1)
       return launched(launch_product(a, PRODUCT_WEIGHTS, t, plan.tile, stream), what);
@@ -580,10 +610,10 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
   const bool dy_sums = product_sums(f.dd.tile) && !f.two;  // which goes through dy twice
   if ((rc = weights(g, g2, 2 * hp * times, 2 * hp, f.x.p, f.x.p, f.x.stride, d->in_features, f.dgu,
                     (void *)dw->gate, (void *)dw->up, hp, d->hidden, false,
-                    "gradients of gate and up")) ||
+                    scales, "gradients of gate and up")) ||
       (rc = weights(f.dy.p, f.dy.p, f.dy.stride, d->out_features, h, h2, hp * times, d->hidden,
                     f.dd, (void *)dw->down, (void *)dw->down, d->out_features, d->out_features,
-                    dw->down_bias && dy_sums, "gradient of down")))
+                    dw->down_bias && dy_sums, scales ? scales + 1 : nullptr, "gradient of down")))
     return rc;
   SumArgs s;
   s.y_type = t;
