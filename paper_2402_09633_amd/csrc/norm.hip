@@ -3,8 +3,8 @@
 //
 // A row's values stay in registers between the reductions: L lanes of a wave
 // hold a row of up to 2048 (C units of eight each), a workgroup of 512 a wider
-// one.  The mean and the sum of squares around it are two passes over the
-// registers, so that a large mean costs no digits.
+// one.  The mean, and then its error and the sum of squares around it, are two
+// passes over the registers, so that a large mean costs no digits.
 //
 // Bound by memory: x is read and y written once forward; x and dy read and dx
 // written backward, whose parameter gradients stay in registers until a workgroup
@@ -112,25 +112,30 @@ __global__ __launch_bounds__(WIDE ? LN_WIDE : 64 * LN_WAVES) void layer_norm(Lay
 #pragma unroll
       for (int j = 0; j < 8; ++j) s[0] += x[c][j];
     row_sum<1, WIDE>(s, at.L, part, turn);
-    const float mean = s[0] / (float)K;  // a constant row deviates by nothing
-    s[0] = 0.f;
+    const float first = s[0] / (float)K;
+    float t[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float d = x[c][j] - mean;
+        const float d = x[c][j] - first;
         x[c][j] = d;
-        s[0] += FULL || 8 * (at.u0 + at.L * c) + j < K ? d * d : 0.f;
+        const float e = FULL || 8 * (at.u0 + at.L * c) + j < K ? d : 0.f;
+        t[0] += e * e;
+        t[1] += e;
       }
-    row_sum<1, WIDE>(s, at.L, part, turn);
-    const float rstd = 1.f / sqrtf(s[0] * inv + a.eps);
+    row_sum<2, WIDE>(t, at.L, part, turn);
+    // The sum's roundings leave `first` off by some last places; the deviations' own mean
+    // says by how much.  So a constant row deviates by nothing.
+    const float off = t[1] * inv, mean = first + off, shift = mean - first;
+    const float rstd = 1.f / sqrtf(fmaxf(t[0] * inv - off * off, 0.f) + a.eps);
     if (!in) continue;
     elem_t<T> *y = (elem_t<T> *)a.y + r * a.y_stride;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       f8 v;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = x[c][j] * rstd * gamma[c][j] + beta[c][j];
+      for (int j = 0; j < 8; ++j) v[j] = (x[c][j] - shift) * rstd * gamma[c][j] + beta[c][j];
       store8<T>(y, 8 * (at.u0 + at.L * c), K, v);
     }
     if (at.u0 == 0 && a.mean) {
