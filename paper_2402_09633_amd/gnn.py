@@ -956,7 +956,8 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, gamma: torch.Tensor,
 
 
 def _gated_args(x, w_gate, w_up, w_down, biases, activation, dev):
-    """(dims, weights, address and stride of x, whether everything is aligned)."""
+    """(dims, weights, address and stride of x, the three biases, whether everything is
+    aligned)."""
     xa, xt, xs = _rows("x", x, None, None, dev)
     if xt not in (GNN_BF16, GNN_F16):
         raise TypeError(f"x: rows of {x.dtype} are not supported, bfloat16 and float16 are")
@@ -982,7 +983,7 @@ def _gated_args(x, w_gate, w_up, w_down, biases, activation, dev):
     dims = make_gated_dims(k, hidden, n_out, xt, act)
     ptrs = (w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr())
     weights = gnn_gated_weights(ctypes.sizeof(gnn_gated_weights), *ptrs, *ba)
-    return dims, weights, xa, xs, _lies_aligned(xa, xs) and all(p % 16 == 0 for p in ptrs)
+    return dims, weights, xa, xs, b, _lies_aligned(xa, xs) and all(p % 16 == 0 for p in ptrs)
 
 
 def _lies_aligned(address: int, stride: int) -> bool:
@@ -998,7 +999,8 @@ def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: tor
     if where is not None:
         with where:
             return gated(x, w_gate, w_up, w_down, biases, activation, out)
-    dims, weights, xa, xs, aligned = _gated_args(x, w_gate, w_up, w_down, biases, activation, dev)
+    dims, weights, xa, xs, _, aligned = _gated_args(x, w_gate, w_up, w_down, biases, activation,
+                                                    dev)
     n = x.shape[0]
     out, ya, ys = _like("out", x, dims.out_features, out, dev)
     nb = lib.gnn_gated_workspace(dims, n, 0, aligned)
@@ -1016,15 +1018,15 @@ def gated_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up
     if where is not None:
         with where:
             return gated_backward(dy, x, w_gate, w_up, w_down, biases, activation, out)
-    dims, weights, xa, xs, aligned = _gated_args(x, w_gate, w_up, w_down, biases, activation, dev)
+    dims, weights, xa, xs, biases, aligned = _gated_args(x, w_gate, w_up, w_down, biases,
+                                                         activation, dev)
     n = x.shape[0]
     da, dt, ds = _rows("dy", dy, dims.out_features, n, dev)
     if dt != dims.dtype:
         raise TypeError(f"dy: expected {x.dtype}, got {dy.dtype}")
     out, oa, os_ = _like("out", x, dims.in_features, out, dev)
     grads = [torch.empty_like(w) for w in (w_gate, w_up, w_down)]
-    grads += [None if b is None else torch.empty_like(b)
-              for b in (biases if biases is not None else (None, None, None))]
+    grads += [None if b is None else torch.empty_like(b) for b in biases]
     into = gnn_gated_weights(ctypes.sizeof(gnn_gated_weights), *map(_addr, grads))
     nb = lib.gnn_gated_workspace(dims, n, 1, aligned and _lies_aligned(da, ds))
     ws = _scratch(nb, dev)
