@@ -115,3 +115,29 @@ def test_zero_gradients(G):
         assert (t == 0).all()
     for t in G.gated_backward(dy, torch.zeros_like(x), *w)[1:4]:
         assert (t == 0).all()
+
+
+def test_the_range_is_found_again_in_a_replay(G):
+    """A captured call takes its powers of two from the numbers of each replay."""
+    sizes = ((9, 64, 96, 32), (300, 64, 96, 40), (300, 37, 75, 29), (33_000, 64, 96, 32))
+    held = [_scaled(*s, 9, 1.0, 1.0) for s in sizes]
+    for x, w, b, dy in held:
+        G.gated_backward(dy, x, *w)
+    torch.cuda.synchronize()
+    graphs, outs, pool = [], [], torch.cuda.graph_pool_handle()
+    for x, w, b, dy in held:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, pool=pool):
+            outs.append(G.gated_backward(dy, x, *w)[:4])
+        graphs.append(g)
+    for turn, (x_by, dy_by) in enumerate(((1.0, 1e-5), (30.0, 1.0), (1e-2, 1e-3), (1.0, 1.0))):
+        for s, (x, w, b, dy), g, out in zip(sizes, held, graphs, outs):
+            fresh = _scaled(*s, 10 + turn, x_by, dy_by)
+            for t, v in zip([x, *w, dy], [fresh[0], *fresh[1], fresh[3]]):
+                t.copy_(v)
+            g.replay()
+            got = [t.clone() for t in out]
+            torch.cuda.synchronize()
+            assert all(torch.equal(p, q) for p, q in zip(got, G.gated_backward(dy, x, *w)[:4]))
+            for have, (v, e) in zip(got, F.gated_backward(dy, x, w, b, "silu")):
+                _held(have, v, e)
