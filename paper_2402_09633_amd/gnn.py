@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import warnings
 
 import numpy as np
 import torch  # imported first so that libgnn.so binds to the HIP runtime torch loaded
@@ -876,6 +877,16 @@ class Mlp(_RowsHandle):
 
 
 # ---- training operators ----
+# None of them records an autograd graph: gradients are what the *_backward calls return.
+
+
+def _no_graph(name: str, *tensors):
+    """Says so where a result stands in a graph that autograd would go back through:
+    beside a residual connection, say, nothing else would tell."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        warnings.warn(f"{name} records no autograd graph, though an argument requires grad: use "
+                      f"{name}_backward, and torch.no_grad() or detach() here", stacklevel=3)
+
 
 _ACTIVATIONS = {"silu": GNN_SILU, "gelu": GNN_GELU, "sigmoid": GNN_SIGMOID, "relu": GNN_RELU}
 
@@ -911,7 +922,8 @@ def _float_rows(what: str, t, width=None, n=None, device=None):
 def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: float = 1e-5,
                out=None, save: bool = False, stream=None):
     """The layer norm of x's rows, of x's type; with ``save`` (y, mean, rstd), which
-    ``layer_norm_backward`` takes.  gamma, beta: fp32.  ``out`` may be x."""
+    ``layer_norm_backward`` takes.  gamma, beta: fp32.  ``out`` may be x.  No autograd graph
+    is recorded."""
     dev, where = _elsewhere("x", x, stream)
     if where is not None:
         with where:
@@ -920,6 +932,7 @@ def layer_norm(x: torch.Tensor, gamma: torch.Tensor, beta: torch.Tensor, eps: fl
     n, k = x.shape
     ga = _vector("gamma", gamma, torch.float32, k, dev)
     ba = _vector("beta", beta, torch.float32, k, dev)
+    _no_graph("layer_norm", x, gamma, beta)
     out, ya, ys = _like("out", x, k, out, dev)
     mean = rstd = None
     if save:
@@ -994,13 +1007,15 @@ def gated(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: tor
           biases=None, activation: str = "silu", out=None, stream=None) -> torch.Tensor:
     """A gated feed-forward block: act(x w_gate^T + b) * (x w_up^T + b) through w_down.
     Rows, weights and biases (of gate, up and down) bfloat16 or float16; activation
-    "silu", "gelu", "sigmoid" or "relu"."""
+    "silu", "gelu", "sigmoid" or "relu".  No autograd graph is recorded
+    (``gated_backward``)."""
     dev, where = _elsewhere("x", x, stream)
     if where is not None:
         with where:
             return gated(x, w_gate, w_up, w_down, biases, activation, out)
-    dims, weights, xa, xs, _, aligned = _gated_args(x, w_gate, w_up, w_down, biases, activation,
-                                                    dev)
+    dims, weights, xa, xs, biases, aligned = _gated_args(x, w_gate, w_up, w_down, biases,
+                                                         activation, dev)
+    _no_graph("gated", x, w_gate, w_up, w_down, *biases)
     n = x.shape[0]
     out, ya, ys = _like("out", x, dims.out_features, out, dev)
     nb = lib.gnn_gated_workspace(dims, n, 0, aligned)

@@ -1,4 +1,6 @@
 """How the training operators take their arguments."""
+import warnings
+
 import pytest
 import torch
 
@@ -26,3 +28,21 @@ def test_biases_may_come_from_an_iterator(G, stream):
         y = G.gated(x, *w, biases=iter(some), stream=stream)
         torch.cuda.synchronize()
         assert torch.equal(y, G.gated(x, *w, biases=some))
+
+
+def test_no_graph_is_recorded_in_silence(G):
+    """x + gated(layer_norm(x)) would go back through x alone."""
+    x, w, b, _ = make(20, 32, 24, 32, torch.bfloat16, 1)
+    gamma, beta = torch.ones(32, device="cuda"), torch.zeros(32, device="cuda")
+    calls = {"layer_norm": ([x, gamma, beta], lambda a: G.layer_norm(*a)),
+             "gated": ([x, *w, *b], lambda a: G.gated(*a[:4], biases=a[4:]))}
+    for name, (args, call) in calls.items():
+        for i, leaf in enumerate(args):
+            some = [t.clone().requires_grad_() if t is leaf else t for t in args]
+            with pytest.warns(UserWarning, match=f"{name} records no autograd graph.*{name}_backward"):
+                assert not call(some).requires_grad
+            with warnings.catch_warnings():
+                warnings.simplefilter("error")
+                with torch.no_grad():
+                    call(some)
+                call([t.detach() for t in some])
