@@ -505,8 +505,8 @@ int gnn_gated_backward(const gnn_gated_dims *dims, const gnn_gated_weights *weig
 /* Gradient clipping: *norm (device, fp32) = the square root of the sum of all
  * elements' squares, over all tensors, in fp64; out = grad min(1, max_norm /
  * (norm + 1e-6)), which is NaN everywhere if the norm is.  out may be grad;
- * otherwise no output may overlap another tensor (checked).  Tensors are
- * contiguous; some may be empty.  Up to 2^37 elements in all. */
+ * otherwise no output, norm among them, may overlap another tensor (checked).
+ * Tensors are contiguous; some may be empty.  Up to 2^37 elements in all. */
 typedef struct gnn_grad {
   const void *grad;
   void *out;

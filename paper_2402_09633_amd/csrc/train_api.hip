@@ -672,15 +672,16 @@ int check_grads(const gnn_grad *g, int32_t n) {
   return GNN_OK;
 }
 
-// Every output has to lie apart from the others and from the gradients, but for
-// its own where it takes its place.
-int check_apart(const gnn_grad *g, int32_t n) {
+// Every output, the norm among them, has to lie apart from the others and from the
+// gradients, but for its own where it takes its place.
+int check_apart(const gnn_grad *g, int32_t n, const float *norm) {
   struct Span {
     uintptr_t lo, hi;
     bool out;
   };
   std::vector<Span> spans;
-  spans.reserve(2 * (size_t)n);
+  spans.reserve(2 * (size_t)n + 1);
+  spans.push_back({(uintptr_t)norm, (uintptr_t)(norm + 1), true});
   for (int32_t i = 0; i < n; ++i) {
     if (g[i].count == 0) continue;
     const uintptr_t bytes = (uintptr_t)g[i].count * type_bytes(g[i].type);
@@ -719,7 +720,7 @@ int gnn_clip_grads(const gnn_grad *grads, int32_t n_grads, float max_norm, float
   if ((rc = check_scratch(workspace, workspace_bytes, gnn_clip_workspace(grads, n_grads))))
     return rc;
   try {
-    if ((rc = check_apart(grads, n_grads))) return rc;
+    if ((rc = check_apart(grads, n_grads, norm))) return rc;
     std::vector<ClipList> lists;
     for (int32_t i = 0; i < n_grads; ++i) {
       if (grads[i].count == 0) continue;
