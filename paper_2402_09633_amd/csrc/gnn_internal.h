@@ -557,7 +557,7 @@ struct JoinArgs {
 hipError_t launch_join(const JoinArgs &a, int type, hipStream_t stream);
 
 // Column sums of a table (norm.hip): sums [width] of rows of any float type, to
-// up to three outputs of one type: columns [0, split) to y[0], [skip, skip +
+// up to two outputs of one type: columns [0, split) to y[0], [skip, skip +
 // split) to y[1].
 struct SumArgs {
   const void *x = nullptr;
@@ -569,7 +569,8 @@ struct SumArgs {
   void *y[2] = {nullptr, nullptr};
   int32_t y_type = 0, split = 0, skip = 0;
 };
-size_t colsum_scratch(int64_t n, int32_t width);
+// as_parts: the rows are fp32 without gaps between them
+size_t colsum_scratch(int64_t n, int32_t width, bool as_parts);
 hipError_t launch_colsum(const SumArgs &a, hipStream_t stream);
 
 // Layer norm of rows and its gradients (norm.hip).

@@ -379,16 +379,26 @@ hipError_t launch_layer_norm_backward(const LayerNormArgs &a, hipStream_t stream
   return ln(a, true, stream);
 }
 
-size_t colsum_scratch(int64_t n, int32_t width) { return (size_t)SUM_PARTS * width * 4; }
+namespace {
+// Rows of partial sums that are written first: none of up to SUM_DIRECT rows that lie as
+// such do (fp32, without gaps).
+int64_t colsum_parts(int64_t n, int32_t width, bool as_parts) {
+  if (n == 0 || (as_parts && n <= SUM_DIRECT)) return 0;
+  const int64_t rows = LN_WAVES * (64 / lanes_of((width + 7) / 8)) * 4;
+  return std::min<int64_t>((n + rows - 1) / rows, SUM_PARTS);
+}
+}  // namespace
+
+size_t colsum_scratch(int64_t n, int32_t width, bool as_parts) {
+  return (size_t)colsum_parts(n, width, as_parts) * width * 4;
+}
 
 hipError_t launch_colsum(const SumArgs &a, hipStream_t stream) {
   const float *part = (const float *)a.x;
   int64_t n = a.n;
-  if (n > SUM_DIRECT || (n > 0 && (a.x_type != T_F32 || a.x_stride != a.width))) {
+  if (const int64_t parts = colsum_parts(n, a.width, a.x_type == T_F32 && a.x_stride == a.width)) {
     const int L = lanes_of((a.width + 7) / 8);
-    const int64_t rows = LN_WAVES * (64 / L) * 4;
-    const dim3 grid((unsigned)std::min<int64_t>((n + rows - 1) / rows, SUM_PARTS),
-                    (unsigned)((a.width + 511) / 512));
+    const dim3 grid((unsigned)parts, (unsigned)((a.width + 511) / 512));
     const dim3 block(64 * LN_WAVES);
     const hipError_t e = a.x_type == T_F32    ? launch(column_parts<T_F32>, grid, block, 0, stream, a, L)
                          : a.x_type == T_BF16 ? launch(column_parts<T_BF16>, grid, block, 0, stream, a, L)

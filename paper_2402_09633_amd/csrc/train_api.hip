@@ -149,8 +149,8 @@ int gnn_layer_norm(const void *x, int32_t type, int64_t x_stride, int64_t n_rows
 
 size_t gnn_layer_norm_workspace(int64_t n_rows, int32_t width) {
   if (n_rows < 0 || n_rows > MAX_ROWS || width < 1 || width > MAX_WIDTH) return 0;
-  return up256((size_t)layer_norm_parts(n_rows, width) * 2 * width * 4) +
-         up256(colsum_scratch(layer_norm_parts(n_rows, width), 2 * width));
+  const int64_t parts = layer_norm_parts(n_rows, width);
+  return up256((size_t)parts * 2 * width * 4) + up256(colsum_scratch(parts, 2 * width, true));
 }
 
 int gnn_layer_norm_backward(const void *dy, int64_t dy_stride, const void *x, int64_t x_stride,
@@ -313,10 +313,11 @@ struct GatedBackward {
   Operand x, dy, gate, up, down;
   ProductPlan grad, dx, dgu, dd;
   // two: h, dg and du in two 16-bit numbers (few rows, as gated_few)
-  bool thin = false, two = false;
+  // dy_sums: dy's sums over rows come with the down projection's gradient
+  bool thin = false, two = false, dy_sums = false;
   // half: fp16, whose h, dg and du are multiplied by powers of two
   bool half = false;
-  size_t h = 0, g = 0, part = 0, sums = 0, dy_sums = 0, colsum = 0, sizes = 0, scales = 0;
+  size_t h = 0, g = 0, part = 0, sums = 0, dy_sum = 0, colsum = 0, sizes = 0, scales = 0;
   int64_t sum_rows = 0;
   Carve c;
   GatedBackward(const gnn_gated_dims &d, int64_t n, int n_cu, const void *xp, int64_t x_ld,
@@ -342,12 +343,14 @@ struct GatedBackward {
     if (dd.splits > 1) most = std::max(most, (size_t)dd.splits * d.out_features * hp * 4);
     part = c.take(most);
     thin = thin_fits(n, d.in_features, d.hidden, d.out_features, n_cu);
-    // sums of dg and du over rows, and of dy with the down projection's gradient
+    // sums of dg and du over rows
     sum_rows = thin ? thin_sum_rows(n) : product_sum_rows(grad.tile, n);
     sums = c.take((size_t)sum_rows * 2 * hp * 4);
-    dy_sums = c.take((size_t)dd.splits * d.out_features * 4);
-    colsum = c.take(std::max(colsum_scratch(sum_rows, (int32_t)(2 * hp)),
-                             colsum_scratch(n, d.out_features)));
+    dy_sum = c.take((size_t)dd.splits * d.out_features * 4);
+    dy_sums = product_sums(dd.tile) && !two;  // which goes through dy twice
+    colsum = c.take(std::max(colsum_scratch(sum_rows, (int32_t)(2 * hp), true),
+                             dy_sums ? colsum_scratch(dd.splits, d.out_features, true)
+                                     : colsum_scratch(n, d.out_features, false)));
     if ((half = d.dtype == GNN_F16 && n > 0)) {
       sizes = c.take(SIZES * SIZE_PARTS * 4);
       scales = c.take(2 * 4);
@@ -585,7 +588,7 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     a.c2 = c2;
     a.ldc = n;
     a.scale = scale;
-    if (sums) a.sums = (float *)(ws + f.dy_sums);
+    if (sums) a.sums = (float *)(ws + f.dy_sum);
     if (plan.splits == 1)
       return launched(launch_product(a, PRODUCT_WEIGHTS, t, plan.tile, stream), what);
     a.c = ws + f.part;
@@ -607,13 +610,12 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
   };
   const unsigned char *g2 = (unsigned char *)g + 2 * hp * 2, *h2 = (unsigned char *)h + hp * 2;
   const int64_t times = f.two ? 2 : 1;
-  const bool dy_sums = product_sums(f.dd.tile) && !f.two;  // which goes through dy twice
   if ((rc = weights(g, g2, 2 * hp * times, 2 * hp, f.x.p, f.x.p, f.x.stride, d->in_features, f.dgu,
                     (void *)dw->gate, (void *)dw->up, hp, d->hidden, false,
                     scales, "gradients of gate and up")) ||
       (rc = weights(f.dy.p, f.dy.p, f.dy.stride, d->out_features, h, h2, hp * times, d->hidden,
                     f.dd, (void *)dw->down, (void *)dw->down, d->out_features, d->out_features,
-                    dw->down_bias && dy_sums, scales ? scales + 1 : nullptr, "gradient of down")))
+                    dw->down_bias && f.dy_sums, scales ? scales + 1 : nullptr, "gradient of down")))
     return rc;
   SumArgs s;
   s.y_type = t;
@@ -629,8 +631,8 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     if ((rc = sum_columns(s, ws + f.colsum, "bias gradients", stream))) return rc;
   }
   if (dw->down_bias) {
-    const bool there = dy_sums;  // dy itself otherwise
-    s.x = there ? ws + f.dy_sums : dy;
+    const bool there = f.dy_sums;  // dy itself otherwise
+    s.x = there ? ws + f.dy_sum : dy;
     s.x_type = there ? GNN_FP32 : t;
     s.x_stride = there ? d->out_features : dy_stride;
     s.n = there ? f.dd.splits : n_rows;
