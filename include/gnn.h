@@ -683,6 +683,17 @@ size_t gnn_debug_frnn_bytes(int64_t n_nodes, int32_t dim, int32_t n_slots);
 int gnn_debug_linear(const gnn_linear_dims *dims, int32_t n_cu, int32_t x_type, int64_t n_rows,
                      int32_t grouped, int32_t y_type, int64_t y_stride, int32_t kernel[6]);
 
+/* Which kernels a gnn_gated (backward: gnn_gated_backward) call of these widths and
+ * rows takes on a device of n_cu compute units (needs no device): kernel[0] 1 if
+ * those for few rows, 2 if the one for narrow rows, 0 if tiles.  Tiles are 0 (128 x
+ * 128), 1 (256 x 128), 2 (256 x 256) and 3 (128 x 128, four stages on their way), -1
+ * where no tile is taken: kernel[1] of gate and up, or of their gradients;
+ * kernel[2] of down, or of dx (few rows: workgroups that share a column's sums).
+ * Backward, kernel[3] the tile and kernel[4] the parts of the sums over rows of the
+ * gradients of gate and up, kernel[5] and kernel[6] of down's; otherwise 0. */
+int gnn_debug_gated(const gnn_gated_dims *dims, int32_t n_cu, int64_t n_rows, int32_t backward,
+                    int32_t kernel[7]);
+
 #ifdef __cplusplus
 }
 #endif

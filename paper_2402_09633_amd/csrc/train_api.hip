@@ -288,6 +288,7 @@ struct GatedForward {
   Operand x, gate, up, down;
   size_t h = 0, part = 0;
   int splits = 1;
+  int gate_tile = 0, down_tile = 0;
   Carve c;
   GatedForward(const gnn_gated_dims &d, int64_t n, int n_cu, const void *xp, int64_t ld, bool x_in,
                const gnn_gated_weights *w, bool w_in)
@@ -304,6 +305,8 @@ struct GatedForward {
       return;
     } else {
       for (Operand *o : {&x, &gate, &up, &down}) o->place(c);
+      gate_tile = product_plan(PRODUCT_GATE, n, d.hidden, d.in_features, n_cu).tile;
+      down_tile = product_plan(PRODUCT_DOWN, n, d.out_features, d.hidden, n_cu).tile;
     }
     h = c.take((size_t)n * up8(d.hidden) * (n <= TWO_ROWS ? 4 : 2));
   }
@@ -434,8 +437,7 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   a.ldc = n_rows <= TWO_ROWS ? 2 * hp : hp;
   a.lo = n_rows <= TWO_ROWS ? (int32_t)hp : 0;
   rc = launched(f.few ? launch_few(a, true, t, 1, stream)
-                      : launch_product(a, PRODUCT_GATE, t,
-                                       product_plan(PRODUCT_GATE, a.M, a.N, a.K, n_cu).tile, stream),
+                      : launch_product(a, PRODUCT_GATE, t, f.gate_tile, stream),
                 "gate");
   if (rc) return rc;
   ProductArgs b;
@@ -452,9 +454,7 @@ int gnn_gated(const gnn_gated_dims *d, const gnn_gated_weights *w, const void *x
   b.ldc = y_stride;
   b.part = (float *)(ws + f.part);
   return launched(f.few ? launch_few(b, false, t, f.splits, stream)
-                        : launch_product(b, PRODUCT_DOWN, t,
-                                         product_plan(PRODUCT_DOWN, b.M, b.N, b.K, n_cu).tile,
-                                         stream),
+                        : launch_product(b, PRODUCT_DOWN, t, f.down_tile, stream),
                   "down projection");
 }
 
@@ -641,6 +641,30 @@ int gnn_gated_backward(const gnn_gated_dims *d, const gnn_gated_weights *w, cons
     s.y[1] = nullptr;
     return sum_columns(s, ws + f.colsum, "bias gradients", stream);
   }
+  return GNN_OK;
+}
+
+int gnn_debug_gated(const gnn_gated_dims *d, int32_t n_cu, int64_t n_rows, int32_t backward,
+                    int32_t kernel[7]) {
+  int rc = check_gated_dims(d);
+  if (rc || (rc = check_rows(n_rows))) return rc;
+  if (n_rows == 0 || n_cu < 1 || !kernel) return bad(GNN_E_INVALID_ARG, "bad arguments");
+  for (int i = 0; i < 7; ++i) kernel[i] = 0;
+  if (!backward) {
+    const GatedForward f(*d, n_rows, n_cu, nullptr, 0, true, nullptr, true);
+    kernel[0] = f.few ? 1 : f.thin ? 2 : 0;
+    kernel[1] = f.few || f.thin ? -1 : f.gate_tile;
+    kernel[2] = f.few ? f.splits : f.thin ? -1 : f.down_tile;
+    return GNN_OK;
+  }
+  const GatedBackward f(*d, n_rows, n_cu, nullptr, 0, nullptr, 0, true, nullptr, true);
+  kernel[0] = f.thin ? 2 : 0;
+  kernel[1] = f.thin ? -1 : f.grad.tile;
+  kernel[2] = f.thin ? -1 : f.dx.tile;
+  kernel[3] = f.dgu.tile;
+  kernel[4] = f.dgu.splits;
+  kernel[5] = f.dd.tile;
+  kernel[6] = f.dd.splits;
   return GNN_OK;
 }
 

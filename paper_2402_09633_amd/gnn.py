@@ -55,7 +55,7 @@ EXPORTS = ("gnn_weight_count", "gnn_create", "gnn_infer", "gnn_infer_logits", "g
            "gnn_mlp_workspace", "gnn_mlp_apply", "gnn_mlp_destroy", "gnn_last_error_code",
            "gnn_debug_linear", "gnn_layer_norm", "gnn_layer_norm_workspace",
            "gnn_layer_norm_backward", "gnn_gated_workspace", "gnn_gated", "gnn_gated_backward",
-           "gnn_clip_workspace", "gnn_clip_grads")
+           "gnn_clip_workspace", "gnn_clip_grads", "gnn_debug_gated")
 STAGES = ("csr", "node_enc", "edge_enc", "edge_update", "aggregate", "node_update",
           "classifier", "total")
 
@@ -272,6 +272,8 @@ def _load():
     L.gnn_gated.argtypes = [gdp, gwp, vp, i64, i64, vp, i64, vp, i64, vp]
     L.gnn_gated_backward.restype = ctypes.c_int
     L.gnn_gated_backward.argtypes = [gdp, gwp, vp, i64, vp, i64, i64, vp, i64, gwp, vp, i64, vp]
+    L.gnn_debug_gated.restype = ctypes.c_int
+    L.gnn_debug_gated.argtypes = [gdp, i32, i64, i32, ctypes.POINTER(ctypes.c_int32)]
     L.gnn_clip_workspace.restype = ctypes.c_size_t
     L.gnn_clip_workspace.argtypes = [vp, i32]
     L.gnn_clip_grads.restype = ctypes.c_int
@@ -1048,6 +1050,13 @@ def gated_backward(dy: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up
     _check(lib.gnn_gated_backward(dims, weights, da, ds, xa, xs, n, oa, os_, into, _addr(ws), nb,
                                   _raw_stream(dev.index)))
     return (out, *grads)
+
+
+def gnn_debug_gated(dims: gnn_gated_dims, n_cu: int, n_rows: int, backward=False) -> tuple:
+    """The C call's kernel[0 .. 6]."""
+    k = (ctypes.c_int32 * 7)()
+    _check(lib.gnn_debug_gated(dims, n_cu, n_rows, int(backward), k))
+    return tuple(k)
 
 
 _FLOATS = frozenset((torch.float32, torch.bfloat16, torch.float16))
