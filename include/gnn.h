@@ -430,9 +430,8 @@ int gnn_mlp_apply(gnn_mlp *m, const void *x, int32_t x_type, int64_t x_stride,
 void gnn_mlp_destroy(gnn_mlp *m); /* waits for the device; NULL-safe */
 
 /* ---- training operators ---------------------------------------------------
- * What networks of the layers above are trained with: layer norm and its
- * gradients, the gated feed-forward block and its gradients, and the global norm
- * of the gradients with clipping.
+ * Layer norm and its gradients, a gated feed-forward block and its gradients, and
+ * the global norm of gradients with clipping.
  *
  * The rules of the row operators hold: tables are a pointer and a stride in
  * elements, of any alignment that their elements have; up to 2^28 rows, widths
@@ -444,7 +443,7 @@ void gnn_mlp_destroy(gnn_mlp *m); /* waits for the device; NULL-safe */
  * these; nothing is enqueued then. */
 
 /* y = gamma (x - mean) rstd + beta over each row's `width` elements, rstd = 1 /
- * sqrt(variance + eps).  x and y of one float type; gamma, beta [width] fp32.
+ * sqrt(variance + eps), 0 < eps < 1.  x and y of one float type; gamma, beta [width] fp32.
  * mean and rstd [n_rows] fp32 keep what the backward pass needs (both or
  * neither NULL).  All sums in fp32, the variance around the mean.  y may be x
  * (with its stride). */

@@ -1,8 +1,8 @@
 // The global norm of many tensors, and their scaling.  Both read everything
 // once, so HBM bounds them; a list of tensors goes with the launch's arguments,
 // and every workgroup takes CLIP_TILE elements of one of them.  302M bf16 elements in
-// 192 tensors: squares 146 us (4.1 TB/s), the norm 6, scaling 215 (5.6 TB/s, some of
-// it from the last-level cache), 342 a call.
+// 192 tensors, 341 us a call; under a profiler, which slows them, squares 146 us (4.1
+// TB/s), the norm 6 and scaling 213 (5.7 TB/s, some of it from the last-level cache).
 #include "rows_common.h"
 
 namespace gnn {

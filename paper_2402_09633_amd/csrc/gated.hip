@@ -1206,7 +1206,8 @@ __global__ __launch_bounds__(64) void few_join(ProductArgs a, int32_t parts, int
 
 // Tables that the products cannot read as they lie (at odd addresses, or with rows
 // of odd lengths) to aligned rows with zeros behind them, all in one launch (63 x 65
-// -> 523 -> 8 forward and backward: 50 us, with a launch to each 60).
+// -> 523 -> 8 bf16 forward and backward: 51 us; with a launch to each 10 more).  The
+// backward pass of fp16 copies them in gated_sizes.
 template <int T>
 __global__ __launch_bounds__(256) void pack_tables(PackArgs a) {
   typedef elem_t<T> E;
@@ -1349,13 +1350,20 @@ ProductPlan product_plan(int kind, int64_t M, int64_t N, int64_t K, int n_cu) {
     return ((M + tm - 1) / tm) * ((N + tn - 1) / tn);
   };
   // The tile whose rounds over the chip take least; a round's cost is next to that of
-  // two workgroups of 128 x 128 on a CU.  us of a forward / backward call by the rule,
-  // and with 128 x 128, 256 x 128, 256 x 256 and four stages of 128 x 128 throughout:
+  // two workgroups of 128 x 128 on a CU.  us of a forward / backward bf16 call by the
+  // rule, and with 128 x 128, 256 x 128, 256 x 256 and four stages of 128 x 128 throughout
+  // (one run of all; clocks of other runs differ by some percent):
   // 4097 x 391 -> 1031 -> 259     45 / 115   50 / 124  56 / 136  68 / 165  50 / 119
   // 8192 x 2048 -> 8192 -> 2048   702 / 1987 826 / 2535 732 / 2248 663 / 1981 945 / 2868
   // 1622 x 5084 -> 2893 -> 1191   159 / 485  216 / 560 210 / 537 219 / 503 191 / 550
+  // 4096 x 1024 -> 4096 -> 1024   101 / 427  119 / 381 124 / 388 147 / 526 135 / 397
+  // 1000 x 512 -> 2048 -> 512     32 / 110   36 / 126  43 / 138  64 / 206  32 / 113
   // 30000 x 256 -> 1024 -> 256    77 / 248   81 / 240  87 / 247  86 / 269  114 / 284
+  // 6774 x 1056 -> 32 -> 960      24 / 57    23 / 64   27 / 70   40 / 108  25 / 61
+  // 100000 x 160 -> 320 -> 160    90 / 258   86 / 246  100 / 253 87 / 257  124 / 293
   // 300 x 2048 -> 2048 -> 2048    38 / 99    49 / 119  54 / 129  87 / 227  39 / 103
+  // The rule does not count what writing and joining parts costs, and loses by up to 12%
+  // where that decides (the fourth row backward).
   static constexpr struct {
     int tile, tm, tn, to_cu;
     double cost;

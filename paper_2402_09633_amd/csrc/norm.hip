@@ -8,9 +8,9 @@
 //
 // Bound by memory: x is read and y written once forward; x and dy read and dx
 // written backward, whose parameter gradients stay in registers until a workgroup
-// has done all its rows.  1000513 x 128 fp32 204 us forward (5.0 TB/s), 310 backward
-// (4.95 TB/s) and 7 for joining 1024 workgroups' sums; 8192 x 8192 bf16 61, 92 (4.4
-// TB/s) and 7; 20011 x 391 of a 396 table fp16 14, 17 and 5.4 (2.2 TB/s: rows that
+// has done all its rows.  1000513 x 128 fp32 205 us forward (5.0 TB/s), 309 backward
+// (5.0 TB/s) and 7 for joining 1024 workgroups' sums; 8192 x 8192 bf16 62, 91 (4.4
+// TB/s) and 7; 20011 x 391 of a 396 table fp16 15, 17 and 5.5 (2.1 TB/s: rows that
 // start anywhere, whose 16-byte accesses cross lines, and a quarter of the lanes idle).
 #include "rows_common.h"
 
