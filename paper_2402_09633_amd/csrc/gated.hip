@@ -261,7 +261,7 @@ __device__ __forceinline__ f4 rest4(const f4 &v) {
 // tables that the products cannot read as they lie are copied on the way, as
 // pack_tables does for bf16.  300000 x 128 -> 256 -> 128: 34 us of 549 forward and
 // backward (4.5 TB/s); 8192 x 2048 -> 8192 -> 2048 31 (5.4 TB/s); 48 x 256 -> 1024 -> 256
-// 6.6; 4097 x 391 -> 1031 -> 259, copies among it, 11 (copies alone 5.3).
+// 6.6; 4097 x 391 -> 1031 -> 259, copies among it, 12 (copies alone 5.3).
 template <int T>
 __global__ __launch_bounds__(1024) void gated_sizes(SizeArgs a) {
   typedef elem_t<T> E;
@@ -1445,7 +1445,8 @@ hipError_t launch_pack(PackArgs a, int type, hipStream_t stream) {
 }
 
 hipError_t launch_sizes(SizeArgs a, hipStream_t stream) {
-  // workgroups by the bytes of a table, at most as many as it keeps busy
+  // workgroups by the bytes of a table, one at least, SIZE_PARTS at most in all; those
+  // left over only clear their parts
   int64_t bytes[SIZES], all = 0, last = 0;
   for (int t = 0; t < SIZES; ++t) all += bytes[t] = a.rows[t] * a.width[t] * 2;
   for (int t = 0; t < SIZES; ++t) {
